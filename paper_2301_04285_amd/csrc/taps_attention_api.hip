@@ -1,0 +1,518 @@
+// taps_attention_api.hip -- the C ABI of taps_attention.h: validation, plans
+// and launches.  Host code only sizes and checks.
+#include <algorithm>
+#include <cmath>
+#include <cstdarg>
+#include <cstdio>
+#include <cstring>
+#include <new>
+#include <vector>
+
+#include "taps_attention_internal.h"
+
+namespace {
+
+thread_local char g_last_error[512] = "";
+
+taps_status fail(taps_status st, const char *fmt, ...) {
+    va_list ap;
+    va_start(ap, fmt);
+    vsnprintf(g_last_error, sizeof g_last_error, fmt, ap);
+    va_end(ap);
+    return st;
+}
+
+taps_status launched(hipError_t err, const char *what) {
+    if (err == hipSuccess) return TAPS_OK;
+    return fail(TAPS_ERR_DEVICE, "%s: %s", what, hipGetErrorString(err));
+}
+
+uint32_t size_of(uint32_t dtype) { return dtype == TAPS_F32 ? 4 : 2; }
+
+bool aligned(const void *p, uint64_t bytes) { return ((uintptr_t)p & (bytes - 1)) == 0; }
+
+// ---------------------------------------------------------------------------
+// norm and rotation
+// ---------------------------------------------------------------------------
+
+taps_status check_types(uint32_t dtype, uint32_t weight_dtype, uint32_t dim, uint32_t rotary,
+                        float eps, const float *table) {
+    if (dtype > TAPS_F32) return fail(TAPS_ERR_ARG, "dtype %u is none", dtype);
+    if (weight_dtype != dtype && weight_dtype != TAPS_F32)
+        return fail(TAPS_ERR_ARG, "weight_dtype %u is neither dtype (%u) nor TAPS_F32", weight_dtype,
+                    dtype);
+    if (dim < 1 || dim > TAPS_MAX_HEAD_DIM)
+        return fail(TAPS_ERR_ARG, "head_dim %u outside 1..%u", dim, TAPS_MAX_HEAD_DIM);
+    if (rotary > dim || rotary % 2)
+        return fail(TAPS_ERR_ARG, "rotary_dim %u is odd or above head_dim %u", rotary, dim);
+    if (rotary && !table) return fail(TAPS_ERR_ARG, "rotary_dim is %u but table is NULL", rotary);
+    if (!aligned(table, 4)) return fail(TAPS_ERR_ARG, "table is not aligned to its elements");
+    if (!(eps >= 0.f) || std::isinf(eps)) return fail(TAPS_ERR_ARG, "eps is negative or not finite");
+    return TAPS_OK;
+}
+
+taps_status check_heads(const taps_heads &t, const char *what, uint32_t dtype) {
+    if (!t.data) return fail(TAPS_ERR_ARG, "%s is NULL", what);
+    if (!aligned(t.data, size_of(dtype)))
+        return fail(TAPS_ERR_ARG, "%s is not aligned to its elements", what);
+    return TAPS_OK;
+}
+
+// Whether every row starts at a multiple of four elements.
+bool by_fours(const taps_heads &t, uint32_t dtype) {
+    return aligned(t.data, 4 * size_of(dtype)) && t.stride[0] % 4 == 0 && t.stride[1] % 4 == 0 &&
+           t.stride[2] % 4 == 0;
+}
+
+bool vectors_fit(uint32_t dim, uint32_t rotary, uint32_t weight_dtype, const void *w0, const void *w1,
+                 const float *table) {
+    const uint32_t w = 4 * size_of(weight_dtype);
+    return dim % 8 == 0 && rotary % 8 == 0 && aligned(w0, w) && aligned(w1, w) && aligned(table, 16);
+}
+
+void set_strides(int64_t (&to)[3], const taps_heads &t) {
+    for (int i = 0; i < 3; ++i) to[i] = t.stride[i];
+}
+
+taps_status check_norm_rotate(const taps_norm_rotate_args *a, taps_rows_launch *p) {
+    if (!a) return fail(TAPS_ERR_ARG, "args is NULL");
+    if (taps_status st = check_types(a->dtype, a->weight_dtype, a->head_dim, a->rotary_dim, a->eps,
+                                     a->table))
+        return st;
+    if (!a->q_heads) return fail(TAPS_ERR_ARG, "q_heads is 0");
+    if ((uint64_t)a->q_heads + a->k_heads > (1u << 20))
+        return fail(TAPS_ERR_ARG, "%u + %u heads are too many", a->q_heads, a->k_heads);
+    if ((uint64_t)a->batch * a->tokens >= (1ull << 31))
+        return fail(TAPS_ERR_ARG, "%u x %u tokens are too many", a->batch, a->tokens);
+    if (a->positions) {
+        if (a->position_bytes != 4 && a->position_bytes != 8)
+            return fail(TAPS_ERR_ARG, "position_bytes %u is neither 4 nor 8", a->position_bytes);
+        if (!aligned(a->positions, a->position_bytes))
+            return fail(TAPS_ERR_ARG, "positions is not aligned to its elements");
+    } else if (a->rotary_dim && a->batch && a->tokens &&
+               (a->first_position < 0 || a->first_position > (int64_t)a->n_positions ||
+                a->tokens > a->n_positions - (uint64_t)a->first_position)) {
+        return fail(TAPS_ERR_ARG, "positions %lld .. + %u exceed the table's %u",
+                    (long long)a->first_position, a->tokens, a->n_positions);
+    }
+    *p = taps_rows_launch{};
+    p->weight[0] = a->q_weight, p->weight[1] = a->k_weight;
+    p->norm[0] = a->q_weight != nullptr, p->norm[1] = a->k_weight != nullptr;
+    p->float_weights = a->weight_dtype == TAPS_F32;
+    p->table = a->table;
+    p->positions = a->positions;
+    p->wide_positions = a->position_bytes == 8;
+    p->first = a->first_position;
+    p->batch = a->batch, p->tokens = a->tokens;
+    p->heads[0] = a->q_heads, p->heads[1] = a->k_heads;
+    p->dim = a->head_dim, p->rotary = a->rotary_dim;
+    p->n_positions = a->n_positions;
+    p->eps = a->eps;
+    p->interleaved = a->interleaved != 0;
+    if (!a->k_heads) p->norm[1] = 0;
+    return TAPS_OK;
+}
+
+// ---------------------------------------------------------------------------
+// plans
+// ---------------------------------------------------------------------------
+
+uint64_t up16(uint64_t v) { return (v + 15) & ~15ull; }
+
+struct Layout {
+    std::vector<taps_plan_seq> seqs;
+    std::vector<taps_plan_item> items;
+    std::vector<taps_plan_join> joins;
+    taps_plan_header head{};
+};
+
+// Query rows that share their keys' loads, before they are split over the keys.
+struct Strip {
+    int32_t seq, row0, rows, lo, hi;
+    bool narrow;
+    // what a key costs: a narrow item waits for its bytes, which come to a
+    // compute unit at about half the rate at which a wide one works keys off
+    int64_t cost() const { return (int64_t)(hi - lo) * (narrow ? 2 : 1); }
+};
+
+// Keys below which a strip is not split further, and the pieces per compute
+// unit that the whole step is cut into.
+constexpr int64_t kLeastPiece = 256;
+constexpr int64_t kPiecesPerUnit = 2;
+
+taps_status lay_out(const taps_paged_batch *b, uint32_t cus, Layout *out) {
+    taps_plan_header &h = out->head;
+    const uint32_t group = b->q_heads / b->kv_heads;
+    const uint32_t log2 = (uint32_t)__builtin_ctz(b->page_size);
+    uint64_t tokens = 0, pages = 0;
+    int64_t most = 0;
+    bool appendable = true;
+    std::vector<int32_t> written;
+    std::vector<Strip> strips;
+    out->seqs.reserve(b->n_seqs);
+    for (uint32_t s = 0; s < b->n_seqs; ++s) {
+        const int64_t n = b->q_lens[s], kv = b->kv_lens[s], from = b->kv_starts ? b->kv_starts[s] : 0;
+        if (n < 0 || kv < 0 || n > (1 << 30) || kv > (1 << 30))
+            return fail(TAPS_ERR_ARG, "sequence %u: lengths %lld and %lld outside 0..2^30", s,
+                        (long long)n, (long long)kv);
+        if (from < 0 || from > kv)
+            return fail(TAPS_ERR_ARG, "sequence %u: its keys start at %lld of %lld", s,
+                        (long long)from, (long long)kv);
+        const int64_t n_pages = (kv + b->page_size - 1) >> log2;
+        if (n_pages > b->pages_stride)
+            return fail(TAPS_ERR_ARG, "sequence %u: %lld keys need %lld pages of %u", s,
+                        (long long)kv, (long long)n_pages, b->pages_stride);
+        if (n * group > (1 << 30))
+            return fail(TAPS_ERR_ARG, "sequence %u: %lld tokens x %u heads are too many", s,
+                        (long long)n, group);
+        const int32_t *row = b->pages + (uint64_t)s * b->pages_stride;
+        for (int64_t g = from >> log2; g < n_pages; ++g)
+            if (from < kv && (row[g] < 0 || (uint32_t)row[g] >= b->n_pages))
+                return fail(TAPS_ERR_ARG, "sequence %u: page %d outside 0..%u", s, row[g],
+                            b->n_pages);
+        const int64_t first = std::max(kv - n, from);   // first appended position
+        for (int64_t g = std::max<int64_t>(first, 0) >> log2; g < n_pages; ++g)
+            if (n && first < kv) written.push_back(row[g]);
+        if (kv < n) appendable = false;
+        if (n) most = std::max(most, kv);
+        taps_plan_seq q{};
+        q.token0 = (int32_t)tokens;
+        q.rows = (int32_t)(n * group);
+        q.kv_start = (int32_t)from, q.kv_len = (int32_t)kv;
+        q.first_pos = (int32_t)(kv - n);
+        q.page0 = (int32_t)pages;
+        out->seqs.push_back(q);
+        tokens += (uint64_t)n;
+        pages += (uint64_t)n_pages;
+        if (tokens >= (1ull << 31) || pages >= (1ull << 31))
+            return fail(TAPS_ERR_ARG, "2^31 or more tokens or pages in all");
+        const bool narrow = q.rows <= kNarrowRows;
+        const int32_t step = narrow ? kNarrowRows : kWideRows;
+        // rows that see the most keys first: the last to start are the shortest
+        for (int32_t r = q.rows ? (q.rows - 1) / step * step : -1; r >= 0; r -= step) {
+            Strip t{(int32_t)s, r, std::min(step, q.rows - r), (int32_t)from, (int32_t)kv, narrow};
+            if (b->causal) {
+                const int64_t pos_a = q.first_pos + r / (int64_t)group;
+                const int64_t pos_b = q.first_pos + (r + t.rows - 1) / (int64_t)group;
+                t.hi = (int32_t)std::max<int64_t>(std::min<int64_t>(kv, pos_b + 1), 0);
+                if (h.window)
+                    t.lo = (int32_t)std::max<int64_t>(t.lo, pos_a - (int64_t)h.window + 1);
+            }
+            if (t.hi < t.lo) t.hi = t.lo;
+            strips.push_back(t);
+        }
+    }
+    std::sort(written.begin(), written.end());
+    if (std::adjacent_find(written.begin(), written.end()) != written.end())
+        return fail(TAPS_ERR_ARG, "page %d is to be written from two places of the page table",
+                    *std::adjacent_find(written.begin(), written.end()));
+
+    int64_t total = 0;
+    for (const Strip &t : strips) total += t.cost();
+    total *= b->kv_heads;
+    const int64_t target = total / ((int64_t)cus * kPiecesPerUnit) + 1;
+    uint64_t part_rows = 0;
+    for (const Strip &t : strips) {
+        const int64_t keys = t.hi - t.lo;
+        int64_t parts = std::min((t.cost() + target - 1) / target, keys / kLeastPiece);
+        parts = std::max<int64_t>(1, std::min<int64_t>(parts, 256));
+        // whole tiles, counted from where the strip's first tile starts
+        const int64_t start = t.lo & ~15, tiles = (t.hi - start + 127) / 128;
+        parts = std::max<int64_t>(1, std::min(parts, tiles));
+        if (parts > 1)
+            out->joins.push_back({t.seq, t.row0, t.rows, (int32_t)part_rows, (int32_t)parts, {}});
+        for (int64_t k = 0; k < parts; ++k) {
+            taps_plan_item i{};
+            i.seq = t.seq, i.row0 = t.row0, i.narrow = t.narrow;
+            i.lo = (int32_t)std::max<int64_t>(t.lo, start + 128 * (tiles * k / parts));
+            i.hi = (int32_t)std::min<int64_t>(t.hi, start + 128 * (tiles * (k + 1) / parts));
+            i.part = parts > 1 ? (int32_t)(part_rows + k * t.rows) : -1;
+            out->items.push_back(i);
+        }
+        if (parts > 1) part_rows += (uint64_t)parts * t.rows;
+        if (part_rows >= (1ull << 31)) return fail(TAPS_ERR_ARG, "too many rows are split");
+    }
+    // dear items first, so that the last to start are cheap
+    std::stable_sort(out->items.begin(), out->items.end(),
+                     [](const taps_plan_item &x, const taps_plan_item &y) {
+                         return (x.hi - x.lo) * (x.narrow ? 2ll : 1ll) / 512 >
+                                (y.hi - y.lo) * (y.narrow ? 2ll : 1ll) / 512;
+                     });
+    if (out->items.size() * b->kv_heads >= (1ull << 31) || b->kv_heads > 65535)
+        return fail(TAPS_ERR_ARG, "too many workgroups");
+
+    h.magic = kPlanMagic;
+    h.n_seqs = b->n_seqs;
+    h.tokens = (uint32_t)tokens;
+    h.q_heads = b->q_heads, h.kv_heads = b->kv_heads, h.head_dim = b->head_dim;
+    h.page_log2 = log2, h.n_pages = b->n_pages, h.causal = b->causal != 0;
+    h.n_items = (uint32_t)out->items.size(), h.n_joins = (uint32_t)out->joins.size();
+    h.part_rows = (uint32_t)part_rows;
+    h.max_positions = (uint32_t)most;
+    h.appendable = appendable;
+    uint64_t at = up16(sizeof h);
+    h.seqs_at = at, at = up16(at + out->seqs.size() * sizeof(taps_plan_seq));
+    h.tokens_at = at, at = up16(at + tokens * sizeof(taps_plan_token));
+    h.pages_at = at, at = up16(at + pages * 4);
+    h.items_at = at, at = up16(at + out->items.size() * sizeof(taps_plan_item));
+    h.joins_at = at, at = up16(at + out->joins.size() * sizeof(taps_plan_join));
+    h.bytes = at;
+    return TAPS_OK;
+}
+
+uint64_t workspace_of(const taps_plan_header &h) {
+    return up16((uint64_t)h.part_rows * h.kv_heads * h.head_dim * 4) +
+           up16((uint64_t)h.part_rows * h.kv_heads * 8);
+}
+
+void write_plan(const taps_paged_batch *b, const Layout &l, char *to) {
+    const taps_plan_header &h = l.head;
+    memcpy(to, &h, sizeof h);
+    if (!l.seqs.empty()) memcpy(to + h.seqs_at, l.seqs.data(), l.seqs.size() * sizeof l.seqs[0]);
+    if (!l.items.empty())
+        memcpy(to + h.items_at, l.items.data(), l.items.size() * sizeof l.items[0]);
+    if (!l.joins.empty())
+        memcpy(to + h.joins_at, l.joins.data(), l.joins.size() * sizeof l.joins[0]);
+    auto *token = (taps_plan_token *)(to + h.tokens_at);
+    auto *pages = (int32_t *)(to + h.pages_at);
+    for (uint32_t s = 0; s < h.n_seqs; ++s) {
+        const int32_t *row = b->pages + (uint64_t)s * b->pages_stride;
+        const taps_plan_seq &q = l.seqs[s];
+        const int64_t n_pages = ((int64_t)q.kv_len + b->page_size - 1) >> h.page_log2;
+        for (int64_t g = 0; g < n_pages; ++g) *pages++ = row[g];
+        for (int64_t p = (int64_t)q.kv_len - b->q_lens[s]; p < q.kv_len; ++p, ++token) {
+            token->position = (int32_t)p;
+            token->slot = p < q.kv_start || p < 0
+                              ? -1
+                              : (int32_t)(((int64_t)row[p >> h.page_log2] << h.page_log2) +
+                                          (p & (b->page_size - 1)));
+        }
+    }
+}
+
+taps_status check_plan(const void *plan, const void *plan_device, const taps_plan_header **h) {
+    if (!plan || !plan_device) return fail(TAPS_ERR_ARG, "plan or plan_device is NULL");
+    if (!aligned(plan, 16) || !aligned(plan_device, 16))
+        return fail(TAPS_ERR_ARG, "plan or plan_device is not 16-byte aligned");
+    *h = (const taps_plan_header *)plan;
+    if ((*h)->magic != kPlanMagic) return fail(TAPS_ERR_ARG, "plan was not made by taps_paged_plan");
+    return TAPS_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+taps_status taps_norm_rotate(const taps_norm_rotate_args *a, taps_heads q, taps_heads k,
+                             taps_heads q_out, taps_heads k_out, void *stream) {
+    taps_rows_launch p;
+    if (taps_status st = check_norm_rotate(a, &p)) return st;
+    if (!a->batch || !a->tokens) return TAPS_OK;
+    const taps_heads src[2] = {q, k}, dst[2] = {q_out, k_out};
+    static const char *const names[2][2] = {{"q", "q_out"}, {"k", "k_out"}};
+    bool vectors = vectors_fit(p.dim, p.rotary, a->weight_dtype, a->q_weight, a->k_weight, a->table);
+    for (int side = 0; side < (a->k_heads ? 2 : 1); ++side) {
+        if (taps_status st = check_heads(src[side], names[side][0], a->dtype)) return st;
+        if (taps_status st = check_heads(dst[side], names[side][1], a->dtype)) return st;
+        p.src[side] = src[side].data, p.dst[side] = dst[side].data;
+        set_strides(p.src_stride[side], src[side]);
+        set_strides(p.dst_stride[side], dst[side]);
+        vectors = vectors && by_fours(src[side], a->dtype) && by_fours(dst[side], a->dtype);
+    }
+    return launched(taps_launch_norm_rotate(p, a->dtype, vectors, (hipStream_t)stream),
+                    "taps_norm_rotate");
+}
+
+taps_status taps_norm_rotate_backward(const taps_norm_rotate_args *a, taps_heads dq_out,
+                                      taps_heads dk_out, taps_heads q, taps_heads k, taps_heads dq,
+                                      taps_heads dk, void *q_weight_grad, void *k_weight_grad,
+                                      void *workspace, uint64_t *workspace_bytes, void *stream) {
+    taps_rows_launch p;
+    if (taps_status st = check_norm_rotate(a, &p)) return st;
+    if (!workspace_bytes) return fail(TAPS_ERR_ARG, "workspace_bytes is NULL");
+    const bool norms = p.norm[0] || p.norm[1];
+    // a partial sum per workgroup; as many workgroups on either path as the other could take
+    const uint64_t need =
+        norms ? up16((uint64_t)std::max(taps_backward_groups(p, true), taps_backward_groups(p, false)) *
+                     2 * p.dim * 4)
+              : 16;
+    if (!workspace) {
+        *workspace_bytes = need;
+        return TAPS_OK;
+    }
+    if (*workspace_bytes < need)
+        return fail(TAPS_ERR_CAPACITY, "workspace of %llu bytes, %llu are needed",
+                    (unsigned long long)*workspace_bytes, (unsigned long long)need);
+    if (!aligned(workspace, 16)) return fail(TAPS_ERR_ARG, "workspace is not 16-byte aligned");
+    const uint32_t sides = a->k_heads ? 2 : 1;
+    if ((q_weight_grad != nullptr) != (a->q_weight != nullptr) ||
+        (sides == 2 && (k_weight_grad != nullptr) != (a->k_weight != nullptr)))
+        return fail(TAPS_ERR_ARG, "a weight and its gradient go together");
+    if (sides == 1) k_weight_grad = nullptr;
+    const uint32_t w = size_of(a->weight_dtype);
+    if (!aligned(q_weight_grad, w) || !aligned(k_weight_grad, w))
+        return fail(TAPS_ERR_ARG, "a weight's gradient is not aligned to its elements");
+    const taps_heads g[2] = {dq_out, dk_out}, x[2] = {q, k}, d[2] = {dq, dk};
+    static const char *const names[2][3] = {{"dq_out", "q", "dq"}, {"dk_out", "k", "dk"}};
+    bool vectors = vectors_fit(p.dim, p.rotary, a->weight_dtype, a->q_weight, a->k_weight, a->table);
+    for (uint32_t side = 0; side < sides && a->batch && a->tokens; ++side) {
+        if (taps_status st = check_heads(g[side], names[side][0], a->dtype)) return st;
+        if (taps_status st = check_heads(x[side], names[side][1], a->dtype)) return st;
+        if (taps_status st = check_heads(d[side], names[side][2], a->dtype)) return st;
+        p.src[side] = g[side].data, p.x[side] = x[side].data, p.dst[side] = d[side].data;
+        set_strides(p.src_stride[side], g[side]);
+        set_strides(p.x_stride[side], x[side]);
+        set_strides(p.dst_stride[side], d[side]);
+        vectors = vectors && by_fours(g[side], a->dtype) && by_fours(x[side], a->dtype) &&
+                  by_fours(d[side], a->dtype);
+    }
+    if (!norms && (!a->batch || !a->tokens)) return TAPS_OK;
+    p.partial = norms ? (float *)workspace : nullptr;
+    return launched(taps_launch_norm_rotate_backward(p, a->dtype, vectors, q_weight_grad,
+                                                     k_weight_grad, (hipStream_t)stream),
+                    "taps_norm_rotate_backward");
+}
+
+taps_status taps_paged_plan(const taps_paged_batch *b, uint32_t cus, void *plan,
+                            uint64_t *plan_bytes, uint64_t *workspace_bytes) {
+    if (!b || !plan_bytes || !workspace_bytes)
+        return fail(TAPS_ERR_ARG, "batch, plan_bytes or workspace_bytes is NULL");
+    if (b->n_seqs && (!b->q_lens || !b->kv_lens || (!b->pages && b->pages_stride)))
+        return fail(TAPS_ERR_ARG, "q_lens, kv_lens or pages is NULL");
+    if (b->page_size < TAPS_MIN_PAGE || b->page_size > TAPS_MAX_PAGE ||
+        (b->page_size & (b->page_size - 1)))
+        return fail(TAPS_ERR_ARG, "page_size %u is not a power of two in %u..%u", b->page_size,
+                    TAPS_MIN_PAGE, TAPS_MAX_PAGE);
+    if ((uint64_t)b->n_pages * b->page_size >= (1ull << 31))
+        return fail(TAPS_ERR_ARG, "%u pages of %u slots are 2^31 slots or more", b->n_pages,
+                    b->page_size);
+    if (!b->kv_heads || !b->q_heads || b->q_heads % b->kv_heads)
+        return fail(TAPS_ERR_ARG, "q_heads %u is not a multiple of kv_heads %u", b->q_heads,
+                    b->kv_heads);
+    if (b->head_dim < 1 || b->head_dim > TAPS_MAX_HEAD_DIM)
+        return fail(TAPS_ERR_ARG, "head_dim %u outside 1..%u", b->head_dim, TAPS_MAX_HEAD_DIM);
+    if (b->window && !b->causal) return fail(TAPS_ERR_ARG, "a window needs causal");
+    try {
+        Layout l;
+        l.head.window = b->window < (1u << 30) ? b->window : 0;   // beyond every length
+        if (taps_status st = lay_out(b, cus ? cus : 256, &l)) return st;
+        const uint64_t room = *plan_bytes;
+        if (plan && room < l.head.bytes)
+            return fail(TAPS_ERR_CAPACITY, "plan of %llu bytes, %llu are needed",
+                        (unsigned long long)room, (unsigned long long)l.head.bytes);
+        if (plan && !aligned(plan, 16)) return fail(TAPS_ERR_ARG, "plan is not 16-byte aligned");
+        *plan_bytes = l.head.bytes;
+        *workspace_bytes = workspace_of(l.head);
+        if (plan) write_plan(b, l, (char *)plan);
+    } catch (const std::bad_alloc &) {
+        return fail(TAPS_ERR_CAPACITY, "out of host memory for a plan");
+    } catch (...) {
+        return fail(TAPS_ERR_ARG, "the plan could not be made");
+    }
+    return TAPS_OK;
+}
+
+taps_status taps_cache_append(const taps_append_args *a, const void *plan, const void *plan_device,
+                              taps_heads k, taps_heads v, taps_heads k_cache, taps_heads v_cache,
+                              void *stream) {
+    if (!a) return fail(TAPS_ERR_ARG, "args is NULL");
+    const taps_plan_header *h;
+    if (taps_status st = check_plan(plan, plan_device, &h)) return st;
+    if (taps_status st = check_types(a->dtype, a->weight_dtype, h->head_dim, a->rotary_dim, a->eps,
+                                     a->table))
+        return st;
+    if (!h->appendable)
+        return fail(TAPS_ERR_ARG, "a sequence of the plan has more new tokens than keys");
+    if (a->rotary_dim && h->max_positions > a->n_positions)
+        return fail(TAPS_ERR_ARG, "positions up to %u exceed the table's %u", h->max_positions,
+                    a->n_positions);
+    if (!h->tokens) return TAPS_OK;
+    taps_rows_launch p{};
+    const taps_heads src[2] = {k, v}, dst[2] = {k_cache, v_cache};
+    static const char *const names[2][2] = {{"k", "k_cache"}, {"v", "v_cache"}};
+    bool vectors =
+        vectors_fit(h->head_dim, a->rotary_dim, a->weight_dtype, a->k_weight, nullptr, a->table);
+    for (int side = 0; side < 2; ++side) {
+        if (taps_status st = check_heads(src[side], names[side][0], a->dtype)) return st;
+        if (taps_status st = check_heads(dst[side], names[side][1], a->dtype)) return st;
+        p.src[side] = src[side].data, p.dst[side] = dst[side].data;
+        set_strides(p.src_stride[side], src[side]);
+        p.src_stride[side][0] = 0;
+        set_strides(p.dst_stride[side], dst[side]);
+        taps_heads rows = src[side];
+        rows.stride[0] = 0;   // not used
+        vectors = vectors && by_fours(rows, a->dtype) && by_fours(dst[side], a->dtype);
+    }
+    p.plan_tokens = (const taps_plan_token *)((const char *)plan_device + h->tokens_at);
+    p.weight[0] = a->k_weight;
+    p.norm[0] = a->k_weight != nullptr;
+    p.float_weights = a->weight_dtype == TAPS_F32;
+    p.table = a->table;
+    p.batch = 1, p.tokens = h->tokens;
+    p.heads[0] = p.heads[1] = h->kv_heads;
+    p.dim = h->head_dim, p.rotary = a->rotary_dim;
+    p.n_positions = a->n_positions;
+    p.page_log2 = h->page_log2;
+    p.eps = a->eps;
+    p.interleaved = a->interleaved != 0;
+    return launched(taps_launch_append(p, a->dtype, vectors, (hipStream_t)stream),
+                    "taps_cache_append");
+}
+
+taps_status taps_attend(uint32_t dtype, const void *plan, const void *plan_device, taps_heads q,
+                        taps_heads k_cache, taps_heads v_cache, float scale, taps_heads out,
+                        float *lse, void *workspace, uint64_t workspace_bytes, void *stream) {
+    if (dtype != TAPS_BF16 && dtype != TAPS_F16)
+        return fail(TAPS_ERR_ARG, "dtype %u is neither TAPS_BF16 nor TAPS_F16", dtype);
+    const taps_plan_header *h;
+    if (taps_status st = check_plan(plan, plan_device, &h)) return st;
+    if (h->head_dim % 8 || h->head_dim > TAPS_MAX_ATTEND_DIM)
+        return fail(TAPS_ERR_ARG, "head_dim %u is not a multiple of 8 up to %u", h->head_dim,
+                    TAPS_MAX_ATTEND_DIM);
+    if (!(scale > 0.f) || std::isinf(scale))
+        return fail(TAPS_ERR_ARG, "scale is not positive and finite");
+    if (!h->tokens) return TAPS_OK;
+    const taps_heads all[4] = {q, k_cache, v_cache, out};
+    static const char *const names[4] = {"q", "k_cache", "v_cache", "out"};
+    for (int i = 0; i < 4; ++i) {
+        const bool cache = i == 1 || i == 2;
+        if (!all[i].data) return fail(TAPS_ERR_ARG, "%s is NULL", names[i]);
+        if (!aligned(all[i].data, 16) || (cache && all[i].stride[0] % 8) || all[i].stride[1] % 8 ||
+            all[i].stride[2] % 8)
+            return fail(TAPS_ERR_ARG, "%s: rows do not start at multiples of 16 bytes", names[i]);
+    }
+    if (!aligned(lse, 4)) return fail(TAPS_ERR_ARG, "lse is not aligned to its elements");
+    const uint64_t need = workspace_of(*h);
+    if (need && !workspace) return fail(TAPS_ERR_ARG, "workspace is NULL");
+    if (need > workspace_bytes)
+        return fail(TAPS_ERR_CAPACITY, "workspace of %llu bytes, %llu are needed",
+                    (unsigned long long)workspace_bytes, (unsigned long long)need);
+    if (!aligned(workspace, 16)) return fail(TAPS_ERR_ARG, "workspace is not 16-byte aligned");
+    taps_attend_launch p{};
+    const char *dev = (const char *)plan_device;
+    p.q = (const char *)q.data, p.out = (char *)out.data, p.lse = lse;
+    p.k_cache = (const char *)k_cache.data, p.v_cache = (const char *)v_cache.data;
+    p.part_o = (float *)workspace;
+    p.part_ml = (float *)((char *)workspace +
+                          up16((uint64_t)h->part_rows * h->kv_heads * h->head_dim * 4));
+    p.seqs = (const taps_plan_seq *)(dev + h->seqs_at);
+    p.pages = (const int32_t *)(dev + h->pages_at);
+    p.items = (const taps_plan_item *)(dev + h->items_at);
+    p.joins = (const taps_plan_join *)(dev + h->joins_at);
+    p.q_token = 2 * q.stride[1], p.q_head = 2 * q.stride[2];
+    p.o_token = 2 * out.stride[1], p.o_head = 2 * out.stride[2];
+    p.k_page = 2 * k_cache.stride[0], p.k_head = 2 * k_cache.stride[1];
+    p.k_slot = 2 * k_cache.stride[2];
+    p.v_page = 2 * v_cache.stride[0], p.v_head = 2 * v_cache.stride[1];
+    p.v_slot = 2 * v_cache.stride[2];
+    p.n_items = h->n_items, p.n_joins = h->n_joins;
+    p.q_heads = h->q_heads, p.kv_heads = h->kv_heads, p.group = h->q_heads / h->kv_heads;
+    p.dim = h->head_dim;
+    p.page_log2 = h->page_log2, p.causal = h->causal, p.window = h->window;
+    p.scale = scale;
+    return launched(taps_launch_attend(p, dtype, (hipStream_t)stream), "taps_attend");
+}
+
+const char *taps_attention_last_error(void) { return g_last_error; }
+
+}  // extern "C"
