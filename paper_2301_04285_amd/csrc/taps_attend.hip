@@ -21,7 +21,8 @@
 //   wide    128 query rows, 32 a wavefront; all share tiles of 64 keys;
 //   narrow  up to 32 query rows; every wavefront takes every fourth tile of 32 keys, and the
 //           four results are joined in LDS.
-// The next tile is loaded into registers while the present one is in use.
+// The next tile is on its way while the present one is in use: straight to a
+// second buffer in LDS (wide), or in registers (narrow).
 // Where a sequence's keys are split over several items, each leaves its
 // unnormalised result, maximum and sum, and k_join adds them up.
 #include "taps_attention_internal.h"
@@ -87,14 +88,24 @@ __device__ __forceinline__ float half_sum(float v) {
     return h.lower + h.upper;
 }
 
-// LDS image of a tile.  Rows of keys are padded so that the reads of eight or
-// more lanes fall on different banks: K is read 16 bytes a lane at the same
-// column of consecutive keys (rows 16 bytes apart modulo the banks), V 8
-// bytes a lane, four lanes a key, at two neighbouring groups of 16 columns (rows 64 bytes apart).
+// LDS image of a tile: rows of keys without gaps, K's and then V's.  Within a
+// row the 16-byte chunks are permuted by a mask of the key's number, so that
+// the reads fall on different banks: K is read 16 bytes a lane at the same
+// column of consecutive keys (8 or 16 of them at a time must differ), V 8
+// bytes a lane, four consecutive keys at four neighbouring chunks.
 template <int D> struct Tile {
-    static constexpr int kChunks = D / 8;   // of 16 bytes
-    static constexpr int kKRow = 2 * D + 16, kVRow = 2 * D + 64;
-    static constexpr int bytes(int keys) { return keys * (kKRow + kVRow); }
+    static constexpr int kChunks = D / 8, kRow = 2 * D;
+    static constexpr int bytes(int keys) { return 2 * keys * kRow; }
+    static __device__ __forceinline__ int k_mask(int key) {
+        if (D == 128) return key & 15;
+        if (D == 64) return ((key >> 1) & 3) | 4 * ((key ^ (key >> 3)) & 1);
+        return (((key >> 1) & 1) | ((key >> 1) & 2)) ^ ((key >> 3) & 1);   // the low two bits
+    }
+    static __device__ __forceinline__ int v_mask(int key) {
+        if (D == 128) return 4 * (key & 1) + 5 * (key & 2);
+        if (D == 64) return 2 * (key & 1) + 2 * (key & 2);
+        return key & 2;
+    }
 };
 
 constexpr int max_of(int a, int b) { return a > b ? a : b; }
@@ -104,40 +115,57 @@ template <int D> constexpr int shared_bytes() {
                          kWaves * kNarrowRows * (D + 4) * 4) + kWaves * kNarrowRows * 2 * 4);
 }
 
-// Loads `Keys` keys from key `t0` on into registers, Threads lanes sharing the
-// work, and stores them to LDS.  Keys outside lo .. hi - 1 and columns beyond
-// the head are zeros in LDS whatever memory holds there (it may never have
-// been written), and no address outside the sequence's pages is formed.
-template <int D, int Keys, int Threads> struct Stage {
-    static constexpr int kChunks = Tile<D>::kChunks;
-    static constexpr int kN = Keys * kChunks / Threads;
-    static_assert(kN * Threads == Keys * kChunks, "whole rounds");
-    u32x4 k[kN], v[kN];
+// The LDS address of a generic pointer to LDS.
+__device__ __forceinline__ uint32_t lds_at(const char *p) {
+    return (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const char *)p;
+}
 
-    __device__ __forceinline__ void load(const taps_attend_launch &p, const int32_t *pages,
-                                         const char *k_head, const char *v_head, int t0, int lo,
-                                         int hi, int thread) {
+// 16 bytes a lane from memory to LDS at `lds` + 16 lane, past the registers.
+// The compiler does not see the load: wait_loads() before the barrier that
+// hands the tile over.
+__device__ __forceinline__ void load_to_lds(const char *from, uint32_t lds) {
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off"
+                 :
+                 : "s"(lds), "v"(from)
+                 : "memory", "m0");
+}
+__device__ __forceinline__ void wait_loads() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
+
+// A wavefront's share of a tile: groups of 16 keys, which share a page.  Lane
+// by lane it takes the chunks in the order in which they lie in LDS.
+template <int D> struct Group {
+    static constexpr int kN = D / 32;   // 16 rows of D / 8 chunks / 64 lanes
+    int key[kN], k_col[kN], v_col[kN];   // chunk numbers of the row, as permuted
+    __device__ __forceinline__ explicit Group(int lane) {
 #pragma unroll
         for (int i = 0; i < kN; ++i) {
-            const int at = thread + i * Threads, key = t0 + at / kChunks, chunk = at % kChunks;
-            k[i] = u32x4{}, v[i] = u32x4{};
-            if (key >= lo && key < hi && 8 * chunk < (int)p.dim) {
-                const int64_t page = pages[key >> p.page_log2];
-                const int64_t slot = key & ((1 << p.page_log2) - 1);
-                k[i] = *(const u32x4 *)(k_head + page * p.k_page + slot * p.k_slot + 16 * chunk);
-                v[i] = *(const u32x4 *)(v_head + page * p.v_page + slot * p.v_slot + 16 * chunk);
-            }
-        }
-    }
-    __device__ __forceinline__ void store(char *lds, int thread) const {
-#pragma unroll
-        for (int i = 0; i < kN; ++i) {
-            const int at = thread + i * Threads, key = at / kChunks, chunk = at % kChunks;
-            *(u32x4 *)(lds + key * Tile<D>::kKRow + 16 * chunk) = k[i];
-            *(u32x4 *)(lds + Keys * Tile<D>::kKRow + key * Tile<D>::kVRow + 16 * chunk) = v[i];
+            const int at = lane + 64 * i;
+            key[i] = at / Tile<D>::kChunks;
+            const int c = at % Tile<D>::kChunks;
+            k_col[i] = c ^ Tile<D>::k_mask(key[i]);
+            v_col[i] = c ^ Tile<D>::v_mask(key[i]);
         }
     }
 };
+
+// Where a group of 16 keys lies; `page` is uniform.
+struct Place {
+    const char *k, *v;
+    __device__ __forceinline__ Place(const taps_attend_launch &p, const char *k_head,
+                                     const char *v_head, int page, int key) {
+        const int64_t slot = key & ((1 << p.page_log2) - 1);
+        k = k_head + page * p.k_page + slot * p.k_slot;
+        v = v_head + page * p.v_page + slot * p.v_slot;
+    }
+};
+
+// The page of key `key` of the sequence; no page before that of `lo` or after
+// that of hi - 1 is looked up.  Uniform: a scalar load.
+__device__ __forceinline__ int page_at(const taps_attend_launch &p, const int32_t *pages, int key,
+                                       int lo, int hi) {
+    const int at = __builtin_amdgcn_readfirstlane(min(max(key, lo), hi - 1) >> p.page_log2);
+    return *(const __attribute__((address_space(4))) int32_t *)(uintptr_t)(pages + at);
+}
 
 // One wavefront's 32 query rows: the rows' operand, running statistics and result.
 template <class T, int D> struct Rows {
@@ -176,25 +204,26 @@ template <class T, int D> struct Rows {
     // Takes Keys keys from LDS; t0 is the first one's number.  `c` = scale log2 e.
     template <int Keys>
     __device__ __forceinline__ void take(const char *lds, int t0, bool masked, float c, int lane) {
-        constexpr int kSub = Keys / 32;
+        constexpr int kSub = Keys / 32, kRow = Tile<D>::kRow;
         const int half = lane >> 5;
         f32x16 s[kSub];
+        const int k_mask = Tile<D>::k_mask(lane & 31);   // the same for key + 32
 #pragma unroll
-        for (int n = 0; n < kSub; ++n) {
-            s[n] = f32x16{};
-            const char *row = lds + (32 * n + (lane & 31)) * Tile<D>::kKRow + 16 * half;
+        for (int n = 0; n < kSub; ++n) s[n] = f32x16{};
 #pragma unroll
-            for (int k = 0; k < kSteps; ++k)
-                s[n] = Mfma<T>::run(*(const s16x8 *)(row + 32 * k), q[k], s[n]);
+        for (int k = 0; k < kSteps; ++k) {
+            const char *at = lds + (lane & 31) * kRow + 16 * ((2 * k + half) ^ k_mask);
+#pragma unroll
+            for (int n = 0; n < kSub; ++n)
+                s[n] = Mfma<T>::run(*(const s16x8 *)(at + 32 * n * kRow), q[k], s[n]);
         }
         if (masked) {
+            const uint32_t seen = max(last - first + 1, 0), at = t0 + 4 * half - first;
 #pragma unroll
             for (int n = 0; n < kSub; ++n)
 #pragma unroll
-                for (int i = 0; i < 16; ++i) {
-                    const int key = t0 + 32 * n + 8 * (i / 4) + 4 * half + i % 4;
-                    s[n][i] = key >= first && key <= last ? s[n][i] : kMinusInf;
-                }
+                for (int i = 0; i < 16; ++i)
+                    s[n][i] = at + (32 * n + 8 * (i / 4) + i % 4) < seen ? s[n][i] : kMinusInf;
         }
         float most = s[0][0];
 #pragma unroll
@@ -202,7 +231,6 @@ template <class T, int D> struct Rows {
 #pragma unroll
             for (int i = 0; i < 16; ++i) most = fmaxf(most, s[n][i]);
         most = half_max(most);
-        // !(<=): a NaN never raises the maximum, and shows in the sum
         if (__any(most * c > m * c + kSlack)) {
             const float to = fmaxf(m, most);
             const float by = to == kMinusInf ? 1.f : __builtin_amdgcn_exp2f((m - to) * c);
@@ -225,8 +253,10 @@ template <class T, int D> struct Rows {
                 pt[n][i] = pack2<T>(a, b);
             }
         // lane of a group of 16: key (lane % 16) / 4, columns 4 (lane % 4) ..
-        const char *vt = lds + Keys * Tile<D>::kKRow + (4 * half + (lane & 15) / 4) * Tile<D>::kVRow +
-                         32 * ((lane >> 4) & 1) + 8 * (lane & 3);
+        const int v_key = 4 * half + (lane & 15) / 4;
+        const int v_chunk = 2 * ((lane >> 4) & 1) + ((lane >> 1) & 1);
+        const int v_mask = Tile<D>::v_mask(v_key);   // the same for keys 8 and 16 further
+        const char *v0 = lds + (Keys + v_key) * kRow + 8 * (lane & 1);
 #pragma unroll
         for (int n = 0; n < kSub; ++n)
 #pragma unroll
@@ -234,8 +264,8 @@ template <class T, int D> struct Rows {
                 const u32x4 pb = {pt[n][4 * k], pt[n][4 * k + 1], pt[n][4 * k + 2], pt[n][4 * k + 3]};
 #pragma unroll
                 for (int b = 0; b < kBlocks; ++b) {
-                    const char *at = vt + (32 * n + 16 * k) * Tile<D>::kVRow + 64 * b;
-                    const s16x4 u = transposed(at), w = transposed(at + 8 * Tile<D>::kVRow);
+                    const char *at = v0 + 16 * ((4 * b + v_chunk) ^ v_mask) + (32 * n + 16 * k) * kRow;
+                    const s16x4 u = transposed(at), w = transposed(at + 8 * kRow);
                     const s16x8 va = {u[0], u[1], u[2], u[3], w[0], w[1], w[2], w[3]};
                     o[b] = Mfma<T>::run(va, __builtin_bit_cast(s16x8, pb), o[b]);
                 }
@@ -284,36 +314,58 @@ __global__ __launch_bounds__(kThreads, 2) void k_attend(taps_attend_launch p) {
     if (!item.narrow) {
         const int row = item.row0 + 32 * wave + (lane & 31);
         rows.start(p, seq, head, row, lo, hi, lane);
-        // what every row of the wavefront sees, and what any does
-        int all_from = lo, all_to = hi - 1, any_from = lo, any_to = hi - 1;
+        // keys that every row of the wavefront sees: all_from .. all_to.  (Tiles that no row of one
+        // wavefront sees are taken all the same, masked: leaving them out costs the other tiles
+        // 64 register moves each.)
+        int all_from = lo, all_to = hi - 1;
         if (p.causal) {
             const int row_a = min(item.row0 + 32 * wave, seq.rows - 1);
             const int row_b = min(item.row0 + 32 * wave + 31, seq.rows - 1);
-            const int pos_a = seq.first_pos + row_a / (int)p.group;
-            const int pos_b = seq.first_pos + row_b / (int)p.group;
-            all_to = min(all_to, pos_a);
-            any_to = min(any_to, pos_b);
-            if (p.window) {
-                all_from = max(all_from, pos_b - (int)p.window + 1);
-                any_from = max(any_from, pos_a - (int)p.window + 1);
-            }
+            all_to = min(all_to, seq.first_pos + row_a / (int)p.group);
+            if (p.window)
+                all_from = max(all_from, seq.first_pos + row_b / (int)p.group - (int)p.window + 1);
         }
-        if (item.row0 + 32 * wave >= seq.rows) any_to = -1;   // no rows: helps to load
-        using S = Stage<D, kWideKeys, kThreads>;
-        S stage;
-        if (lo < hi) stage.load(p, pages, k_head, v_head, start, lo, hi, threadIdx.x);
-        int buffer = 0;
+        // Each wavefront loads 16 of a tile's 64 keys.  Keys outside lo .. hi - 1 and columns
+        // beyond the head come from a block of zeros in the plan: what memory holds in their
+        // place (it may never have been written) must not reach a product.
+        const Group<D> g(lane);
+        const uint32_t mine = __builtin_amdgcn_readfirstlane(lds_at(lds) + 16 * wave * Tile<D>::kRow);
+        const bool ragged = p.dim < D;
+        const auto load = [&](int t0, int page, int buffer) {
+            const int key = t0 + 16 * wave;
+            const Place at(p, k_head, v_head, page, key);
+            const uint32_t to = mine + buffer * Tile<D>::bytes(kWideKeys);
+            const bool whole = !ragged && key >= lo && key + 16 <= hi;
+#pragma unroll
+            for (int i = 0; i < Group<D>::kN; ++i) {
+                const char *k = at.k + g.key[i] * p.k_slot + 16 * g.k_col[i];
+                const char *v = at.v + g.key[i] * p.v_slot + 16 * g.v_col[i];
+                if (!whole) {
+                    const bool in = key + g.key[i] >= lo && key + g.key[i] < hi;
+                    k = in && 8 * g.k_col[i] < (int)p.dim ? k : p.zeros;
+                    v = in && 8 * g.v_col[i] < (int)p.dim ? v : p.zeros;
+                }
+                load_to_lds(k, to + 1024 * i);
+                load_to_lds(v, to + 1024 * i + kWideKeys * Tile<D>::kRow);
+            }
+        };
+        int page = 0, buffer = 0;
+        if (lo < hi) {
+            load(start, page_at(p, pages, start + 16 * wave, lo, hi), 0);
+            page = page_at(p, pages, start + kWideKeys + 16 * wave, lo, hi);
+        }
         for (int t0 = start; lo < hi && t0 < hi; t0 += kWideKeys, buffer ^= 1) {
-            char *tile = lds + buffer * Tile<D>::bytes(kWideKeys);
-            stage.store(tile, threadIdx.x);
-            // one barrier a tile: who writes this buffer again has passed the
-            // next barrier, which no wavefront reaches before it is done here
+            // one barrier a tile: the tile's loads have ended in every wavefront, and every
+            // wavefront is done with the other buffer
+            wait_loads();
             __syncthreads();
-            if (t0 + kWideKeys < hi)
-                stage.load(p, pages, k_head, v_head, t0 + kWideKeys, lo, hi, threadIdx.x);
-            if (t0 > any_to || t0 + kWideKeys <= any_from) continue;
+            if (t0 + kWideKeys < hi) {
+                load(t0 + kWideKeys, page, buffer ^ 1);
+                page = page_at(p, pages, t0 + 2 * kWideKeys + 16 * wave, lo, hi);
+            }
             const bool masked = t0 < all_from || t0 + kWideKeys - 1 > all_to;
-            rows.template take<kWideKeys>(tile, t0, masked, c, lane);
+            rows.template take<kWideKeys>(lds + buffer * Tile<D>::bytes(kWideKeys), t0, masked, c,
+                                          lane);
         }
         const float l = half_sum(rows.l);
         if (row >= seq.rows) return;
@@ -355,17 +407,61 @@ __global__ __launch_bounds__(kThreads, 2) void k_attend(taps_attend_launch p) {
         // one token's rows all see the item's keys; several tokens' need masks
         const bool one = item.row0 / (int)p.group == last_row / (int)p.group || !p.causal;
         char *tile = lds + wave * Tile<D>::bytes(kNarrowKeys);
-        using S = Stage<D, kNarrowKeys, 64>;
-        S stage;
-        int t0 = start + kNarrowKeys * wave;
-        if (lo < hi && t0 < hi) stage.load(p, pages, k_head, v_head, t0, lo, hi, lane);
-        for (; lo < hi && t0 < hi; t0 += kWaves * kNarrowKeys) {
-            stage.store(tile, lane);
+        // The next tile, two groups of 16 keys, waits in registers; keys outside lo .. hi - 1 are
+        // loaded from an end of that range and become zeros on the way to LDS, as do columns
+        // beyond the head.
+        const Group<D> g(lane);
+        constexpr int kN = Group<D>::kN;
+        u32x4 kr[2][kN], vr[2][kN];
+        const bool ragged = p.dim < D;
+        const auto load = [&](int t0, int page0, int page1) {
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                // a group wholly outside: the address of the nearest key's group inside
+                const int key = min(max(t0 + 16 * h, start), (hi - 1) & ~15);
+                const Place at(p, k_head, v_head, h ? page1 : page0, key);
+#pragma unroll
+                for (int i = 0; i < kN; ++i) {
+                    const int row = min(max(key + g.key[i], lo), hi - 1) - key;
+                    const int kc = ragged && 8 * g.k_col[i] >= (int)p.dim ? 0 : g.k_col[i];
+                    const int vc = ragged && 8 * g.v_col[i] >= (int)p.dim ? 0 : g.v_col[i];
+                    kr[h][i] = *(const u32x4 *)(at.k + row * p.k_slot + 16 * kc);
+                    vr[h][i] = *(const u32x4 *)(at.v + row * p.v_slot + 16 * vc);
+                }
+            }
+        };
+        int t0 = start + kNarrowKeys * wave, page0 = 0, page1 = 0;
+        constexpr int kStep = kWaves * kNarrowKeys;
+        if (lo < hi && t0 < hi) {
+            load(t0, page_at(p, pages, t0, lo, hi), page_at(p, pages, t0 + 16, lo, hi));
+            page0 = page_at(p, pages, t0 + kStep, lo, hi);
+            page1 = page_at(p, pages, t0 + kStep + 16, lo, hi);
+        }
+        for (; lo < hi && t0 < hi; t0 += kStep) {
+            const bool whole = !ragged && t0 >= lo && t0 + kNarrowKeys <= hi;
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+#pragma unroll
+                for (int i = 0; i < kN; ++i) {
+                    const int key = 16 * h + g.key[i];
+                    u32x4 k = kr[h][i], v = vr[h][i];
+                    if (!whole) {
+                        const bool in = t0 + key >= lo && t0 + key < hi;
+                        k = in && 8 * g.k_col[i] < (int)p.dim ? k : u32x4{};
+                        v = in && 8 * g.v_col[i] < (int)p.dim ? v : u32x4{};
+                    }
+                    char *to = tile + 16 * h * Tile<D>::kRow + 16 * (lane + 64 * i);
+                    *(u32x4 *)to = k;
+                    *(u32x4 *)(to + kNarrowKeys * Tile<D>::kRow) = v;
+                }
             __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
             __builtin_amdgcn_wave_barrier();
             __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
-            const int next = t0 + kWaves * kNarrowKeys;
-            if (next < hi) stage.load(p, pages, k_head, v_head, next, lo, hi, lane);
+            if (t0 + kStep < hi) {
+                load(t0 + kStep, page0, page1);
+                page0 = page_at(p, pages, t0 + 2 * kStep, lo, hi);
+                page1 = page_at(p, pages, t0 + 2 * kStep + 16, lo, hi);
+            }
             const bool masked = !one || t0 < lo || t0 + kNarrowKeys > hi;
             rows.template take<kNarrowKeys>(tile, t0, masked, c, lane);
             __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");

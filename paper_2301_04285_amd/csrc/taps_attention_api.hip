@@ -492,6 +492,7 @@ taps_status taps_attend(uint32_t dtype, const void *plan, const void *plan_devic
     const char *dev = (const char *)plan_device;
     p.q = (const char *)q.data, p.out = (char *)out.data, p.lse = lse;
     p.k_cache = (const char *)k_cache.data, p.v_cache = (const char *)v_cache.data;
+    p.zeros = dev + offsetof(taps_plan_header, zeros);
     p.part_o = (float *)workspace;
     p.part_ml = (float *)((char *)workspace +
                           up16((uint64_t)h->part_rows * h->kv_heads * h->head_dim * 4));

@@ -2,6 +2,7 @@
 // its kernels share: the layout of a plan and the launch parameters.
 #pragma once
 #include <hip/hip_runtime.h>
+#include <stddef.h>
 #include <stdint.h>
 
 #include "taps_attention.h"
@@ -32,7 +33,9 @@ struct taps_plan_header {
     uint32_t reserved;
     // byte offsets of the arrays
     uint64_t seqs_at, tokens_at, pages_at, items_at, joins_at;
+    uint32_t zeros[4];   // what attention reads for keys that are not there
 };
+static_assert(offsetof(taps_plan_header, zeros) % 16 == 0, "read 16 bytes at a time");
 
 struct taps_plan_seq {
     int32_t token0;      // its first token
@@ -99,6 +102,7 @@ hipError_t taps_launch_norm_rotate_backward(const taps_rows_launch &p, uint32_t 
 
 struct taps_attend_launch {
     const char *q, *k_cache, *v_cache;
+    const char *zeros;   // 16 bytes
     char *out;
     float *lse;
     float *part_o, *part_ml;   // [part_rows][kv_heads][dim], [part_rows][kv_heads][2]
