@@ -219,8 +219,11 @@ taps_status lay_out(const taps_paged_batch *b, uint32_t cus, Layout *out) {
         // whole tiles, counted from where the strip's first tile starts
         const int64_t start = t.lo & ~15, tiles = (t.hi - start + 127) / 128;
         parts = std::max<int64_t>(1, std::min(parts, tiles));
-        if (parts > 1)
+        if (parts > 1) {
+            const uint32_t rows = 8 / taps_join_across((int)parts);
+            h.join_rounds = std::max(h.join_rounds, (t.rows + rows - 1) / rows);
             out->joins.push_back({t.seq, t.row0, t.rows, (int32_t)part_rows, (int32_t)parts, {}});
+        }
         for (int64_t k = 0; k < parts; ++k) {
             taps_plan_item i{};
             i.seq = t.seq, i.row0 = t.row0, i.narrow = t.narrow;
@@ -506,7 +509,7 @@ taps_status taps_attend(uint32_t dtype, const void *plan, const void *plan_devic
     p.k_slot = 2 * k_cache.stride[2];
     p.v_page = 2 * v_cache.stride[0], p.v_head = 2 * v_cache.stride[1];
     p.v_slot = 2 * v_cache.stride[2];
-    p.n_items = h->n_items, p.n_joins = h->n_joins;
+    p.n_items = h->n_items, p.n_joins = h->n_joins, p.join_rounds = h->join_rounds;
     p.q_heads = h->q_heads, p.kv_heads = h->kv_heads, p.group = h->q_heads / h->kv_heads;
     p.dim = h->head_dim;
     p.page_log2 = h->page_log2, p.causal = h->causal, p.window = h->window;

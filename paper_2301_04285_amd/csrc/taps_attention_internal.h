@@ -30,7 +30,7 @@ struct taps_plan_header {
     uint32_t part_rows;       // rows of partial results over all split pieces
     uint32_t max_positions;   // largest position of a new token, plus one
     uint32_t appendable;      // every sequence has kv_lens >= q_lens
-    uint32_t reserved;
+    uint32_t join_rounds;     // workgroups that the rows of a join are spread over, at most
     // byte offsets of the arrays
     uint64_t seqs_at, tokens_at, pages_at, items_at, joins_at;
     uint32_t zeros[4];   // what attention reads for keys that are not there
@@ -65,6 +65,11 @@ struct taps_plan_join {
     int32_t seq, row0, rows, part, parts;
     int32_t reserved[3];
 };
+
+// Groups of lanes that share a row's pieces in k_join: 1, 2, 4 or 8 of a workgroup's 8.
+__host__ __device__ inline int taps_join_across(int parts) {
+    return parts <= 1 ? 1 : parts <= 2 ? 2 : parts <= 4 ? 4 : 8;
+}
 
 // ---------------------------------------------------------------------------
 // launches
@@ -113,7 +118,7 @@ struct taps_attend_launch {
     // strides in bytes
     int64_t q_token, q_head, o_token, o_head;
     int64_t k_page, k_head, k_slot, v_page, v_head, v_slot;
-    uint32_t n_items, n_joins, q_heads, kv_heads, group, dim;
+    uint32_t n_items, n_joins, join_rounds, q_heads, kv_heads, group, dim;
     uint32_t page_log2, causal, window;
     float scale;
 };
