@@ -19,6 +19,8 @@
 namespace {
 
 constexpr int kThreads = 256;
+// Rows that a group of lanes has on their way at once.
+constexpr int kAtOnce = 4;
 
 template <class T> __device__ __forceinline__ float to_f32(T v) { return (float)v; }
 template <class T> __device__ __forceinline__ T from_f32(float v) { return (T)v; }
@@ -53,21 +55,28 @@ template <> struct Pairs<true> {
         }
     }
     __device__ __forceinline__ bool has(int) const { return live; }
-    template <class T>
-    __device__ __forceinline__ void load(const T *row, float (&a)[kN], float (&b)[kN]) const {
+    template <class T> struct Raw {
         typedef T v4 __attribute__((ext_vector_type(4)));
         v4 u = {}, v = {};
+    };
+    template <class T> __device__ __forceinline__ Raw<T> fetch(const T *row) const {
+        typedef typename Raw<T>::v4 v4;
+        Raw<T> r;
         if (live) {
-            u = *(const v4 *)(row + a0);
-            v = *(const v4 *)(row + b0);
+            r.u = *(const v4 *)(row + a0);
+            r.v = *(const v4 *)(row + b0);
         }
+        return r;
+    }
+    template <class T>
+    __device__ __forceinline__ void unpack(const Raw<T> &r, float (&a)[kN], float (&b)[kN]) const {
         if (interleaved) {
             for (int i = 0; i < 2; ++i) {
-                a[i] = to_f32<T>(u[2 * i]), b[i] = to_f32<T>(u[2 * i + 1]);
-                a[2 + i] = to_f32<T>(v[2 * i]), b[2 + i] = to_f32<T>(v[2 * i + 1]);
+                a[i] = to_f32<T>(r.u[2 * i]), b[i] = to_f32<T>(r.u[2 * i + 1]);
+                a[2 + i] = to_f32<T>(r.v[2 * i]), b[2 + i] = to_f32<T>(r.v[2 * i + 1]);
             }
         } else {
-            for (int i = 0; i < 4; ++i) a[i] = to_f32<T>(u[i]), b[i] = to_f32<T>(v[i]);
+            for (int i = 0; i < 4; ++i) a[i] = to_f32<T>(r.u[i]), b[i] = to_f32<T>(r.v[i]);
         }
     }
     template <class T>
@@ -119,12 +128,20 @@ template <> struct Pairs<false> {
             if (ib[i] >= (int)p.dim) ib[i] = -1;
         }
     }
-    template <class T>
-    __device__ __forceinline__ void load(const T *row, float (&a)[kN], float (&b)[kN]) const {
+    template <class T> struct Raw {
+        T a[kN], b[kN];
+    };
+    template <class T> __device__ __forceinline__ Raw<T> fetch(const T *row) const {
+        Raw<T> r;
         for (int i = 0; i < kN; ++i) {
-            a[i] = ia[i] >= 0 ? to_f32<T>(row[ia[i]]) : 0.f;
-            b[i] = ib[i] >= 0 ? to_f32<T>(row[ib[i]]) : 0.f;
+            r.a[i] = ia[i] >= 0 ? row[ia[i]] : (T)0.f;
+            r.b[i] = ib[i] >= 0 ? row[ib[i]] : (T)0.f;
         }
+        return r;
+    }
+    template <class T>
+    __device__ __forceinline__ void unpack(const Raw<T> &r, float (&a)[kN], float (&b)[kN]) const {
+        for (int i = 0; i < kN; ++i) a[i] = to_f32<T>(r.a[i]), b[i] = to_f32<T>(r.b[i]);
     }
     template <class T>
     __device__ __forceinline__ void store(T *row, const float (&a)[kN], const float (&b)[kN]) const {
@@ -149,9 +166,9 @@ __device__ __forceinline__ void load_weight(const taps_rows_launch &p, const P &
     if (!p.norm[side]) {
         for (int i = 0; i < P::kN; ++i) a[i] = b[i] = 1.f;
     } else if (p.float_weights) {
-        pairs.load((const float *)p.weight[side], a, b);
+        pairs.unpack(pairs.fetch((const float *)p.weight[side]), a, b);
     } else {
-        pairs.load((const T *)p.weight[side], a, b);
+        pairs.unpack(pairs.fetch((const T *)p.weight[side]), a, b);
     }
 }
 
@@ -167,6 +184,17 @@ __device__ __forceinline__ int64_t position_of(const taps_rows_launch &p, uint32
     const uint64_t at = (uint64_t)b * p.tokens + t;
     return p.wide_positions ? ((const int64_t *)p.positions)[at]
                             : (int64_t)((const int32_t *)p.positions)[at];
+}
+
+// Row (b, t, h) of a side's tensor; h counts the heads of both sides.
+template <class T>
+__device__ __forceinline__ T *row_of(const taps_rows_launch &p, const void *const (&data)[2],
+                                     const int64_t (&stride)[2][3], uint32_t b, uint32_t t,
+                                     uint32_t h) {
+    const int side = h >= p.heads[0];
+    const uint32_t hh = side ? h - p.heads[0] : h;
+    return (T *)(side ? data[1] : data[0]) + b * (side ? stride[1][0] : stride[0][0]) +
+           t * (side ? stride[1][1] : stride[0][1]) + hh * (side ? stride[1][2] : stride[0][2]);
 }
 
 // How a workgroup's groups of lanes share tokens and heads: `across` groups
@@ -201,29 +229,37 @@ __global__ __launch_bounds__(kThreads) void k_norm_rotate(taps_rows_launch p) {
     load_weight<P, T>(p, pairs, 0, wa[0], wb[0]);
     load_weight<P, T>(p, pairs, 1, wa[1], wb[1]);
     const float inv_dim = 1.f / (float)p.dim;
-    for (uint32_t h = group % split.across; h < heads; h += split.across) {
-        const int side = h >= p.heads[0];
-        const uint32_t hh = side ? h - p.heads[0] : h;
-        float a[N], bb[N];
-        pairs.load((const T *)p.src[side] + b * p.src_stride[side][0] + t * p.src_stride[side][1] +
-                       hh * p.src_stride[side][2], a, bb);
-        float rstd = 1.f;
-        if (p.norm[side]) {
-            float sum = 0.f;
-            for (int i = 0; i < N; ++i) sum += a[i] * a[i] + bb[i] * bb[i];
-            rstd = rsqrtf(row_sum<Lanes>(sum) * inv_dim + p.eps);
+    for (uint32_t h0 = group % split.across; h0 < heads; h0 += kAtOnce * split.across) {
+        typename P::template Raw<T> raw[kAtOnce];
+#pragma unroll
+        for (int u = 0; u < kAtOnce; ++u)
+            if (h0 + u * split.across < heads)
+                raw[u] = pairs.fetch(row_of<const T>(p, p.src, p.src_stride, b, t,
+                                                     h0 + u * split.across));
+#pragma unroll
+        for (int u = 0; u < kAtOnce; ++u) {
+            const uint32_t h = h0 + u * split.across;
+            if (h >= heads) break;
+            const int side = h >= p.heads[0];
+            float a[N], bb[N];
+            pairs.unpack(raw[u], a, bb);
+            float rstd = 1.f;
+            if (p.norm[side]) {
+                float sum = 0.f;
+                for (int i = 0; i < N; ++i) sum += a[i] * a[i] + bb[i] * bb[i];
+                rstd = rsqrtf(row_sum<Lanes>(sum) * inv_dim + p.eps);
+            }
+            for (int i = 0; i < N; ++i) {
+                const float na = a[i] * rstd * (side ? wa[1][i] : wa[0][i]);
+                const float nb = bb[i] * rstd * (side ? wb[1][i] : wb[0][i]);
+                a[i] = na * c[i] - nb * s[i];
+                bb[i] = nb * c[i] + na * s[i];
+            }
+            // a position off the table: what is not rotated is NaN too
+            if (!good)
+                for (int i = 0; i < N; ++i) a[i] = bb[i] = __builtin_nanf("");
+            pairs.store(row_of<T>(p, p.dst, p.dst_stride, b, t, h), a, bb);
         }
-        for (int i = 0; i < N; ++i) {
-            const float na = a[i] * rstd * (side ? wa[1][i] : wa[0][i]);
-            const float nb = bb[i] * rstd * (side ? wb[1][i] : wb[0][i]);
-            a[i] = na * c[i] - nb * s[i];
-            bb[i] = nb * c[i] + na * s[i];
-        }
-        // a position off the table: what is not rotated is NaN too
-        if (!good)
-            for (int i = 0; i < N; ++i) a[i] = bb[i] = __builtin_nanf("");
-        pairs.store((T *)p.dst[side] + b * p.dst_stride[side][0] + t * p.dst_stride[side][1] +
-                        hh * p.dst_stride[side][2], a, bb);
     }
 }
 
@@ -246,27 +282,37 @@ __global__ __launch_bounds__(kThreads) void k_append(taps_rows_launch p) {
     pairs.angles(p, place.position, c, s);
     load_weight<P, T>(p, pairs, 0, wa, wb);
     const float inv_dim = 1.f / (float)p.dim;
-    for (uint32_t h = group % split.across; h < heads; h += split.across) {
-        const int side = h >= p.heads[0];
-        const uint32_t hh = side ? h - p.heads[0] : h;
-        float a[N], b[N];
-        pairs.load((const T *)p.src[side] + t * p.src_stride[side][1] + hh * p.src_stride[side][2], a,
-                   b);
-        if (!side) {
-            float rstd = 1.f;
-            if (p.norm[0]) {
-                float sum = 0.f;
-                for (int i = 0; i < N; ++i) sum += a[i] * a[i] + b[i] * b[i];
-                rstd = rsqrtf(row_sum<Lanes>(sum) * inv_dim + p.eps);
+    for (uint32_t h0 = group % split.across; h0 < heads; h0 += kAtOnce * split.across) {
+        typename P::template Raw<T> raw[kAtOnce];
+#pragma unroll
+        for (int u = 0; u < kAtOnce; ++u)
+            if (h0 + u * split.across < heads)
+                raw[u] = pairs.fetch(row_of<const T>(p, p.src, p.src_stride, 0, t,
+                                                     h0 + u * split.across));
+#pragma unroll
+        for (int u = 0; u < kAtOnce; ++u) {
+            const uint32_t h = h0 + u * split.across;
+            if (h >= heads) break;
+            const int side = h >= p.heads[0];
+            const uint32_t hh = side ? h - p.heads[0] : h;
+            float a[N], b[N];
+            pairs.unpack(raw[u], a, b);
+            if (!side) {
+                float rstd = 1.f;
+                if (p.norm[0]) {
+                    float sum = 0.f;
+                    for (int i = 0; i < N; ++i) sum += a[i] * a[i] + b[i] * b[i];
+                    rstd = rsqrtf(row_sum<Lanes>(sum) * inv_dim + p.eps);
+                }
+                for (int i = 0; i < N; ++i) {
+                    const float na = a[i] * rstd * wa[i], nb = b[i] * rstd * wb[i];
+                    a[i] = na * c[i] - nb * s[i];
+                    b[i] = nb * c[i] + na * s[i];
+                }
             }
-            for (int i = 0; i < N; ++i) {
-                const float na = a[i] * rstd * wa[i], nb = b[i] * rstd * wb[i];
-                a[i] = na * c[i] - nb * s[i];
-                b[i] = nb * c[i] + na * s[i];
-            }
+            pairs.store((T *)p.dst[side] + page * p.dst_stride[side][0] +
+                            hh * p.dst_stride[side][1] + slot * p.dst_stride[side][2], a, b);
         }
-        pairs.store((T *)p.dst[side] + page * p.dst_stride[side][0] + hh * p.dst_stride[side][1] +
-                        slot * p.dst_stride[side][2], a, b);
     }
 }
 
@@ -295,42 +341,51 @@ __global__ __launch_bounds__(kThreads) void k_norm_rotate_backward(taps_rows_lau
         pairs.angles(p, good ? pos : 0, c, s);
         if (!good)
             for (int i = 0; i < N; ++i) c[i] = s[i] = __builtin_nanf("");
-        for (uint32_t h = group % split.across; h < heads; h += split.across) {
-            const int side = h >= p.heads[0];
-            const uint32_t hh = side ? h - p.heads[0] : h;
-            float ya[N], yb[N], a[N], bb[N];
-            pairs.load((const T *)p.src[side] + b * p.src_stride[side][0] +
-                           t * p.src_stride[side][1] + hh * p.src_stride[side][2], ya, yb);
-            if (p.norm[side])
-                pairs.load((const T *)p.x[side] + b * p.x_stride[side][0] +
-                               t * p.x_stride[side][1] + hh * p.x_stride[side][2], a, bb);
-            for (int i = 0; i < N; ++i) {   // h = R^T g
-                const float u = ya[i] * c[i] + yb[i] * s[i];
-                yb[i] = yb[i] * c[i] - ya[i] * s[i];
-                ya[i] = u;
-            }
-            if (!good)
-                for (int i = 0; i < N; ++i) ya[i] = yb[i] = __builtin_nanf("");
-            if (p.norm[side]) {
-                float sum = 0.f, dot = 0.f;
-                for (int i = 0; i < N; ++i) {
-                    sum += a[i] * a[i] + bb[i] * bb[i];
-                    dot += ya[i] * (side ? wa[1][i] : wa[0][i]) * a[i] +
-                           yb[i] * (side ? wb[1][i] : wb[0][i]) * bb[i];
-                }
-                const float rstd = rsqrtf(row_sum<Lanes>(sum) * inv_dim + p.eps);
-                const float mean = row_sum<Lanes>(dot) * rstd * inv_dim;   // mean(h w xh)
-                for (int i = 0; i < N; ++i) {
-                    const float xa = a[i] * rstd, xb = bb[i] * rstd;
-                    const float da = ya[i] * xa, db = yb[i] * xb;
-                    ga[0][i] += side ? 0.f : da, gb[0][i] += side ? 0.f : db;
-                    ga[1][i] += side ? da : 0.f, gb[1][i] += side ? db : 0.f;
-                    ya[i] = rstd * (ya[i] * (side ? wa[1][i] : wa[0][i]) - xa * mean);
-                    yb[i] = rstd * (yb[i] * (side ? wb[1][i] : wb[0][i]) - xb * mean);
+        for (uint32_t h0 = group % split.across; h0 < heads; h0 += kAtOnce * split.across) {
+            typename P::template Raw<T> raw_g[kAtOnce], raw_x[kAtOnce];
+#pragma unroll
+            for (int u = 0; u < kAtOnce; ++u) {
+                const uint32_t h = h0 + u * split.across;
+                if (h < heads) {
+                    raw_g[u] = pairs.fetch(row_of<const T>(p, p.src, p.src_stride, b, t, h));
+                    raw_x[u] = pairs.fetch(row_of<const T>(p, p.x, p.x_stride, b, t, h));
                 }
             }
-            pairs.store((T *)p.dst[side] + b * p.dst_stride[side][0] + t * p.dst_stride[side][1] +
-                            hh * p.dst_stride[side][2], ya, yb);
+#pragma unroll
+            for (int u = 0; u < kAtOnce; ++u) {
+                const uint32_t h = h0 + u * split.across;
+                if (h >= heads) break;
+                const int side = h >= p.heads[0];
+                float ya[N], yb[N], a[N], bb[N];
+                pairs.unpack(raw_g[u], ya, yb);
+                pairs.unpack(raw_x[u], a, bb);
+                for (int i = 0; i < N; ++i) {   // h = R^T g
+                    const float v = ya[i] * c[i] + yb[i] * s[i];
+                    yb[i] = yb[i] * c[i] - ya[i] * s[i];
+                    ya[i] = v;
+                }
+                if (!good)
+                    for (int i = 0; i < N; ++i) ya[i] = yb[i] = __builtin_nanf("");
+                if (p.norm[side]) {
+                    float sum = 0.f, dot = 0.f;
+                    for (int i = 0; i < N; ++i) {
+                        sum += a[i] * a[i] + bb[i] * bb[i];
+                        dot += ya[i] * (side ? wa[1][i] : wa[0][i]) * a[i] +
+                               yb[i] * (side ? wb[1][i] : wb[0][i]) * bb[i];
+                    }
+                    const float rstd = rsqrtf(row_sum<Lanes>(sum) * inv_dim + p.eps);
+                    const float mean = row_sum<Lanes>(dot) * rstd * inv_dim;   // mean(h w xh)
+                    for (int i = 0; i < N; ++i) {
+                        const float xa = a[i] * rstd, xb = bb[i] * rstd;
+                        const float da = ya[i] * xa, db = yb[i] * xb;
+                        ga[0][i] += side ? 0.f : da, gb[0][i] += side ? 0.f : db;
+                        ga[1][i] += side ? da : 0.f, gb[1][i] += side ? db : 0.f;
+                        ya[i] = rstd * (ya[i] * (side ? wa[1][i] : wa[0][i]) - xa * mean);
+                        yb[i] = rstd * (yb[i] * (side ? wb[1][i] : wb[0][i]) - xb * mean);
+                    }
+                }
+                pairs.store(row_of<T>(p, p.dst, p.dst_stride, b, t, h), ya, yb);
+            }
         }
     }
     if (!p.partial) return;
