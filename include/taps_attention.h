@@ -52,6 +52,8 @@ extern "C" {
 
 #define TAPS_MAX_HEAD_DIM 256   /* norm_rotate, cache_append */
 #define TAPS_MAX_ATTEND_DIM 128 /* attend: a multiple of 8 up to this */
+/* taps_norm_rotate_backward never needs more bytes of workspace */
+#define TAPS_NORM_ROTATE_WORKSPACE(head_dim) (8192u * (head_dim))
 #define TAPS_MIN_PAGE 16        /* slots of a page: a power of two, 16 .. 4096 */
 #define TAPS_MAX_PAGE 4096
 
@@ -92,11 +94,11 @@ taps_status taps_norm_rotate(const taps_norm_rotate_args *args, taps_heads q, ta
 /* The gradients of taps_norm_rotate: from those of its outputs (dq_out,
  * dk_out) and its inputs (q, k) to those of its inputs (dq, dk) and weights
  * (device [head_dim] in weight_dtype, each NULL exactly if the weight is).
- * dq may be dq_out and dk dk_out.  The weights' gradients are sums over all rows, held in 32 bits and
- * added in an order that only the sizes determine.  `workspace` (device, 16-byte aligned) holds
- * partial sums; with workspace NULL the call only writes the bytes it needs
- * to *workspace_bytes, otherwise *workspace_bytes says how many there are
- * (TAPS_ERR_CAPACITY if too few). */
+ * dq may be dq_out and dk dk_out.  The weights' gradients are sums over all
+ * rows, held in 32 bits and added in an order that only the sizes determine.
+ * `workspace` (device, 16-byte aligned) holds partial sums; with workspace
+ * NULL the call only writes the bytes it needs to *workspace_bytes, otherwise
+ * *workspace_bytes says how many there are (TAPS_ERR_CAPACITY if too few). */
 taps_status taps_norm_rotate_backward(const taps_norm_rotate_args *args, taps_heads dq_out,
                                       taps_heads dk_out, taps_heads q, taps_heads k, taps_heads dq,
                                       taps_heads dk, void *q_weight_grad, void *k_weight_grad,

@@ -15,13 +15,13 @@ stream that the call runs on (``stream``, or the current one).
 """
 from __future__ import annotations
 
-import contextlib
 import ctypes as C
 import os
 import re
 from typing import List
 
 import numpy as np
+import torch
 
 from . import taps
 from .taps import TapsError, _stream   # noqa: F401
@@ -33,10 +33,12 @@ HEADER = os.path.join(os.path.dirname(HERE), "include", "taps_attention.h")
 BF16, F16, F32 = range(3)
 MAX_HEAD_DIM = 256
 MAX_ATTEND_DIM = 128
+WORKSPACE_PER_ELEMENT = 8192   # bytes of taps_norm_rotate_backward's per element of a head
 
 
-class Heads(C.Structure):
-    _fields_ = [("data", C.c_void_p), ("stride", C.c_int64 * 3)]
+class Heads(C.Structure):   # stride[3] field by field: made in half the time
+    _fields_ = [("data", C.c_void_p), ("stride0", C.c_int64), ("stride1", C.c_int64),
+                ("stride2", C.c_int64)]
 
 
 class NormRotateArgs(C.Structure):
@@ -117,81 +119,83 @@ def _check(status: int, call: str) -> None:
 # marshalling
 # ---------------------------------------------------------------------------
 
-_DTYPES = {}
+# A small call takes less time on the GPU than its marshalling does, so the
+# checks are made the short way; one call fetches the device and stream once.
+
+_DTYPES = {torch.bfloat16: BF16, torch.float16: F16, torch.float32: F32}
 
 
 def _dtype(t) -> int:
-    if not _DTYPES:
-        import torch
-        _DTYPES.update({torch.bfloat16: BF16, torch.float16: F16, torch.float32: F32})
-    if t.dtype not in _DTYPES:
+    code = _DTYPES.get(t.dtype)
+    if code is None:
         raise ValueError(f"tensors of {t.dtype} are not supported")
-    return _DTYPES[t.dtype]
+    return code
 
 
-def _on_gpu(t, what: str) -> None:
-    import torch
-    if t.device.type != "cuda":
+def _device() -> int:
+    return torch._C._cuda_getDevice()
+
+
+def _on_gpu(t, what: str, device: int) -> None:
+    if not t.is_cuda:
         raise ValueError(f"{what} is not on the GPU")
-    if t.device.index != torch.cuda.current_device():
+    if t.get_device() != device:
         raise ValueError(f"{what} is on {t.device}, not on the current GPU")
 
 
-def _heads(t, what: str, like=None, shape=None, rank=4) -> Heads:
+def _heads(t, what: str, device: int, dtype, shape, rank: int) -> Heads:
     """A tensor [batch, tokens, heads, dim], or [tokens, heads, dim] as one sequence."""
-    if like is not None and t.dtype != like.dtype:
-        raise ValueError(f"{what} is {t.dtype}, not {like.dtype}")
-    if shape is not None and tuple(t.shape) != tuple(shape):
+    if t.dtype is not dtype:
+        raise ValueError(f"{what} is {t.dtype}, not {dtype}")
+    if t.shape != shape:
         raise ValueError(f"{what} is {tuple(t.shape)}, not {tuple(shape)}")
-    _on_gpu(t, what)
+    _on_gpu(t, what, device)
     s = t.stride()
     if s[-1] != 1 and t.shape[-1] > 1:
         raise ValueError(f"{what}: the elements of a head are not contiguous")
     if rank == 3:
-        return Heads(t.data_ptr(), (0, s[0], s[1]))
-    return Heads(t.data_ptr(), (s[0], s[1], s[2]))
+        return Heads(t.data_ptr(), 0, s[0], s[1])
+    return Heads(t.data_ptr(), s[0], s[1], s[2])
 
 
-_NONE = Heads(None, (0, 0, 0))
+_NONE = Heads(None, 0, 0, 0)
 
 
-def _vector(w, what: str, dim: int, like, second=None):
-    """(pointer, dtype code) of a head's weights; both weights have one dtype."""
-    if w is None:
-        return None, None
-    if tuple(w.shape) != (dim,) or (dim > 1 and w.stride(0) != 1):
+def _vector(w, what: str, dim: int, device: int, dtype) -> int:
+    """Pointer to a head's weights."""
+    if w.shape != (dim,) or (dim > 1 and w.stride(0) != 1):
         raise ValueError(f"{what} is not a contiguous vector of {dim}")
-    if w.dtype != like.dtype and _dtype(w) != F32:
-        raise ValueError(f"{what} is {w.dtype}, neither {like.dtype} nor 32-bit")
-    if second is not None and second.dtype != w.dtype:
-        raise ValueError("the weights of queries and keys differ in type")
-    _on_gpu(w, what)
-    return w.data_ptr(), _dtype(w)
+    if w.dtype is not dtype and w.dtype is not torch.float32:
+        raise ValueError(f"{what} is {w.dtype}, neither {dtype} nor 32-bit")
+    _on_gpu(w, what, device)
+    return w.data_ptr()
 
 
-def _table(table, dim: int):
+def _table(table, dim: int, device: int):
     """(pointer, positions, rotated elements) of a rotation table [positions, 2, rotary / 2]."""
     if table is None:
         return None, 0, 0
-    if table.dim() != 3 or table.shape[1] != 2 or not table.is_contiguous() or \
-            _dtype(table) != F32:
+    shape = table.shape
+    if len(shape) != 3 or shape[1] != 2 or table.dtype is not torch.float32 or \
+            not table.is_contiguous():
         raise ValueError("table is not a contiguous 32-bit tensor [positions, 2, pairs]")
-    _on_gpu(table, "table")
-    if 2 * table.shape[2] > dim:
-        raise ValueError(f"table rotates {2 * table.shape[2]} of {dim} elements")
-    return table.data_ptr(), table.shape[0], 2 * table.shape[2]
+    _on_gpu(table, "table", device)
+    if 2 * shape[2] > dim:
+        raise ValueError(f"table rotates {2 * shape[2]} of {dim} elements")
+    return table.data_ptr(), shape[0], 2 * shape[2]
 
 
-def _on(stream):
+def _on(stream, make):
     """New tensors belong to the stream that fills them."""
-    import torch
-    return contextlib.nullcontext() if stream is None else torch.cuda.stream(stream)
+    if stream is None:
+        return make()
+    with torch.cuda.stream(stream):
+        return make()
 
 
 def rotation_table(n_positions: int, rotary_dim: int, base: float = 10000.0, device="cuda"):
     """Cosines and sines of position x base^(-2 i / rotary_dim) as a 32-bit tensor
     [n_positions, 2, rotary_dim // 2], angles computed in 64 bits."""
-    import torch
     if rotary_dim < 0 or rotary_dim % 2:
         raise ValueError("rotary_dim is odd or negative")
     inv = base ** (-torch.arange(0, rotary_dim, 2, dtype=torch.float64) / max(rotary_dim, 1))
@@ -203,31 +207,43 @@ def rotation_table(n_positions: int, rotary_dim: int, base: float = 10000.0, dev
 # norm and rotation
 # ---------------------------------------------------------------------------
 
-def _norm_rotate_args(q, k, q_weight, k_weight, table, positions, first, eps, interleaved):
-    if q.dim() not in (3, 4):
+def _norm_rotate_args(q, k, q_weight, k_weight, table, positions, first, eps, interleaved, device):
+    shape = q.shape
+    rank = len(shape)
+    if rank == 4:
+        batch, tokens, q_heads, dim = shape
+    elif rank == 3:
+        batch, (tokens, q_heads, dim) = 1, shape
+    else:
         raise ValueError("q is not [batch, tokens, heads, dim] or [tokens, heads, dim]")
-    if k is not None and (k.dim() != q.dim() or k.shape[:-2] != q.shape[:-2] or
-                          k.shape[-1] != q.shape[-1]):
-        raise ValueError(f"k is {tuple(k.shape)} beside q {tuple(q.shape)}")
-    if k is None and k_weight is not None:
+    k_heads = 0
+    if k is not None:
+        if k.shape[:-2] != shape[:-2] or k.shape[-1] != dim:
+            raise ValueError(f"k is {tuple(k.shape)} beside q {tuple(shape)}")
+        k_heads = k.shape[-2]
+    elif k_weight is not None:
         raise ValueError("k_weight without k")
-    dim = q.shape[-1]
-    qw, qt = _vector(q_weight, "q_weight", dim, q, k_weight)
-    kw, kt = _vector(k_weight, "k_weight", dim, q)
-    at, rows, rotary = _table(table, dim)
-    batch, tokens = q.shape[:2] if q.dim() == 4 else (1, q.shape[0])
+    dtype = weight = _dtype(q)
+    qw = kw = None
+    if q_weight is not None:
+        qw = _vector(q_weight, "q_weight", dim, device, q.dtype)
+        weight = _DTYPES[q_weight.dtype]
+    if k_weight is not None:
+        kw = _vector(k_weight, "k_weight", dim, device, q.dtype)
+        if qw is not None and _DTYPES[k_weight.dtype] != weight:
+            raise ValueError("the weights of queries and keys differ in type")
+        weight = _DTYPES[k_weight.dtype]
+    at, rows, rotary = _table(table, dim, device)
     pos, size = None, 4
     if positions is not None and rotary:
-        _on_gpu(positions, "positions")
-        if tuple(positions.shape) != tuple(q.shape[:-2]) or not positions.is_contiguous() or \
-                positions.is_floating_point() or positions.element_size() not in (4, 8):
-            raise ValueError(f"positions is not a contiguous integer tensor {tuple(q.shape[:-2])}")
-        pos, size = positions.data_ptr(), positions.element_size()
-    dtype = _dtype(q)
-    weight = qt if qt is not None else kt if kt is not None else dtype
-    return NormRotateArgs(batch, tokens, q.shape[-2], 0 if k is None else k.shape[-2], dim, rotary,
-                          dtype, weight, int(bool(interleaved)), eps, qw, kw, at, rows, size, pos,
-                          first)
+        _on_gpu(positions, "positions", device)
+        size = positions.element_size()
+        if positions.shape != shape[:-2] or not positions.is_contiguous() or \
+                positions.dtype not in (torch.int32, torch.int64):
+            raise ValueError(f"positions is not a contiguous integer tensor {tuple(shape[:-2])}")
+        pos = positions.data_ptr()
+    return NormRotateArgs(batch, tokens, q_heads, k_heads, dim, rotary, dtype, weight,
+                          1 if interleaved else 0, eps, qw, kw, at, rows, size, pos, first)
 
 
 def taps_norm_rotate(q, k, q_weight, k_weight, table, positions=None, first=0, eps=1e-6,
@@ -241,21 +257,20 @@ def taps_norm_rotate(q, k, q_weight, k_weight, table, positions=None, first=0, e
     positions: integers of q's leading dimensions (one that is no row of the
     table makes its token NaN), or None for first, first + 1, ...
     out: (q_out, k_out) to fill; they may be (q, k)."""
-    import torch
-    args = _norm_rotate_args(q, k, q_weight, k_weight, table, positions, first, eps, interleaved)
-    if out is None:
-        with _on(stream):
-            # dense even where q and k are slices of one projection
-            out = (torch.empty(q.shape, dtype=q.dtype, device=q.device),
-                   None if k is None else torch.empty(k.shape, dtype=k.dtype, device=k.device))
+    device = _device()
+    args = _norm_rotate_args(q, k, q_weight, k_weight, table, positions, first, eps, interleaved,
+                             device)
+    dtype, shape = q.dtype, q.shape
+    rank = len(shape)
+    kh = _NONE if k is None else _heads(k, "k", device, dtype, k.shape, rank)
+    qh = _heads(q, "q", device, dtype, shape, rank)
+    if out is None:   # dense even where q and k are slices of one projection
+        out = _on(stream, lambda: (q.new_empty(shape), None if k is None else k.new_empty(k.shape)))
     q_out, k_out = out
-    rank = q.dim()
-    none = k is None
     _check(load().taps_norm_rotate(
-        C.byref(args), _heads(q, "q", rank=rank), _NONE if none else _heads(k, "k", q, rank=rank),
-        _heads(q_out, "out[0]", q, q.shape, rank),
-        _NONE if none else _heads(k_out, "out[1]", q, k.shape, rank), _stream(stream)),
-        "taps_norm_rotate")
+        C.byref(args), qh, kh, _heads(q_out, "out[0]", device, dtype, shape, rank),
+        _NONE if k is None else _heads(k_out, "out[1]", device, dtype, k.shape, rank),
+        _stream(stream)), "taps_norm_rotate")
     return q_out, k_out
 
 
@@ -265,27 +280,32 @@ def taps_norm_rotate_backward(dq_out, dk_out, q, k, q_weight, k_weight, table, p
     those of its outputs, with its other arguments as they were (None where the
     input is None).  The weights' gradients are summed in 32 bits, in the same
     order every time, and rounded to the weights' type."""
-    import torch
-    args = _norm_rotate_args(q, k, q_weight, k_weight, table, positions, first, eps, interleaved)
-    rank, none, raw = q.dim(), k is None, _stream(stream)
-    need = C.c_uint64()
-    L = load()
-    _check(L.taps_norm_rotate_backward(C.byref(args), _NONE, _NONE, _NONE, _NONE, _NONE, _NONE,
-                                       None, None, None, C.byref(need), raw),
-           "taps_norm_rotate_backward")
-    with _on(stream):
-        dq = torch.empty(q.shape, dtype=q.dtype, device=q.device)
-        dk = None if none else torch.empty(k.shape, dtype=k.dtype, device=k.device)
-        dqw = None if q_weight is None else torch.empty_like(q_weight)
-        dkw = None if k_weight is None else torch.empty_like(k_weight)
-        workspace = torch.empty(need.value, dtype=torch.uint8, device=q.device)
-    _check(L.taps_norm_rotate_backward(
-        C.byref(args), _heads(dq_out, "dq_out", q, q.shape, rank),
-        _NONE if none else _heads(dk_out, "dk_out", q, k.shape, rank), _heads(q, "q", rank=rank),
-        _NONE if none else _heads(k, "k", q, rank=rank), _heads(dq, "dq", rank=rank),
-        _NONE if none else _heads(dk, "dk", rank=rank),
+    device = _device()
+    args = _norm_rotate_args(q, k, q_weight, k_weight, table, positions, first, eps, interleaved,
+                             device)
+    dtype, shape = q.dtype, q.shape
+    rank = len(shape)
+    qh = _heads(q, "q", device, dtype, shape, rank)
+    gqh = _heads(dq_out, "dq_out", device, dtype, shape, rank)
+    kh = gkh = dkh = _NONE
+    if k is not None:
+        kh = _heads(k, "k", device, dtype, k.shape, rank)
+        gkh = _heads(dk_out, "dk_out", device, dtype, k.shape, rank)
+    size = WORKSPACE_PER_ELEMENT * shape[-1]
+
+    def make():
+        return (q.new_empty(shape), None if k is None else k.new_empty(k.shape),
+                None if q_weight is None else q_weight.new_empty(q_weight.shape),
+                None if k_weight is None else k_weight.new_empty(k_weight.shape),
+                torch.empty(size, dtype=torch.uint8, device=q.device))
+    dq, dk, dqw, dkw, workspace = _on(stream, make)
+    if k is not None:
+        dkh = _heads(dk, "dk", device, dtype, k.shape, rank)
+    _check(load().taps_norm_rotate_backward(
+        C.byref(args), gqh, gkh, qh, kh, _heads(dq, "dq", device, dtype, shape, rank), dkh,
         None if dqw is None else dqw.data_ptr(), None if dkw is None else dkw.data_ptr(),
-        workspace.data_ptr(), C.byref(need), raw), "taps_norm_rotate_backward")
+        workspace.data_ptr(), C.byref(C.c_uint64(size)), _stream(stream)),
+        "taps_norm_rotate_backward")
     return dq, dk, dqw, dkw
 
 
@@ -298,8 +318,6 @@ def norm_rotate(q, k, q_weight, k_weight, table, positions=None, first=0, eps=1e
     weights come from ``taps_norm_rotate_backward``."""
     global _function
     if _function is None:
-        import torch
-
         class NormRotate(torch.autograd.Function):
             @staticmethod
             def forward(ctx, q, k, q_weight, k_weight, table, positions, how):
@@ -375,7 +393,6 @@ class PagedPlan:
         self._make(batch, units, device)
 
     def _make(self, batch, units, device) -> None:
-        import torch
         size, work = C.c_uint64(), C.c_uint64()
         L = load()
         cus = units or 0
@@ -397,37 +414,39 @@ class PagedPlan:
                 self._made_on = _stream(None)
                 self._ready = torch.cuda.Event()
                 self._ready.record()
+            self._at = self._host.data_ptr(), self._gpu.data_ptr()
+        self._q_shape = self.tokens, self.q_heads, self.head_dim
+        self._k_shape = self.tokens, self.kv_heads, self.head_dim
+        self._page_shape = self.kv_heads, self.page_size, self.head_dim
 
-    def pointers(self, stream):
-        """(host, device) copies, once ``stream`` may read the second."""
-        import torch
+    def pointers(self, stream, raw, device):
+        """(host, device) copies, once ``stream`` (its handle: raw) may read the second."""
         if self._gpu is None:
             raise ValueError("the plan was made without a GPU")
-        _on_gpu(self._gpu, "plan")
-        if _stream(stream) != self._made_on:
+        _on_gpu(self._gpu, "plan", device)
+        if raw != self._made_on:
             s = torch.cuda.current_stream() if stream is None else stream
             s.wait_event(self._ready)
             self._gpu.record_stream(s)
-        return self._host.data_ptr(), self._gpu.data_ptr()
+        return self._at
 
 
 _units_of = {}
 
 
 def _units(device) -> int:
-    import torch
     if device not in _units_of:
         _units_of[device] = torch.cuda.get_device_properties(device).multi_processor_count
     return _units_of[device]
 
 
-def _cache(t, what: str, plan: PagedPlan, like) -> Heads:
+def _cache(t, what: str, plan: PagedPlan, device: int, dtype) -> Heads:
     """A cache [pages, kv_heads, page_size, dim] of any strides but the last."""
-    if t.dim() != 4 or t.shape[0] < plan.n_pages or \
-            tuple(t.shape[1:]) != (plan.kv_heads, plan.page_size, plan.head_dim):
-        raise ValueError(f"{what} is {tuple(t.shape)}, not at least {plan.n_pages} x "
-                         f"({plan.kv_heads}, {plan.page_size}, {plan.head_dim})")
-    return _heads(t, what, like)
+    shape = t.shape
+    if len(shape) != 4 or shape[0] < plan.n_pages or shape[1:] != plan._page_shape:
+        raise ValueError(f"{what} is {tuple(shape)}, not at least {plan.n_pages} x "
+                         f"{plan._page_shape}")
+    return _heads(t, what, device, dtype, shape, 4)
 
 
 def taps_cache_append(k, v, k_cache, v_cache, plan: PagedPlan, table=None, k_weight=None, eps=1e-6,
@@ -438,16 +457,20 @@ def taps_cache_append(k, v, k_cache, v_cache, plan: PagedPlan, table=None, k_wei
 
     k, v: [tokens, kv_heads, dim]; k_cache, v_cache: [pages, kv_heads,
     page_size, dim]."""
-    shape = (plan.tokens, plan.kv_heads, plan.head_dim)
-    kw, kt = _vector(k_weight, "k_weight", plan.head_dim, k)
-    at, rows, rotary = _table(table, plan.head_dim)
-    dtype = _dtype(k)
-    args = AppendArgs(dtype, dtype if kt is None else kt, rotary, int(bool(interleaved)), eps, kw,
-                      at, rows)
-    heads = (_heads(k, "k", k, shape, 3), _heads(v, "v", k, shape, 3),
-             _cache(k_cache, "k_cache", plan, k), _cache(v_cache, "v_cache", plan, k))
-    _check(load().taps_cache_append(C.byref(args), *plan.pointers(stream), *heads,
-                                    _stream(stream)), "taps_cache_append")
+    device, raw, dtype = _device(), _stream(stream), k.dtype
+    code = weight = _dtype(k)
+    at, rows, rotary = _table(table, plan.head_dim, device)
+    kw = None
+    if k_weight is not None:
+        kw = _vector(k_weight, "k_weight", plan.head_dim, device, dtype)
+        weight = _DTYPES[k_weight.dtype]
+    args = AppendArgs(code, weight, rotary, 1 if interleaved else 0, eps, kw, at, rows)
+    _check(load().taps_cache_append(
+        C.byref(args), *plan.pointers(stream, raw, device),
+        _heads(k, "k", device, dtype, plan._k_shape, 3),
+        _heads(v, "v", device, dtype, plan._k_shape, 3),
+        _cache(k_cache, "k_cache", plan, device, dtype),
+        _cache(v_cache, "v_cache", plan, device, dtype), raw), "taps_cache_append")
 
 
 def taps_attend(q, k_cache, v_cache, plan: PagedPlan, scale=None, out=None, lse=False, stream=None):
@@ -455,19 +478,23 @@ def taps_attend(q, k_cache, v_cache, plan: PagedPlan, scale=None, out=None, lse=
     q [tokens, q_heads, dim] -> out of the same shape; a token that sees no key gets
     zeros.  scale: dim ** -0.5 unless given.  lse: also return [tokens, q_heads]
     in 32 bits, the log of every row's sum of exponentials (-inf without keys)."""
-    import torch
-    shape = (plan.tokens, plan.q_heads, plan.head_dim)
-    heads = (_heads(q, "q", q, shape, 3), _cache(k_cache, "k_cache", plan, q),
-             _cache(v_cache, "v_cache", plan, q))
-    with _on(stream):
-        if out is None:
-            out = torch.empty(shape, dtype=q.dtype, device=q.device)
-        sums = torch.empty(shape[:2], dtype=torch.float32, device=q.device) if lse else None
-        n = plan.workspace_bytes
-        workspace = torch.empty(n, dtype=torch.uint8, device=q.device) if n else None
+    device, raw, dtype, shape = _device(), _stream(stream), q.dtype, plan._q_shape
+    code = _dtype(q)
+    qh = _heads(q, "q", device, dtype, shape, 3)
+    kh = _cache(k_cache, "k_cache", plan, device, dtype)
+    vh = _cache(v_cache, "v_cache", plan, device, dtype)
+    n = plan.workspace_bytes
+    sums = workspace = None
+    if out is None:
+        out = _on(stream, lambda: q.new_empty(shape))
+    if lse:
+        sums = _on(stream, lambda: torch.empty(shape[:2], dtype=torch.float32, device=q.device))
+    if n:
+        workspace = _on(stream, lambda: torch.empty(n, dtype=torch.uint8, device=q.device))
     _check(load().taps_attend(
-        _dtype(q), *plan.pointers(stream), *heads,
-        plan.head_dim ** -0.5 if scale is None else scale, _heads(out, "out", q, shape, 3),
+        code, *plan.pointers(stream, raw, device), qh, kh, vh,
+        plan.head_dim ** -0.5 if scale is None else scale,
+        _heads(out, "out", device, dtype, shape, 3),
         None if sums is None else sums.data_ptr(),
-        None if workspace is None else workspace.data_ptr(), n, _stream(stream)), "taps_attend")
+        None if workspace is None else workspace.data_ptr(), n, raw), "taps_attend")
     return (out, sums) if lse else out

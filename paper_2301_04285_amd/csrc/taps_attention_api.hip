@@ -335,10 +335,9 @@ taps_status taps_norm_rotate_backward(const taps_norm_rotate_args *a, taps_heads
     if (!workspace_bytes) return fail(TAPS_ERR_ARG, "workspace_bytes is NULL");
     const bool norms = p.norm[0] || p.norm[1];
     // a partial sum per workgroup; as many workgroups on either path as the other could take
-    const uint64_t need =
-        norms ? up16((uint64_t)std::max(taps_backward_groups(p, true), taps_backward_groups(p, false)) *
-                     2 * p.dim * 4)
-              : 16;
+    const uint64_t groups = std::max(taps_backward_groups(p, true), taps_backward_groups(p, false));
+    const uint64_t need = norms ? up16(groups * 2 * p.dim * 4) : 16;
+    static_assert(TAPS_NORM_ROTATE_WORKSPACE(1) == kMostBackwardGroups * 2 * 4, "as declared");
     if (!workspace) {
         *workspace_bytes = need;
         return TAPS_OK;

@@ -99,7 +99,9 @@ hipError_t taps_launch_norm_rotate(const taps_rows_launch &p, uint32_t dtype, bo
                                    hipStream_t stream);
 hipError_t taps_launch_append(const taps_rows_launch &p, uint32_t dtype, bool vectors,
                               hipStream_t stream);
-// Workgroups of the backward kernel, each of which leaves one partial sum.
+// Workgroups of the backward kernel, each of which leaves one partial sum:
+// enough to fill 256 compute units four times over.
+constexpr uint32_t kMostBackwardGroups = 1024;
 uint32_t taps_backward_groups(const taps_rows_launch &p, bool vectors);
 hipError_t taps_launch_norm_rotate_backward(const taps_rows_launch &p, uint32_t dtype, bool vectors,
                                             void *q_weight_grad, void *k_weight_grad,

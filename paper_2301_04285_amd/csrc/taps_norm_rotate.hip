@@ -516,11 +516,10 @@ hipError_t taps_launch_append(const taps_rows_launch &p, uint32_t dtype, bool ve
     return hipGetLastError();
 }
 
-// Enough workgroups to fill 256 compute units four times over; each leaves a partial sum.
 uint32_t taps_backward_groups(const taps_rows_launch &p, bool vectors) {
     const uint32_t groups = token_groups((uint64_t)p.batch * p.tokens, p.heads[0] + p.heads[1],
                                          lanes_of(p.dim, vectors));
-    return groups < 1 ? 1 : groups < 1024 ? groups : 1024;
+    return groups < 1 ? 1 : groups < kMostBackwardGroups ? groups : kMostBackwardGroups;
 }
 
 hipError_t taps_launch_norm_rotate_backward(const taps_rows_launch &p, uint32_t dtype, bool vectors,

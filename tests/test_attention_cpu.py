@@ -179,7 +179,7 @@ def test_pages_may_be_read_twice_and_gone_pages_are_not_looked_at():
 
 
 def _heads(ptr=0x1000, strides=(512, 512, 64)):
-    return A.Heads(ptr, strides)
+    return A.Heads(ptr, *strides)
 
 
 def _status(call, *args):
@@ -210,7 +210,7 @@ def _args(**kw):
 ])
 def test_norm_rotate_refusals(match, kw):
     a = _args(**kw)
-    none = A.Heads(None, (0, 0, 0))
+    none = A.Heads(None, 0, 0, 0)
     st, said = _status("taps_norm_rotate", C.byref(a), _heads(), none, _heads(), none, None)
     assert st == taps.ERR_ARG and match in said
     need = C.c_uint64()
@@ -220,7 +220,7 @@ def test_norm_rotate_refusals(match, kw):
 
 
 def test_pointer_refusals():
-    none = A.Heads(None, (0, 0, 0))
+    none = A.Heads(None, 0, 0, 0)
     L = A.load()
     assert L.taps_norm_rotate(None, none, none, none, none, None) == taps.ERR_ARG
     a = _args()
@@ -258,7 +258,7 @@ def test_attend_and_append_refusals():
         return _status("taps_attend", dtype, plan, dev, q, kc, vc, scale, out, lse, work, n, None)
     for match, kw in [("TAPS_BF16", {"dtype": A.F32}), ("NULL", {"plan": None}),
                       ("NULL", {"dev": None}), ("16-byte", {"dev": 0x1008}),
-                      ("q is NULL", {"q": A.Heads(None, (0, 0, 0))}),
+                      ("q is NULL", {"q": A.Heads(None, 0, 0, 0)}),
                       ("v_cache: rows", {"vc": _heads(0x1008)}),
                       ("k_cache: rows", {"kc": _heads(strides=(4, 8, 8))}),
                       ("out: rows", {"out": _heads(strides=(0, 8, 12))}),
@@ -291,7 +291,7 @@ def test_attend_and_append_refusals():
     for match, kw in [("dtype", {"dtype": 9}), ("rotary_dim", {"rotary_dim": 66}),
                       ("table is NULL", {"table": None}), ("eps", {"eps": -1.0}),
                       ("positions up to 20", {"n_positions": 19}),
-                      ("k is NULL", {"k": A.Heads(None, (0, 0, 0))}),
+                      ("k is NULL", {"k": A.Heads(None, 0, 0, 0)}),
                       ("k_cache is not aligned", {"kc": _heads(0x1001)}),
                       ("more new tokens than keys", {"plan": short._host.data_ptr()}),
                       ("NULL", {"plan": None}), ("weight_dtype", {"weight_dtype": A.F16})]:
