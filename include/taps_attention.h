@@ -83,13 +83,15 @@ typedef struct {
 
 /* q_out = rotate(norm(q)), k_out = rotate(norm(k)), with
  *   norm(x)_i = x_i (mean_j x_j^2 + eps)^(-1/2) weight_i.
+ * k and k_out are not looked at (and may be NULL) if k_heads is 0.
  * q_out may be q and k_out k (the same data and strides); otherwise outputs
  * overlap nothing.  first_position .. first_position + tokens - 1 must be
  * rows of the table (TAPS_ERR_ARG); a value of `positions` that is not one
  * makes that token's outputs NaN (in the gradients: those of its inputs and
  * of the weights). */
-taps_status taps_norm_rotate(const taps_norm_rotate_args *args, taps_heads q, taps_heads k,
-                             taps_heads q_out, taps_heads k_out, void *stream);
+taps_status taps_norm_rotate(const taps_norm_rotate_args *args, const taps_heads *q,
+                             const taps_heads *k, const taps_heads *q_out, const taps_heads *k_out,
+                             void *stream);
 
 /* The gradients of taps_norm_rotate: from those of its outputs (dq_out,
  * dk_out) and its inputs (q, k) to those of its inputs (dq, dk) and weights
@@ -99,10 +101,12 @@ taps_status taps_norm_rotate(const taps_norm_rotate_args *args, taps_heads q, ta
  * `workspace` (device, 16-byte aligned) holds partial sums; with workspace
  * NULL the call only writes the bytes it needs to *workspace_bytes, otherwise
  * *workspace_bytes says how many there are (TAPS_ERR_CAPACITY if too few). */
-taps_status taps_norm_rotate_backward(const taps_norm_rotate_args *args, taps_heads dq_out,
-                                      taps_heads dk_out, taps_heads q, taps_heads k, taps_heads dq,
-                                      taps_heads dk, void *q_weight_grad, void *k_weight_grad,
-                                      void *workspace, uint64_t *workspace_bytes, void *stream);
+taps_status taps_norm_rotate_backward(const taps_norm_rotate_args *args, const taps_heads *dq_out,
+                                      const taps_heads *dk_out, const taps_heads *q,
+                                      const taps_heads *k, const taps_heads *dq,
+                                      const taps_heads *dk, void *q_weight_grad,
+                                      void *k_weight_grad, void *workspace,
+                                      uint64_t *workspace_bytes, void *stream);
 
 /* The sequences of one step.  After the append of its q_lens[s] new tokens,
  * sequence s has kv_lens[s] keys; key j is in page
@@ -151,8 +155,9 @@ typedef struct {
  * values into the cache.  TAPS_ERR_ARG if a token's position is not a row of the
  * table or the plan has a sequence with kv_lens < q_lens. */
 taps_status taps_cache_append(const taps_append_args *args, const void *plan,
-                              const void *plan_device, taps_heads k, taps_heads v,
-                              taps_heads k_cache, taps_heads v_cache, void *stream);
+                              const void *plan_device, const taps_heads *k, const taps_heads *v,
+                              const taps_heads *k_cache, const taps_heads *v_cache,
+                              void *stream);
 
 /* out = softmax(scale q k^T) v over the keys each token sees; query head h
  * reads key head h / (q_heads / kv_heads).  A token that sees no key gets
@@ -163,9 +168,10 @@ taps_status taps_cache_append(const taps_append_args *args, const void *plan,
  *          exp(scale q k) of every token and head.
  *   workspace  device, 16-byte aligned, workspace_bytes as the plan said.
  * Every data pointer must be 16-byte aligned and every stride used a multiple of 8. */
-taps_status taps_attend(uint32_t dtype, const void *plan, const void *plan_device, taps_heads q,
-                        taps_heads k_cache, taps_heads v_cache, float scale, taps_heads out,
-                        float *lse, void *workspace, uint64_t workspace_bytes, void *stream);
+taps_status taps_attend(uint32_t dtype, const void *plan, const void *plan_device,
+                        const taps_heads *q, const taps_heads *k_cache, const taps_heads *v_cache,
+                        float scale, const taps_heads *out, float *lse, void *workspace,
+                        uint64_t workspace_bytes, void *stream);
 
 /* Description of the calling thread's last failure ("" if none). */
 const char *taps_attention_last_error(void);

@@ -78,20 +78,21 @@ def load():
         L = C.CDLL(LIB_PATH)
         P = C.POINTER
         L.taps_norm_rotate.restype = C.c_int
-        L.taps_norm_rotate.argtypes = [P(NormRotateArgs), Heads, Heads, Heads, Heads, C.c_void_p]
+        H = P(Heads)
+        L.taps_norm_rotate.argtypes = [P(NormRotateArgs), H, H, H, H, C.c_void_p]
         L.taps_norm_rotate_backward.restype = C.c_int
-        L.taps_norm_rotate_backward.argtypes = [P(NormRotateArgs), Heads, Heads, Heads, Heads,
-                                                Heads, Heads, C.c_void_p, C.c_void_p, C.c_void_p,
+        L.taps_norm_rotate_backward.argtypes = [P(NormRotateArgs), H, H, H, H, H, H,
+                                                C.c_void_p, C.c_void_p, C.c_void_p,
                                                 P(C.c_uint64), C.c_void_p]
         L.taps_paged_plan.restype = C.c_int
         L.taps_paged_plan.argtypes = [P(PagedBatch), C.c_uint32, C.c_void_p, P(C.c_uint64),
                                       P(C.c_uint64)]
         L.taps_cache_append.restype = C.c_int
-        L.taps_cache_append.argtypes = [P(AppendArgs), C.c_void_p, C.c_void_p, Heads, Heads, Heads,
-                                        Heads, C.c_void_p]
+        L.taps_cache_append.argtypes = [P(AppendArgs), C.c_void_p, C.c_void_p, H, H, H, H,
+                                        C.c_void_p]
         L.taps_attend.restype = C.c_int
-        L.taps_attend.argtypes = [C.c_uint32, C.c_void_p, C.c_void_p, Heads, Heads, Heads,
-                                  C.c_float, Heads, C.c_void_p, C.c_void_p, C.c_uint64, C.c_void_p]
+        L.taps_attend.argtypes = [C.c_uint32, C.c_void_p, C.c_void_p, H, H, H, C.c_float, H,
+                                  C.c_void_p, C.c_void_p, C.c_uint64, C.c_void_p]
         L.taps_attention_last_error.restype = C.c_char_p
         L.taps_attention_last_error.argtypes = []
         _lib = L
@@ -158,8 +159,6 @@ def _heads(t, what: str, device: int, dtype, shape, rank: int) -> Heads:
     return Heads(t.data_ptr(), s[0], s[1], s[2])
 
 
-_NONE = Heads(None, 0, 0, 0)
-
 
 def _vector(w, what: str, dim: int, device: int, dtype) -> int:
     """Pointer to a head's weights."""
@@ -183,6 +182,9 @@ def _table(table, dim: int, device: int):
     if 2 * shape[2] > dim:
         raise ValueError(f"table rotates {2 * shape[2]} of {dim} elements")
     return table.data_ptr(), shape[0], 2 * shape[2]
+
+
+_like = torch.empty_like   # of every way to an output the shortest
 
 
 def _on(stream, make):
@@ -262,14 +264,14 @@ def taps_norm_rotate(q, k, q_weight, k_weight, table, positions=None, first=0, e
                              device)
     dtype, shape = q.dtype, q.shape
     rank = len(shape)
-    kh = _NONE if k is None else _heads(k, "k", device, dtype, k.shape, rank)
+    kh = None if k is None else _heads(k, "k", device, dtype, k.shape, rank)
     qh = _heads(q, "q", device, dtype, shape, rank)
     if out is None:   # dense even where q and k are slices of one projection
-        out = _on(stream, lambda: (q.new_empty(shape), None if k is None else k.new_empty(k.shape)))
+        out = _on(stream, lambda: (_like(q), None if k is None else _like(k)))
     q_out, k_out = out
     _check(load().taps_norm_rotate(
         C.byref(args), qh, kh, _heads(q_out, "out[0]", device, dtype, shape, rank),
-        _NONE if k is None else _heads(k_out, "out[1]", device, dtype, k.shape, rank),
+        None if k is None else _heads(k_out, "out[1]", device, dtype, k.shape, rank),
         _stream(stream)), "taps_norm_rotate")
     return q_out, k_out
 
@@ -287,16 +289,16 @@ def taps_norm_rotate_backward(dq_out, dk_out, q, k, q_weight, k_weight, table, p
     rank = len(shape)
     qh = _heads(q, "q", device, dtype, shape, rank)
     gqh = _heads(dq_out, "dq_out", device, dtype, shape, rank)
-    kh = gkh = dkh = _NONE
+    kh = gkh = dkh = None
     if k is not None:
         kh = _heads(k, "k", device, dtype, k.shape, rank)
         gkh = _heads(dk_out, "dk_out", device, dtype, k.shape, rank)
     size = WORKSPACE_PER_ELEMENT * shape[-1]
 
     def make():
-        return (q.new_empty(shape), None if k is None else k.new_empty(k.shape),
-                None if q_weight is None else q_weight.new_empty(q_weight.shape),
-                None if k_weight is None else k_weight.new_empty(k_weight.shape),
+        return (_like(q), None if k is None else _like(k),
+                None if q_weight is None else _like(q_weight),
+                None if k_weight is None else _like(k_weight),
                 torch.empty(size, dtype=torch.uint8, device=q.device))
     dq, dk, dqw, dkw, workspace = _on(stream, make)
     if k is not None:
@@ -486,7 +488,7 @@ def taps_attend(q, k_cache, v_cache, plan: PagedPlan, scale=None, out=None, lse=
     n = plan.workspace_bytes
     sums = workspace = None
     if out is None:
-        out = _on(stream, lambda: q.new_empty(shape))
+        out = _on(stream, lambda: _like(q))
     if lse:
         sums = _on(stream, lambda: torch.empty(shape[:2], dtype=torch.float32, device=q.device))
     if n:

@@ -51,9 +51,9 @@ taps_status check_types(uint32_t dtype, uint32_t weight_dtype, uint32_t dim, uin
     return TAPS_OK;
 }
 
-taps_status check_heads(const taps_heads &t, const char *what, uint32_t dtype) {
-    if (!t.data) return fail(TAPS_ERR_ARG, "%s is NULL", what);
-    if (!aligned(t.data, size_of(dtype)))
+taps_status check_heads(const taps_heads *t, const char *what, uint32_t dtype) {
+    if (!t || !t->data) return fail(TAPS_ERR_ARG, "%s is NULL", what);
+    if (!aligned(t->data, size_of(dtype)))
         return fail(TAPS_ERR_ARG, "%s is not aligned to its elements", what);
     return TAPS_OK;
 }
@@ -306,29 +306,29 @@ taps_status check_plan(const void *plan, const void *plan_device, const taps_pla
 
 extern "C" {
 
-taps_status taps_norm_rotate(const taps_norm_rotate_args *a, taps_heads q, taps_heads k,
-                             taps_heads q_out, taps_heads k_out, void *stream) {
+taps_status taps_norm_rotate(const taps_norm_rotate_args *a, const taps_heads *q, const taps_heads *k,
+                             const taps_heads *q_out, const taps_heads *k_out, void *stream) {
     taps_rows_launch p;
     if (taps_status st = check_norm_rotate(a, &p)) return st;
     if (!a->batch || !a->tokens) return TAPS_OK;
-    const taps_heads src[2] = {q, k}, dst[2] = {q_out, k_out};
+    const taps_heads *const src[2] = {q, k}, *const dst[2] = {q_out, k_out};
     static const char *const names[2][2] = {{"q", "q_out"}, {"k", "k_out"}};
     bool vectors = vectors_fit(p.dim, p.rotary, a->weight_dtype, a->q_weight, a->k_weight, a->table);
     for (int side = 0; side < (a->k_heads ? 2 : 1); ++side) {
         if (taps_status st = check_heads(src[side], names[side][0], a->dtype)) return st;
         if (taps_status st = check_heads(dst[side], names[side][1], a->dtype)) return st;
-        p.src[side] = src[side].data, p.dst[side] = dst[side].data;
-        set_strides(p.src_stride[side], src[side]);
-        set_strides(p.dst_stride[side], dst[side]);
-        vectors = vectors && by_fours(src[side], a->dtype) && by_fours(dst[side], a->dtype);
+        p.src[side] = src[side]->data, p.dst[side] = dst[side]->data;
+        set_strides(p.src_stride[side], *src[side]);
+        set_strides(p.dst_stride[side], *dst[side]);
+        vectors = vectors && by_fours(*src[side], a->dtype) && by_fours(*dst[side], a->dtype);
     }
     return launched(taps_launch_norm_rotate(p, a->dtype, vectors, (hipStream_t)stream),
                     "taps_norm_rotate");
 }
 
-taps_status taps_norm_rotate_backward(const taps_norm_rotate_args *a, taps_heads dq_out,
-                                      taps_heads dk_out, taps_heads q, taps_heads k, taps_heads dq,
-                                      taps_heads dk, void *q_weight_grad, void *k_weight_grad,
+taps_status taps_norm_rotate_backward(const taps_norm_rotate_args *a, const taps_heads *dq_out,
+                                      const taps_heads *dk_out, const taps_heads *q, const taps_heads *k, const taps_heads *dq,
+                                      const taps_heads *dk, void *q_weight_grad, void *k_weight_grad,
                                       void *workspace, uint64_t *workspace_bytes, void *stream) {
     taps_rows_launch p;
     if (taps_status st = check_norm_rotate(a, &p)) return st;
@@ -354,19 +354,19 @@ taps_status taps_norm_rotate_backward(const taps_norm_rotate_args *a, taps_heads
     const uint32_t w = size_of(a->weight_dtype);
     if (!aligned(q_weight_grad, w) || !aligned(k_weight_grad, w))
         return fail(TAPS_ERR_ARG, "a weight's gradient is not aligned to its elements");
-    const taps_heads g[2] = {dq_out, dk_out}, x[2] = {q, k}, d[2] = {dq, dk};
+    const taps_heads *const g[2] = {dq_out, dk_out}, *const x[2] = {q, k}, *const d[2] = {dq, dk};
     static const char *const names[2][3] = {{"dq_out", "q", "dq"}, {"dk_out", "k", "dk"}};
     bool vectors = vectors_fit(p.dim, p.rotary, a->weight_dtype, a->q_weight, a->k_weight, a->table);
     for (uint32_t side = 0; side < sides && a->batch && a->tokens; ++side) {
         if (taps_status st = check_heads(g[side], names[side][0], a->dtype)) return st;
         if (taps_status st = check_heads(x[side], names[side][1], a->dtype)) return st;
         if (taps_status st = check_heads(d[side], names[side][2], a->dtype)) return st;
-        p.src[side] = g[side].data, p.x[side] = x[side].data, p.dst[side] = d[side].data;
-        set_strides(p.src_stride[side], g[side]);
-        set_strides(p.x_stride[side], x[side]);
-        set_strides(p.dst_stride[side], d[side]);
-        vectors = vectors && by_fours(g[side], a->dtype) && by_fours(x[side], a->dtype) &&
-                  by_fours(d[side], a->dtype);
+        p.src[side] = g[side]->data, p.x[side] = x[side]->data, p.dst[side] = d[side]->data;
+        set_strides(p.src_stride[side], *g[side]);
+        set_strides(p.x_stride[side], *x[side]);
+        set_strides(p.dst_stride[side], *d[side]);
+        vectors = vectors && by_fours(*g[side], a->dtype) && by_fours(*x[side], a->dtype) &&
+                  by_fours(*d[side], a->dtype);
     }
     if (!norms && (!a->batch || !a->tokens)) return TAPS_OK;
     p.partial = norms ? (float *)workspace : nullptr;
@@ -415,7 +415,7 @@ taps_status taps_paged_plan(const taps_paged_batch *b, uint32_t cus, void *plan,
 }
 
 taps_status taps_cache_append(const taps_append_args *a, const void *plan, const void *plan_device,
-                              taps_heads k, taps_heads v, taps_heads k_cache, taps_heads v_cache,
+                              const taps_heads *k, const taps_heads *v, const taps_heads *k_cache, const taps_heads *v_cache,
                               void *stream) {
     if (!a) return fail(TAPS_ERR_ARG, "args is NULL");
     const taps_plan_header *h;
@@ -430,20 +430,20 @@ taps_status taps_cache_append(const taps_append_args *a, const void *plan, const
                     a->n_positions);
     if (!h->tokens) return TAPS_OK;
     taps_rows_launch p{};
-    const taps_heads src[2] = {k, v}, dst[2] = {k_cache, v_cache};
+    const taps_heads *const src[2] = {k, v}, *const dst[2] = {k_cache, v_cache};
     static const char *const names[2][2] = {{"k", "k_cache"}, {"v", "v_cache"}};
     bool vectors =
         vectors_fit(h->head_dim, a->rotary_dim, a->weight_dtype, a->k_weight, nullptr, a->table);
     for (int side = 0; side < 2; ++side) {
         if (taps_status st = check_heads(src[side], names[side][0], a->dtype)) return st;
         if (taps_status st = check_heads(dst[side], names[side][1], a->dtype)) return st;
-        p.src[side] = src[side].data, p.dst[side] = dst[side].data;
-        set_strides(p.src_stride[side], src[side]);
+        p.src[side] = src[side]->data, p.dst[side] = dst[side]->data;
+        set_strides(p.src_stride[side], *src[side]);
         p.src_stride[side][0] = 0;
-        set_strides(p.dst_stride[side], dst[side]);
-        taps_heads rows = src[side];
+        set_strides(p.dst_stride[side], *dst[side]);
+        taps_heads rows = *src[side];
         rows.stride[0] = 0;   // not used
-        vectors = vectors && by_fours(rows, a->dtype) && by_fours(dst[side], a->dtype);
+        vectors = vectors && by_fours(rows, a->dtype) && by_fours(*dst[side], a->dtype);
     }
     p.plan_tokens = (const taps_plan_token *)((const char *)plan_device + h->tokens_at);
     p.weight[0] = a->k_weight;
@@ -461,8 +461,8 @@ taps_status taps_cache_append(const taps_append_args *a, const void *plan, const
                     "taps_cache_append");
 }
 
-taps_status taps_attend(uint32_t dtype, const void *plan, const void *plan_device, taps_heads q,
-                        taps_heads k_cache, taps_heads v_cache, float scale, taps_heads out,
+taps_status taps_attend(uint32_t dtype, const void *plan, const void *plan_device, const taps_heads *q,
+                        const taps_heads *k_cache, const taps_heads *v_cache, float scale, const taps_heads *out,
                         float *lse, void *workspace, uint64_t workspace_bytes, void *stream) {
     if (dtype != TAPS_BF16 && dtype != TAPS_F16)
         return fail(TAPS_ERR_ARG, "dtype %u is neither TAPS_BF16 nor TAPS_F16", dtype);
@@ -474,13 +474,13 @@ taps_status taps_attend(uint32_t dtype, const void *plan, const void *plan_devic
     if (!(scale > 0.f) || std::isinf(scale))
         return fail(TAPS_ERR_ARG, "scale is not positive and finite");
     if (!h->tokens) return TAPS_OK;
-    const taps_heads all[4] = {q, k_cache, v_cache, out};
+    const taps_heads *const all[4] = {q, k_cache, v_cache, out};
     static const char *const names[4] = {"q", "k_cache", "v_cache", "out"};
     for (int i = 0; i < 4; ++i) {
         const bool cache = i == 1 || i == 2;
-        if (!all[i].data) return fail(TAPS_ERR_ARG, "%s is NULL", names[i]);
-        if (!aligned(all[i].data, 16) || (cache && all[i].stride[0] % 8) || all[i].stride[1] % 8 ||
-            all[i].stride[2] % 8)
+        if (!all[i] || !all[i]->data) return fail(TAPS_ERR_ARG, "%s is NULL", names[i]);
+        if (!aligned(all[i]->data, 16) || (cache && all[i]->stride[0] % 8) || all[i]->stride[1] % 8 ||
+            all[i]->stride[2] % 8)
             return fail(TAPS_ERR_ARG, "%s: rows do not start at multiples of 16 bytes", names[i]);
     }
     if (!aligned(lse, 4)) return fail(TAPS_ERR_ARG, "lse is not aligned to its elements");
@@ -492,8 +492,8 @@ taps_status taps_attend(uint32_t dtype, const void *plan, const void *plan_devic
     if (!aligned(workspace, 16)) return fail(TAPS_ERR_ARG, "workspace is not 16-byte aligned");
     taps_attend_launch p{};
     const char *dev = (const char *)plan_device;
-    p.q = (const char *)q.data, p.out = (char *)out.data, p.lse = lse;
-    p.k_cache = (const char *)k_cache.data, p.v_cache = (const char *)v_cache.data;
+    p.q = (const char *)q->data, p.out = (char *)out->data, p.lse = lse;
+    p.k_cache = (const char *)k_cache->data, p.v_cache = (const char *)v_cache->data;
     p.zeros = dev + offsetof(taps_plan_header, zeros);
     p.part_o = (float *)workspace;
     p.part_ml = (float *)((char *)workspace +
@@ -502,12 +502,12 @@ taps_status taps_attend(uint32_t dtype, const void *plan, const void *plan_devic
     p.pages = (const int32_t *)(dev + h->pages_at);
     p.items = (const taps_plan_item *)(dev + h->items_at);
     p.joins = (const taps_plan_join *)(dev + h->joins_at);
-    p.q_token = 2 * q.stride[1], p.q_head = 2 * q.stride[2];
-    p.o_token = 2 * out.stride[1], p.o_head = 2 * out.stride[2];
-    p.k_page = 2 * k_cache.stride[0], p.k_head = 2 * k_cache.stride[1];
-    p.k_slot = 2 * k_cache.stride[2];
-    p.v_page = 2 * v_cache.stride[0], p.v_head = 2 * v_cache.stride[1];
-    p.v_slot = 2 * v_cache.stride[2];
+    p.q_token = 2 * q->stride[1], p.q_head = 2 * q->stride[2];
+    p.o_token = 2 * out->stride[1], p.o_head = 2 * out->stride[2];
+    p.k_page = 2 * k_cache->stride[0], p.k_head = 2 * k_cache->stride[1];
+    p.k_slot = 2 * k_cache->stride[2];
+    p.v_page = 2 * v_cache->stride[0], p.v_head = 2 * v_cache->stride[1];
+    p.v_slot = 2 * v_cache->stride[2];
     p.n_items = h->n_items, p.n_joins = h->n_joins, p.join_rounds = h->join_rounds;
     p.q_heads = h->q_heads, p.kv_heads = h->kv_heads, p.group = h->q_heads / h->kv_heads;
     p.dim = h->head_dim;
