@@ -129,7 +129,13 @@ __device__ __forceinline__ void load_to_lds(const char *from, uint32_t lds) {
                  : "s"(lds), "v"(from)
                  : "memory", "m0");
 }
-__device__ __forceinline__ void wait_loads() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
+// (the builtin, unlike an instruction in asm, tells the compiler too that no
+// load of its own is under way, or it would wait again inside the loop)
+__device__ __forceinline__ void wait_loads() {
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_waitcnt(0x0f70);   // vmcnt(0)
+    asm volatile("" ::: "memory");
+}
 
 // A wavefront's share of a tile: groups of 16 keys, which share a page.  Lane
 // by lane it takes the chunks in the order in which they lie in LDS.

@@ -135,10 +135,15 @@ struct Strip {
     int64_t cost() const { return (int64_t)(hi - lo) * (narrow ? 2 : 1); }
 };
 
-// Keys below which a strip is not split further, and the pieces per compute
-// unit that the whole step is cut into.
-constexpr int64_t kLeastPiece = 256;
-constexpr int64_t kPiecesPerUnit = 2;
+// Pieces shorter than this are not made: a split costs a launch and a pass
+// over partial results, some 5 us, in which a workgroup takes about this many
+// keys (one token over 1024 keys of 16 heads: 11.3 us whole, 13.7 in four).
+constexpr int64_t kLeastPiece = 1024;
+// Pieces per compute unit that a step is cut into.  Two narrow ones fill a
+// unit and their bytes set the time; wide ones do not all take the same time,
+// and with twice as many the last ones end sooner (512 tokens over 32768 keys:
+// 425 us at two a unit, 370 at four; two tokens over 131001: 187 and 192).
+constexpr int64_t kNarrowPieces = 2, kWidePieces = 4;
 
 taps_status lay_out(const taps_paged_batch *b, uint32_t cus, Layout *out) {
     taps_plan_header &h = out->head;
@@ -210,10 +215,10 @@ taps_status lay_out(const taps_paged_batch *b, uint32_t cus, Layout *out) {
     int64_t total = 0;
     for (const Strip &t : strips) total += t.cost();
     total *= b->kv_heads;
-    const int64_t target = total / ((int64_t)cus * kPiecesPerUnit) + 1;
     uint64_t part_rows = 0;
     for (const Strip &t : strips) {
         const int64_t keys = t.hi - t.lo;
+        const int64_t target = total / (cus * (t.narrow ? kNarrowPieces : kWidePieces)) + 1;
         int64_t parts = std::min((t.cost() + target - 1) / target, keys / kLeastPiece);
         parts = std::max<int64_t>(1, std::min<int64_t>(parts, 256));
         // whole tiles, counted from where the strip's first tile starts
