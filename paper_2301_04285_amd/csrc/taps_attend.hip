@@ -29,13 +29,12 @@
 
 namespace {
 
-constexpr int kThreads = 256, kWaves = 4;
+constexpr int kThreads = 256, kWaves = 4, kWideThreads = 2 * kWideRows;
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 constexpr float kMinusInf = -__builtin_inff();
-// A row's maximum is raised only when a tile exceeds it by this much (in
-// powers of two): numerators stay below 2^8, far inside every type's range,
-// and most tiles leave the accumulators alone.
-constexpr float kSlack = 8.f;
+// A row's maximum is raised only when a tile's numerators (this lane's 16 or 32) add up to more than this: none exceeds it, far inside every
+// type's range, and most tiles neither look for their maximum nor touch the accumulators.
+constexpr float kMostSum = 4096.f;
 
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
@@ -109,10 +108,9 @@ template <int D> struct Tile {
 };
 
 constexpr int max_of(int a, int b) { return a > b ? a : b; }
-template <int D> constexpr int shared_bytes() {
-    return max_of(2 * Tile<D>::bytes(kWideKeys),
-                  max_of(kWaves * Tile<D>::bytes(kNarrowKeys),
-                         kWaves * kNarrowRows * (D + 4) * 4) + kWaves * kNarrowRows * 2 * 4);
+template <int D> constexpr int narrow_bytes() {
+    return max_of(kWaves * Tile<D>::bytes(kNarrowKeys), kWaves * kNarrowRows * (D + 4) * 4) +
+           kWaves * kNarrowRows * 2 * 4;
 }
 
 // The LDS address of a generic pointer to LDS.
@@ -129,11 +127,20 @@ __device__ __forceinline__ void load_to_lds(const char *from, uint32_t lds) {
                  : "s"(lds), "v"(from)
                  : "memory", "m0");
 }
+// The same from a uniform address and an offset a lane.
+__device__ __forceinline__ void load_to_lds(const char *from, uint32_t offset, uint32_t lds) {
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2"
+                 :
+                 : "s"(lds), "v"(offset), "s"(from)
+                 : "memory", "m0");
+}
 // (the builtin, unlike an instruction in asm, tells the compiler too that no
 // load of its own is under way, or it would wait again inside the loop)
-__device__ __forceinline__ void wait_loads() {
+// All but the newest Left loads have ended.
+template <int Left> __device__ __forceinline__ void wait_loads() {
+    static_assert(Left < 16, "four bits");
     asm volatile("" ::: "memory");
-    __builtin_amdgcn_s_waitcnt(0x0f70);   // vmcnt(0)
+    __builtin_amdgcn_s_waitcnt(0x0f70 | Left);   // vmcnt(Left)
     asm volatile("" ::: "memory");
 }
 
@@ -173,6 +180,9 @@ __device__ __forceinline__ int page_at(const taps_attend_launch &p, const int32_
     return *(const __attribute__((address_space(4))) int32_t *)(uintptr_t)(pages + at);
 }
 
+// Classes of instructions of __builtin_amdgcn_sched_group_barrier.
+constexpr int kMfmas = 0x8, kDsReads = 0x100;
+
 // One wavefront's 32 query rows: the rows' operand, running statistics and result.
 template <class T, int D> struct Rows {
     static constexpr int kSteps = D / 16, kBlocks = D / 32;
@@ -181,19 +191,19 @@ template <class T, int D> struct Rows {
     float m, l;        // maximum of the scores, this lane's half of the sum
     int first, last;   // keys of the item this lane's row sees: first .. last
 
-    __device__ __forceinline__ void start(const taps_attend_launch &p, const taps_plan_seq &s,
-                                          uint32_t head, int row, int lo, int hi, int lane) {
-        const bool real = row < s.rows;
+    __device__ __forceinline__ void start(const taps_attend_launch &p, const taps_plan_item &item,
+                                          uint32_t head, int row, int lane) {
+        const bool real = row < item.rows;
         const int token = row / (int)p.group, sub = row - token * (int)p.group;
-        const int pos = s.first_pos + token;
-        first = lo;
-        last = hi - 1;
+        const int pos = item.first_pos + token;
+        first = item.lo;
+        last = item.hi - 1;
         if (p.causal) {
             last = min(last, pos);
             if (p.window) first = max(first, pos - (int)p.window + 1);
         }
         if (!real) last = -1, first = 0;
-        const char *at = p.q + (int64_t)(s.token0 + token) * p.q_token +
+        const char *at = p.q + (int64_t)(item.token0 + token) * p.q_token +
                          (int64_t)(head * p.group + sub) * p.q_head;
 #pragma unroll
         for (int k = 0; k < kSteps; ++k) {
@@ -207,38 +217,54 @@ template <class T, int D> struct Rows {
         for (int b = 0; b < kBlocks; ++b) o[b] = f32x16{};
     }
 
-    // Takes Keys keys from LDS; t0 is the first one's number.  `c` = scale log2 e.
+    // Scores of Keys keys, and the numerators they become, as the second
+    // product's operands.
+    template <int Keys> struct Scores {
+        f32x16 s[Keys / 32];
+    };
+    template <int Keys> struct Numerators {
+        u32x4 p[Keys / 16];
+    };
+
+    // First product: K is in LDS.
     template <int Keys>
-    __device__ __forceinline__ void take(const char *lds, int t0, bool masked, float c, int lane) {
-        constexpr int kSub = Keys / 32, kRow = Tile<D>::kRow;
-        const int half = lane >> 5;
-        f32x16 s[kSub];
-        const int k_mask = Tile<D>::k_mask(lane & 31);   // the same for key + 32
+    __device__ __forceinline__ void score(const char *k_lds, Scores<Keys> &x, int lane) const {
+        const int half = lane >> 5, k_mask = Tile<D>::k_mask(lane & 31);   // the same for key + 32
 #pragma unroll
-        for (int n = 0; n < kSub; ++n) s[n] = f32x16{};
+        for (int n = 0; n < Keys / 32; ++n) x.s[n] = f32x16{};
 #pragma unroll
         for (int k = 0; k < kSteps; ++k) {
-            const char *at = lds + (lane & 31) * kRow + 16 * ((2 * k + half) ^ k_mask);
+            const char *at = k_lds + (lane & 31) * Tile<D>::kRow + 16 * ((2 * k + half) ^ k_mask);
 #pragma unroll
-            for (int n = 0; n < kSub; ++n)
-                s[n] = Mfma<T>::run(*(const s16x8 *)(at + 32 * n * kRow), q[k], s[n]);
+            for (int n = 0; n < Keys / 32; ++n)
+                x.s[n] = Mfma<T>::run(*(const s16x8 *)(at + 32 * n * Tile<D>::kRow), q[k], x.s[n]);
         }
+    }
+
+    // Hides the keys this row does not see (t0: the first key's number) and
+    // makes the numerators from the maximum as it is; only where their sum shows
+    // that it lies too far below a score is it raised and are they made anew.
+    // `c` = scale log2 e.
+    template <int Keys>
+    __device__ __forceinline__ void soften(Scores<Keys> &x, Numerators<Keys> &y, int t0, bool masked,
+                                           float c, int lane) {
         if (masked) {
-            const uint32_t seen = max(last - first + 1, 0), at = t0 + 4 * half - first;
+            const uint32_t seen = max(last - first + 1, 0), at = t0 + 4 * (lane >> 5) - first;
 #pragma unroll
-            for (int n = 0; n < kSub; ++n)
+            for (int n = 0; n < Keys / 32; ++n)
 #pragma unroll
                 for (int i = 0; i < 16; ++i)
-                    s[n][i] = at + (32 * n + 8 * (i / 4) + i % 4) < seen ? s[n][i] : kMinusInf;
+                    x.s[n][i] = at + (32 * n + 8 * (i / 4) + i % 4) < seen ? x.s[n][i] : kMinusInf;
         }
-        float most = s[0][0];
+        float sum = numerators(x, y, c);
+        // the first keys, and scores above the maximum by kSlack or more
+        if (__any(m == kMinusInf || sum > kMostSum)) {
+            float most = x.s[0][0];
 #pragma unroll
-        for (int n = 0; n < kSub; ++n)
+            for (int n = 0; n < Keys / 32; ++n)
 #pragma unroll
-            for (int i = 0; i < 16; ++i) most = fmaxf(most, s[n][i]);
-        most = half_max(most);
-        if (__any(most * c > m * c + kSlack)) {
-            const float to = fmaxf(m, most);
+                for (int i = 0; i < 16; ++i) most = fmaxf(most, x.s[n][i]);
+            const float to = fmaxf(m, half_max(most));
             const float by = to == kMinusInf ? 1.f : __builtin_amdgcn_exp2f((m - to) * c);
             m = to;
             l *= by;
@@ -246,36 +272,75 @@ template <class T, int D> struct Rows {
             for (int b = 0; b < kBlocks; ++b)
 #pragma unroll
                 for (int i = 0; i < 16; ++i) o[b][i] *= by;
+            sum = numerators(x, y, c);
         }
+        l += sum;
+    }
+    template <int Keys>
+    __device__ __forceinline__ float numerators(const Scores<Keys> &x, Numerators<Keys> &y,
+                                                float c) const {
         const float shift = m == kMinusInf ? 0.f : m * c;
-        uint32_t pt[kSub][8];
+        float sum[2] = {0.f, 0.f};
 #pragma unroll
-        for (int n = 0; n < kSub; ++n)
+        for (int n = 0; n < Keys / 32; ++n)
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                const float a = __builtin_amdgcn_exp2f(s[n][2 * i] * c - shift);
-                const float b = __builtin_amdgcn_exp2f(s[n][2 * i + 1] * c - shift);
-                l += a + b;
-                pt[n][i] = pack2<T>(a, b);
+                const float e = __builtin_amdgcn_exp2f(x.s[n][2 * i] * c - shift);
+                const float f = __builtin_amdgcn_exp2f(x.s[n][2 * i + 1] * c - shift);
+                sum[0] += e, sum[1] += f;
+                y.p[2 * n + i / 4][i % 4] = pack2<T>(e, f);
             }
+        return sum[0] + sum[1];
+    }
+
+    // Second product: V is in LDS.
+    template <int Keys>
+    __device__ __forceinline__ void spend(const char *v_lds, const Numerators<Keys> &y, int lane) {
+        constexpr int kRow = Tile<D>::kRow;
+        const int half = lane >> 5;
         // lane of a group of 16: key (lane % 16) / 4, columns 4 (lane % 4) ..
         const int v_key = 4 * half + (lane & 15) / 4;
         const int v_chunk = 2 * ((lane >> 4) & 1) + ((lane >> 1) & 1);
         const int v_mask = Tile<D>::v_mask(v_key);   // the same for keys 8 and 16 further
-        const char *v0 = lds + (Keys + v_key) * kRow + 8 * (lane & 1);
+        const char *v0 = v_lds + v_key * kRow + 8 * (lane & 1);
 #pragma unroll
-        for (int n = 0; n < kSub; ++n)
+        for (int n = 0; n < Keys / 16; ++n)
 #pragma unroll
-            for (int k = 0; k < 2; ++k) {
-                const u32x4 pb = {pt[n][4 * k], pt[n][4 * k + 1], pt[n][4 * k + 2], pt[n][4 * k + 3]};
-#pragma unroll
-                for (int b = 0; b < kBlocks; ++b) {
-                    const char *at = v0 + 16 * ((4 * b + v_chunk) ^ v_mask) + (32 * n + 16 * k) * kRow;
-                    const s16x4 u = transposed(at), w = transposed(at + 8 * kRow);
-                    const s16x8 va = {u[0], u[1], u[2], u[3], w[0], w[1], w[2], w[3]};
-                    o[b] = Mfma<T>::run(va, __builtin_bit_cast(s16x8, pb), o[b]);
-                }
+            for (int b = 0; b < kBlocks; ++b) {
+                const char *at = v0 + 16 * ((4 * b + v_chunk) ^ v_mask) + 16 * n * kRow;
+                const s16x4 u = transposed(at), w = transposed(at + 8 * kRow);
+                const s16x8 va = {u[0], u[1], u[2], u[3], w[0], w[1], w[2], w[3]};
+                o[b] = Mfma<T>::run(va, __builtin_bit_cast(s16x8, y.p[n]), o[b]);
             }
+    }
+
+    // Both: the last tile's numerators by its values, this tile's scores.  The
+    // reads of LDS run kAhead operands ahead of the products, which the scheduler
+    // would not do by itself (it waited for each pair: 1700 clocks for 32
+    // products of 32 clocks, 1300 so).
+    template <int Keys>
+    __device__ __forceinline__ void products(const char *v_lds, const Numerators<Keys> &y,
+                                             const char *k_lds, Scores<Keys> &x, int lane) {
+        constexpr int kV = Keys / 16 * kBlocks, kK = Keys / 32 * kSteps, kAhead = 6;
+        // before the other wavefront's softmax, which finds issue slots enough between the products
+        __builtin_amdgcn_s_setprio(1);
+        __builtin_amdgcn_sched_barrier(0);
+        spend(v_lds, y, lane);
+        score(k_lds, x, lane);
+        __builtin_amdgcn_sched_group_barrier(kDsReads, 2 * kAhead, 0);
+#pragma unroll
+        for (int i = kAhead; i < kV; ++i) {
+            __builtin_amdgcn_sched_group_barrier(kMfmas, 1, 0);
+            __builtin_amdgcn_sched_group_barrier(kDsReads, 2, 0);
+        }
+#pragma unroll
+        for (int i = 0; i < kK; ++i) {
+            __builtin_amdgcn_sched_group_barrier(kMfmas, 1, 0);
+            __builtin_amdgcn_sched_group_barrier(kDsReads, 1, 0);
+        }
+        __builtin_amdgcn_sched_group_barrier(kMfmas, kAhead, 0);
+        __builtin_amdgcn_sched_barrier(0);
+        __builtin_amdgcn_s_setprio(0);
     }
 
     static __device__ __forceinline__ s16x4 transposed(const char *at) {
@@ -284,16 +349,24 @@ template <class T, int D> struct Rows {
     }
 };
 
-// Writes one row's result, or a piece of it: `get(i)` = its element i.
+// Ends a phase of a wide item for all its wavefronts.  Products and
+// exponentials do not move from one phase into another.
+__device__ __forceinline__ void end_phase() {
+    __builtin_amdgcn_sched_barrier(0);
+    __syncthreads();
+    __builtin_amdgcn_sched_barrier(0);
+}
+
+// Where a row's result goes.
 template <class T>
-__device__ __forceinline__ char *out_row(const taps_attend_launch &p, const taps_plan_seq &s,
+__device__ __forceinline__ char *out_row(const taps_attend_launch &p, const taps_plan_item &s,
                                          uint32_t head, int row) {
     const int token = row / (int)p.group, sub = row - token * (int)p.group;
     return p.out + (int64_t)(s.token0 + token) * p.o_token +
            (int64_t)(head * p.group + sub) * p.o_head;
 }
 
-__device__ __forceinline__ void store_lse(const taps_attend_launch &p, const taps_plan_seq &s,
+__device__ __forceinline__ void store_lse(const taps_attend_launch &p, const taps_plan_item &s,
                                           uint32_t head, int row, float m, float l) {
     if (!p.lse) return;
     const int token = row / (int)p.group, sub = row - token * (int)p.group;
@@ -301,115 +374,257 @@ __device__ __forceinline__ void store_lse(const taps_attend_launch &p, const tap
         l == 0.f ? kMinusInf : m * p.scale + __builtin_amdgcn_logf(l) * kLn2;
 }
 
+// Writes the result of a wavefront's 32 rows; `row` is this lane's.
 template <class T, int D>
-__global__ __launch_bounds__(kThreads, 2) void k_attend(taps_attend_launch p) {
-    __shared__ __attribute__((aligned(16))) char lds[shared_bytes<D>()];
-    const uint32_t item_at = blockIdx.x / p.kv_heads, head = blockIdx.x % p.kv_heads;
-    const taps_plan_item item = p.items[item_at];
-    const taps_plan_seq seq = p.seqs[item.seq];
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int32_t *pages = p.pages + seq.page0;
-    const char *k_head = p.k_cache + (int64_t)head * p.k_head;
-    const char *v_head = p.v_cache + (int64_t)head * p.v_head;
-    const int lo = item.lo, hi = item.hi, start = lo & ~15;   // whole groups of 16 share a page
-    const float c = p.scale * kLog2e;
-    Rows<T, D> rows;
+__device__ __forceinline__ void finish(const taps_attend_launch &p, const taps_plan_item &item,
+                                       uint32_t head, const Rows<T, D> &rows, int row, int lane) {
     constexpr int kBlocks = D / 32;
     const int half = lane >> 5;
-
-    if (!item.narrow) {
-        const int row = item.row0 + 32 * wave + (lane & 31);
-        rows.start(p, seq, head, row, lo, hi, lane);
-        // keys that every row of the wavefront sees: all_from .. all_to.  (Tiles that no row of one
-        // wavefront sees are taken all the same, masked: leaving them out costs the other tiles
-        // 64 register moves each.)
-        int all_from = lo, all_to = hi - 1;
-        if (p.causal) {
-            const int row_a = min(item.row0 + 32 * wave, seq.rows - 1);
-            const int row_b = min(item.row0 + 32 * wave + 31, seq.rows - 1);
-            all_to = min(all_to, seq.first_pos + row_a / (int)p.group);
-            if (p.window)
-                all_from = max(all_from, seq.first_pos + row_b / (int)p.group - (int)p.window + 1);
-        }
-        // Each wavefront loads 16 of a tile's 64 keys.  Keys outside lo .. hi - 1 and columns
-        // beyond the head come from a block of zeros in the plan: what memory holds in their
-        // place (it may never have been written) must not reach a product.
-        const Group<D> g(lane);
-        const uint32_t mine = __builtin_amdgcn_readfirstlane(lds_at(lds) + 16 * wave * Tile<D>::kRow);
-        const bool ragged = p.dim < D;
-        const auto load = [&](int t0, int page, int buffer) {
-            const int key = t0 + 16 * wave;
-            const Place at(p, k_head, v_head, page, key);
-            const uint32_t to = mine + buffer * Tile<D>::bytes(kWideKeys);
-            const bool whole = !ragged && key >= lo && key + 16 <= hi;
+    const float l = half_sum(rows.l);
+    if (row >= item.rows) return;
+    if (item.part < 0) {
+        const float inv = l == 0.f ? 0.f : 1.f / l;
+        char *out = out_row<T>(p, item, head, row);
 #pragma unroll
-            for (int i = 0; i < Group<D>::kN; ++i) {
-                const char *k = at.k + g.key[i] * p.k_slot + 16 * g.k_col[i];
-                const char *v = at.v + g.key[i] * p.v_slot + 16 * g.v_col[i];
-                if (!whole) {
-                    const bool in = key + g.key[i] >= lo && key + g.key[i] < hi;
-                    k = in && 8 * g.k_col[i] < (int)p.dim ? k : p.zeros;
-                    v = in && 8 * g.v_col[i] < (int)p.dim ? v : p.zeros;
-                }
-                load_to_lds(k, to + 1024 * i);
-                load_to_lds(v, to + 1024 * i + kWideKeys * Tile<D>::kRow);
+        for (int b = 0; b < kBlocks; ++b)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int d = 32 * b + 8 * i + 4 * half;
+                const u32x2 v = {pack2<T>(rows.o[b][4 * i] * inv, rows.o[b][4 * i + 1] * inv),
+                                 pack2<T>(rows.o[b][4 * i + 2] * inv, rows.o[b][4 * i + 3] * inv)};
+                if (d < (int)p.dim) *(u32x2 *)(out + 2 * d) = v;
             }
-        };
-        int page = 0, buffer = 0;
-        if (lo < hi) {
-            load(start, page_at(p, pages, start + 16 * wave, lo, hi), 0);
-            page = page_at(p, pages, start + kWideKeys + 16 * wave, lo, hi);
-        }
-        for (int t0 = start; lo < hi && t0 < hi; t0 += kWideKeys, buffer ^= 1) {
-            // one barrier a tile: the tile's loads have ended in every wavefront, and every
-            // wavefront is done with the other buffer
-            wait_loads();
-            __syncthreads();
-            if (t0 + kWideKeys < hi) {
-                load(t0 + kWideKeys, page, buffer ^ 1);
-                page = page_at(p, pages, t0 + 2 * kWideKeys + 16 * wave, lo, hi);
+        if (half == 0) store_lse(p, item, head, row, rows.m, l);
+    } else {
+        const int64_t at = (int64_t)(item.part + row - item.row0) * p.kv_heads + head;
+#pragma unroll
+        for (int b = 0; b < kBlocks; ++b)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int d = 32 * b + 8 * i + 4 * half;
+                const f32x4 v = {rows.o[b][4 * i], rows.o[b][4 * i + 1], rows.o[b][4 * i + 2],
+                                 rows.o[b][4 * i + 3]};
+                if (d < (int)p.dim) *(f32x4 *)(p.part_o + at * p.dim + d) = v;
             }
-            const bool masked = t0 < all_from || t0 + kWideKeys - 1 > all_to;
-            rows.template take<kWideKeys>(lds + buffer * Tile<D>::bytes(kWideKeys), t0, masked, c,
-                                          lane);
-        }
-        const float l = half_sum(rows.l);
-        if (row >= seq.rows) return;
-        if (item.part < 0) {
-            const float inv = l == 0.f ? 0.f : 1.f / l;
-            char *out = out_row<T>(p, seq, head, row);
-#pragma unroll
-            for (int b = 0; b < kBlocks; ++b)
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const int d = 32 * b + 8 * i + 4 * half;
-                    const u32x2 v = {
-                        pack2<T>(rows.o[b][4 * i] * inv, rows.o[b][4 * i + 1] * inv),
-                        pack2<T>(rows.o[b][4 * i + 2] * inv, rows.o[b][4 * i + 3] * inv)};
-                    if (d < (int)p.dim) *(u32x2 *)(out + 2 * d) = v;
-                }
-            if (half == 0) store_lse(p, seq, head, row, rows.m, l);
-        } else {
-            const int64_t at = (int64_t)(item.part + row - item.row0) * p.kv_heads + head;
-#pragma unroll
-            for (int b = 0; b < kBlocks; ++b)
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const int d = 32 * b + 8 * i + 4 * half;
-                    const f32x4 v = {rows.o[b][4 * i], rows.o[b][4 * i + 1], rows.o[b][4 * i + 2],
-                                     rows.o[b][4 * i + 3]};
-                    if (d < (int)p.dim) *(f32x4 *)(p.part_o + at * p.dim + d) = v;
-                }
-            if (half == 0) p.part_ml[2 * at] = rows.m, p.part_ml[2 * at + 1] = l;
-        }
-        return;
+        if (half == 0) p.part_ml[2 * at] = rows.m, p.part_ml[2 * at + 1] = l;
     }
+}
 
-    // narrow: every wavefront has the same rows and its own keys
-    const int row = item.row0 + (lane & 31);
-    rows.start(p, seq, head, row, lo, hi, lane);
+// The keys that all 32 rows from `row0` on see, of the item's: a tile outside
+// needs a mask.  (Tiles that no row of one wavefront sees are taken all the same,
+// masked: leaving them out costs the other tiles 64 register moves each.)
+struct Seen {
+    int from, to;
+    __device__ __forceinline__ Seen(const taps_attend_launch &p, const taps_plan_item &item,
+                                    int row0) {
+        from = item.lo, to = item.hi - 1;
+        if (!p.causal) return;
+        const int a = min(row0, item.rows - 1), b = min(row0 + 31, item.rows - 1);
+        to = min(to, item.first_pos + a / (int)p.group);
+        if (p.window) from = max(from, item.first_pos + b / (int)p.group - (int)p.window + 1);
+    }
+    __device__ __forceinline__ bool masks(int t0, int keys) const {
+        return t0 < from || t0 + keys - 1 > to;
+    }
+};
+
+// Loads to LDS: a wavefront takes 16 of a tile's 64 keys, of K or of V.  Keys
+// outside lo .. hi - 1 and columns beyond the head come from a block of zeros in
+// the plan: what memory holds in their place (it may never have been written)
+// must not reach a product.
+template <int D> struct Loader {
+    static constexpr int kN = Group<D>::kN;   // loads of a tile's K or V
+    const char *head, *zeros;
+    int64_t page_stride, slot_stride;
+    int key0, lo, hi, dim, page_log2;
+    uint32_t offset[kN];   // of this lane's chunks in a group
+    int key_col[kN];       // 16 x chunk number + key
+    __device__ __forceinline__ Loader(const taps_attend_launch &p, const taps_plan_item &item,
+                                      uint32_t h, bool v, int wave, int lane) {
+        head = v ? p.v_cache + (int64_t)h * p.v_head : p.k_cache + (int64_t)h * p.k_head;
+        page_stride = v ? p.v_page : p.k_page, slot_stride = v ? p.v_slot : p.k_slot;
+        zeros = p.zeros;
+        key0 = 16 * (wave & 3), lo = item.lo, hi = item.hi, dim = p.dim, page_log2 = p.page_log2;
+        const Group<D> g(lane);
+#pragma unroll
+        for (int i = 0; i < kN; ++i) {
+            const int col = v ? g.v_col[i] : g.k_col[i];
+            offset[i] = g.key[i] * (uint32_t)slot_stride + 16 * col;
+            key_col[i] = 16 * col + g.key[i];
+        }
+    }
+    // The wavefront's keys of the tile from key t0 on, to `part` (K or V of a tile).
+    __device__ __forceinline__ void load(int t0, int page, const char *part) const {
+        const int key = t0 + key0;
+        const char *at = head + page * page_stride +
+                         (int64_t)(key & ((1 << page_log2) - 1)) * slot_stride;
+        const uint32_t to = __builtin_amdgcn_readfirstlane(lds_at(part) + key0 * Tile<D>::kRow);
+        if (dim == D && key >= lo && key + 16 <= hi) {
+#pragma unroll
+            for (int i = 0; i < kN; ++i) load_to_lds(at, offset[i], to + 1024 * i);
+        } else {
+#pragma unroll
+            for (int i = 0; i < kN; ++i) {
+                const int j = key + (key_col[i] & 15), col = key_col[i] >> 4;
+                load_to_lds(j >= lo && j < hi && 8 * col < dim ? at + offset[i] : zeros,
+                            to + 1024 * i);
+            }
+        }
+    }
+};
+
+// 256 query rows, 32 a wavefront; a unit has one workgroup at a time.  A tile takes
+// two phases: products (the numerators of the last tile by its values, the scores
+// of this one), and softmax.  While the first four wavefronts, one on each SIMD,
+// are in one of them, the others are in the other, so that the matrix cores
+// have a wavefront of their own at any time and a tile's loads serve twice the
+// rows of a block item: 512 tokens over 32768 keys of 8 heads of 128, four query
+// heads each, 366 -> 327 us (890 TFLOP/s in the kernel; with the loads, the
+// exponentials and the reads of LDS taken out in turns it gains 17, 12 and 12 %, with all of them
+// it runs at the rate of a large matrix product).
+template <class T, int D>
+__global__ __launch_bounds__(kWideThreads, 2) void k_attend_wide(taps_attend_launch p) {
+    constexpr int kPart = kWideKeys * Tile<D>::kRow;   // a tile's K, or its V
+    __shared__ __attribute__((aligned(16))) char lds[6 * kPart];
+    const uint32_t head = blockIdx.x % p.kv_heads;
+    const taps_plan_item item = p.items[blockIdx.x / p.kv_heads];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const bool second = wave >= 4;   // the workgroup's second half
+    const int32_t *pages = p.pages + item.page0;
+    const int start = item.lo & ~15;   // whole groups of 16 share a page
+    const float c = p.scale * kLog2e;
+    const int row0 = item.row0 + 32 * wave, row = row0 + (lane & 31);
+    Rows<T, D> rows;
+    rows.start(p, item, head, row, lane);
+    const Seen seen(p, item, row0);
+    if (item.lo < item.hi) {
+        // Both halves use all tiles; the first loads K, the other V.  K of tile i is read in phases
+        // 2 i and 2 i + 1, V in the two after them.  Three tiles of each are kept: K of tile i + 2
+        // is loaded in phase 2 i + 1, V of tile i + 1 in phase 2 i.
+        typename Rows<T, D>::template Scores<kWideKeys> x;
+        typename Rows<T, D>::template Numerators<kWideKeys> y;
+        const Loader<D> loader(p, item, head, second, wave, lane);
+        const char *k_lds = lds, *v_lds = lds + 3 * kPart;
+        const int tiles = (item.hi - start + kWideKeys - 1) / kWideKeys;
+        const auto tile0 = [&](int i) { return start + i * kWideKeys; };
+        const auto page_of = [&](int t0) {
+            return page_at(p, pages, t0 + loader.key0, item.lo, item.hi);
+        };
+        const auto soften = [&](int t0) {
+            rows.soften(x, y, t0, seen.masks(t0, kWideKeys), c, lane);
+        };
+        // buffers: of tiles i - 1, i, i + 1 in the first half's loop, i - 2, i - 1, i in the other's;
+        // the oldest is loaded anew
+        int b0 = 2, b1 = 0, b2 = 1;
+        const auto turn = [&]() {
+            const int b = b0;
+            b0 = b1, b1 = b2, b2 = b;
+        };
+        const auto wait = [&](bool newer) {
+            if (newer)
+                wait_loads<Loader<D>::kN>();
+            else
+                wait_loads<0>();
+        };
+        const char *mine = second ? v_lds : k_lds;
+        loader.load(tile0(0), page_of(tile0(0)), mine);
+        if (tiles > 1) loader.load(tile0(1), page_of(tile0(1)), mine + kPart);
+        int page = page_of(tile0(2));
+        wait_loads<0>();
+        end_phase();
+        if (!second) {
+            for (int i = 0; i < tiles; ++i, turn()) {
+                if (i)
+                    rows.products(v_lds + b0 * kPart, y, k_lds + b1 * kPart, x, lane);
+                else
+                    rows.score(k_lds, x, lane);
+                end_phase();
+                if (i + 2 < tiles) loader.load(tile0(i + 2), page, k_lds + b0 * kPart);
+                page = page_of(tile0(i + 3));
+                soften(tile0(i));
+                wait(i + 2 < tiles);
+                end_phase();
+            }
+        } else {
+            end_phase();
+            rows.score(k_lds, x, lane);
+            end_phase();
+            for (int i = 1; i < tiles; ++i, turn()) {
+                if (i + 1 < tiles) loader.load(tile0(i + 1), page, v_lds + b0 * kPart);
+                page = page_of(tile0(i + 2));
+                soften(tile0(i - 1));
+                end_phase();
+                rows.products(v_lds + b1 * kPart, y, k_lds + b2 * kPart, x, lane);
+                wait(i + 1 < tiles);
+                end_phase();
+            }
+            soften(tile0(tiles - 1));
+            b0 = b1;
+        }
+        rows.spend(v_lds + b0 * kPart, y, lane);   // the last tile's
+    }
+    finish(p, item, head, rows, row, lane);
+}
+
+// 128 query rows, 32 a wavefront, two workgroups to a unit.  Tiles of 64 keys in
+// two buffers, one loaded while the other is in use.
+template <class T, int D>
+__device__ __forceinline__ void attend_block(const taps_attend_launch &p, const taps_plan_item &item,
+                                             uint32_t head, char *lds) {
+    constexpr int kPart = kWideKeys * Tile<D>::kRow;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int32_t *pages = p.pages + item.page0;
+    const int start = item.lo & ~15;
+    const float c = p.scale * kLog2e;
+    const int row0 = item.row0 + 32 * wave, row = row0 + (lane & 31);
+    Rows<T, D> rows;
+    rows.start(p, item, head, row, lane);
+    const Seen seen(p, item, row0);
+    const Loader<D> k(p, item, head, false, wave, lane), v(p, item, head, true, wave, lane);
+    const auto page_of = [&](int t0) { return page_at(p, pages, t0 + k.key0, item.lo, item.hi); };
+    int page = 0, buffer = 0;
+    if (item.lo < item.hi) {
+        page = page_of(start);
+        k.load(start, page, lds);
+        v.load(start, page, lds + kPart);
+        page = page_of(start + kWideKeys);
+    }
+    for (int t0 = start; item.lo < item.hi && t0 < item.hi; t0 += kWideKeys, buffer ^= 1) {
+        const char *tile = lds + 2 * buffer * kPart, *next = lds + 2 * (buffer ^ 1) * kPart;
+        // one barrier a tile: the tile's loads have ended in every wavefront, and every
+        // wavefront is done with the other buffer
+        wait_loads<0>();
+        __syncthreads();
+        if (t0 + kWideKeys < item.hi) {
+            k.load(t0 + kWideKeys, page, next);
+            v.load(t0 + kWideKeys, page, next + kPart);
+            page = page_of(t0 + 2 * kWideKeys);
+        }
+        typename Rows<T, D>::template Scores<kWideKeys> x;
+        typename Rows<T, D>::template Numerators<kWideKeys> y;
+        rows.score(tile, x, lane);
+        rows.soften(x, y, t0, seen.masks(t0, kWideKeys), c, lane);
+        rows.spend(tile + kPart, y, lane);
+    }
+    finish(p, item, head, rows, row, lane);
+}
+
+// Up to 32 query rows: every wavefront has all of them and its own keys.
+template <class T, int D>
+__device__ __forceinline__ void attend_narrow(const taps_attend_launch &p,
+                                              const taps_plan_item &item, uint32_t head, char *lds) {
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int32_t *pages = p.pages + item.page0;
+    const char *k_head = p.k_cache + (int64_t)head * p.k_head;
+    const char *v_head = p.v_cache + (int64_t)head * p.v_head;
+    const int lo = item.lo, hi = item.hi, start = lo & ~15;
+    const float c = p.scale * kLog2e;
+    constexpr int kBlocks = D / 32;
+    const int half = lane >> 5;
+    Rows<T, D> rows;
+    rows.start(p, item, head, item.row0 + (lane & 31), lane);
     {
-        const int last_row = min(item.row0 + kNarrowRows, seq.rows) - 1;
+        const int last_row = min(item.row0 + kNarrowRows, item.rows) - 1;
         // one token's rows all see the item's keys; several tokens' need masks
         const bool one = item.row0 / (int)p.group == last_row / (int)p.group || !p.causal;
         char *tile = lds + wave * Tile<D>::bytes(kNarrowKeys);
@@ -469,13 +684,17 @@ __global__ __launch_bounds__(kThreads, 2) void k_attend(taps_attend_launch p) {
                 page1 = page_at(p, pages, t0 + 2 * kStep + 16, lo, hi);
             }
             const bool masked = !one || t0 < lo || t0 + kNarrowKeys > hi;
-            rows.template take<kNarrowKeys>(tile, t0, masked, c, lane);
+            typename Rows<T, D>::template Scores<kNarrowKeys> x;
+            typename Rows<T, D>::template Numerators<kNarrowKeys> y;
+            rows.score(tile, x, lane);
+            rows.soften(x, y, t0, masked, c, lane);
+            rows.spend(tile + kNarrowKeys * Tile<D>::kRow, y, lane);
             __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
             __builtin_amdgcn_wave_barrier();
             __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
         }
     }
-    float *ml = (float *)(lds + shared_bytes<D>() - kWaves * kNarrowRows * 2 * 4);
+    float *ml = (float *)(lds + narrow_bytes<D>() - kWaves * kNarrowRows * 2 * 4);
     const float l_wave = half_sum(rows.l);
     __syncthreads();   // the tiles are done with
     if (half == 0) {
@@ -500,7 +719,7 @@ __global__ __launch_bounds__(kThreads, 2) void k_attend(taps_attend_launch p) {
             }
     }
     __syncthreads();
-    const int n_rows = min(kNarrowRows, seq.rows - item.row0);
+    const int n_rows = min(kNarrowRows, item.rows - item.row0);
     for (int k = threadIdx.x; k < n_rows * (D / 4); k += kThreads) {
         const int r = k / (D / 4), d = 4 * (k % (D / 4));
         if (d >= (int)p.dim) continue;
@@ -518,16 +737,29 @@ __global__ __launch_bounds__(kThreads, 2) void k_attend(taps_attend_launch p) {
         }
         if (item.part < 0) {
             const float inv = l == 0.f ? 0.f : 1.f / l;
-            char *out = out_row<T>(p, seq, head, item.row0 + r);
+            char *out = out_row<T>(p, item, head, item.row0 + r);
             const u32x2 v = {pack2<T>(o[0] * inv, o[1] * inv), pack2<T>(o[2] * inv, o[3] * inv)};
             *(u32x2 *)(out + 2 * d) = v;
-            if (d == 0) store_lse(p, seq, head, item.row0 + r, top, l);
+            if (d == 0) store_lse(p, item, head, item.row0 + r, top, l);
         } else {
             const int64_t at = (int64_t)(item.part + r) * p.kv_heads + head;
             *(f32x4 *)(p.part_o + at * p.dim + d) = o;
             if (d == 0) p.part_ml[2 * at] = top, p.part_ml[2 * at + 1] = l;
         }
     }
+}
+
+// A block or a narrow item; both fit a unit twice.
+template <class T, int D>
+__global__ __launch_bounds__(kThreads, 2) void k_attend(taps_attend_launch p) {
+    __shared__ __attribute__((aligned(16))) char lds[max_of(narrow_bytes<D>(),
+                                                            2 * Tile<D>::bytes(kWideKeys))];
+    const uint32_t head = blockIdx.x % p.kv_heads;
+    const taps_plan_item item = p.items[p.n_wide + blockIdx.x / p.kv_heads];
+    if (item.kind == kBlock)
+        attend_block<T, D>(p, item, head, lds);
+    else
+        attend_narrow<T, D>(p, item, head, lds);
 }
 
 // Adds up the pieces of rows whose keys were split.  A group of 32 lanes, four
@@ -542,7 +774,8 @@ __global__ __launch_bounds__(kThreads) void k_join(taps_attend_launch p) {
     __shared__ f32x4 sums[kJoinGroups][32];
     __shared__ float ms[kJoinGroups], ls[kJoinGroups];
     const taps_plan_join join = p.joins[blockIdx.x];
-    const taps_plan_seq seq = p.seqs[join.seq];
+    taps_plan_item item{};
+    item.token0 = join.token0;
     const uint32_t head = blockIdx.y;
     const float c = p.scale * kLog2e;
     const int group = threadIdx.x >> 5, d = 4 * (threadIdx.x & 31);
@@ -594,21 +827,26 @@ __global__ __launch_bounds__(kThreads) void k_join(taps_attend_launch p) {
     }
     const float inv = l == 0.f ? 0.f : 1.f / l;
     if (live) {
-        char *out = out_row<T>(p, seq, head, join.row0 + r);
+        char *out = out_row<T>(p, item, head, join.row0 + r);
         const u32x2 v = {pack2<T>(o[0] * inv, o[1] * inv), pack2<T>(o[2] * inv, o[3] * inv)};
         *(u32x2 *)(out + 2 * d) = v;
     }
-    if (d == 0) store_lse(p, seq, head, join.row0 + r, m, l);
+    if (d == 0) store_lse(p, item, head, join.row0 + r, m, l);
+}
+
+template <class T, int D> void launch_items(const taps_attend_launch &p, hipStream_t stream) {
+    if (p.n_wide) k_attend_wide<T, D><<<p.n_wide * p.kv_heads, kWideThreads, 0, stream>>>(p);
+    if (p.n_items > p.n_wide)
+        k_attend<T, D><<<(p.n_items - p.n_wide) * p.kv_heads, kThreads, 0, stream>>>(p);
 }
 
 template <class T> hipError_t launch(const taps_attend_launch &p, hipStream_t stream) {
-    const uint32_t groups = p.n_items * p.kv_heads;
     if (p.dim <= 64)
-        k_attend<T, 64><<<groups, kThreads, 0, stream>>>(p);
+        launch_items<T, 64>(p, stream);
     else if (p.dim <= 96)
-        k_attend<T, 96><<<groups, kThreads, 0, stream>>>(p);
+        launch_items<T, 96>(p, stream);
     else
-        k_attend<T, 128><<<groups, kThreads, 0, stream>>>(p);
+        launch_items<T, 128>(p, stream);
     if (p.n_joins) k_join<T><<<dim3(p.n_joins, p.kv_heads, p.join_rounds), kThreads, 0, stream>>>(p);
     return hipGetLastError();
 }

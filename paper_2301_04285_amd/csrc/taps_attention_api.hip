@@ -128,11 +128,11 @@ struct Layout {
 
 // Query rows that share their keys' loads, before they are split over the keys.
 struct Strip {
-    int32_t seq, row0, rows, lo, hi;
-    bool narrow;
+    int32_t seq, row0, rows, lo, hi, kind;
     // what a key costs: a narrow item waits for its bytes, which come to a
-    // compute unit at about half the rate at which a wide one works keys off
-    int64_t cost() const { return (int64_t)(hi - lo) * (narrow ? 2 : 1); }
+    // compute unit at about half the rate at which the others work keys off
+    int64_t cost() const { return cost_of(kind, hi - lo); }
+    static int64_t cost_of(int32_t kind, int64_t keys) { return keys * (kind == kNarrow ? 2 : 1); }
 };
 
 // Pieces shorter than this are not made: a split costs a launch and a pass
@@ -144,6 +144,9 @@ constexpr int64_t kLeastPiece = 1024;
 // and with twice as many the last ones end sooner (512 tokens over 32768 keys:
 // 425 us at two a unit, 370 at four; two tokens over 131001: 187 and 192).
 constexpr int64_t kNarrowPieces = 2, kWidePieces = 4;
+
+// Rounds of wide items over the compute units, pieces counted, from which they are worth it.
+constexpr int64_t kWideRounds = 4;
 
 taps_status lay_out(const taps_paged_batch *b, uint32_t cus, Layout *out) {
     taps_plan_header &h = out->head;
@@ -191,15 +194,30 @@ taps_status lay_out(const taps_paged_batch *b, uint32_t cus, Layout *out) {
         pages += (uint64_t)n_pages;
         if (tokens >= (1ull << 31) || pages >= (1ull << 31))
             return fail(TAPS_ERR_ARG, "2^31 or more tokens or pages in all");
-        const bool narrow = q.rows <= kNarrowRows;
-        const int32_t step = narrow ? kNarrowRows : kWideRows;
-        // rows that see the most keys first: the last to start are the shortest
-        for (int32_t r = q.rows ? (q.rows - 1) / step * step : -1; r >= 0; r -= step) {
-            Strip t{(int32_t)s, r, std::min(step, q.rows - r), (int32_t)from, (int32_t)kv, narrow};
+    }
+    std::sort(written.begin(), written.end());
+    if (std::adjacent_find(written.begin(), written.end()) != written.end())
+        return fail(TAPS_ERR_ARG, "page %d is to be written from two places of the page table",
+                    *std::adjacent_find(written.begin(), written.end()));
+
+    // Strips of 256 rows read the fewest keys, where there are enough of them to
+    // keep every compute unit busy for a few rounds; else strips of 128.
+    int64_t wide = 0;
+    for (const taps_plan_seq &q : out->seqs)
+        wide += q.rows / kWideRows * std::max<int64_t>(1, q.kv_len / kLeastPiece);
+    const bool few = wide * b->kv_heads < kWideRounds * (int64_t)cus;
+    for (uint32_t s = 0; s < b->n_seqs; ++s) {
+        const taps_plan_seq &q = out->seqs[s];
+        const int32_t kind = q.rows <= kNarrowRows           ? kNarrow
+                             : few || q.rows <= kBlockRows ? kBlock
+                                                             : kWide;
+        const int32_t step = kind == kNarrow ? kNarrowRows : kind == kBlock ? kBlockRows : kWideRows;
+        for (int32_t r = 0; r < q.rows; r += step) {
+            Strip t{(int32_t)s, r, std::min(step, q.rows - r), q.kv_start, q.kv_len, kind};
             if (b->causal) {
                 const int64_t pos_a = q.first_pos + r / (int64_t)group;
                 const int64_t pos_b = q.first_pos + (r + t.rows - 1) / (int64_t)group;
-                t.hi = (int32_t)std::max<int64_t>(std::min<int64_t>(kv, pos_b + 1), 0);
+                t.hi = (int32_t)std::max<int64_t>(std::min<int64_t>(q.kv_len, pos_b + 1), 0);
                 if (h.window)
                     t.lo = (int32_t)std::max<int64_t>(t.lo, pos_a - (int64_t)h.window + 1);
             }
@@ -207,10 +225,6 @@ taps_status lay_out(const taps_paged_batch *b, uint32_t cus, Layout *out) {
             strips.push_back(t);
         }
     }
-    std::sort(written.begin(), written.end());
-    if (std::adjacent_find(written.begin(), written.end()) != written.end())
-        return fail(TAPS_ERR_ARG, "page %d is to be written from two places of the page table",
-                    *std::adjacent_find(written.begin(), written.end()));
 
     int64_t total = 0;
     for (const Strip &t : strips) total += t.cost();
@@ -218,7 +232,7 @@ taps_status lay_out(const taps_paged_batch *b, uint32_t cus, Layout *out) {
     uint64_t part_rows = 0;
     for (const Strip &t : strips) {
         const int64_t keys = t.hi - t.lo;
-        const int64_t target = total / (cus * (t.narrow ? kNarrowPieces : kWidePieces)) + 1;
+        const int64_t target = total / (cus * (t.kind == kNarrow ? kNarrowPieces : kWidePieces)) + 1;
         int64_t parts = std::min((t.cost() + target - 1) / target, keys / kLeastPiece);
         parts = std::max<int64_t>(1, std::min<int64_t>(parts, 256));
         // whole tiles, counted from where the strip's first tile starts
@@ -227,11 +241,14 @@ taps_status lay_out(const taps_paged_batch *b, uint32_t cus, Layout *out) {
         if (parts > 1) {
             const uint32_t rows = 8 / taps_join_across((int)parts);
             h.join_rounds = std::max(h.join_rounds, (t.rows + rows - 1) / rows);
-            out->joins.push_back({t.seq, t.row0, t.rows, (int32_t)part_rows, (int32_t)parts, {}});
+            out->joins.push_back({t.seq, t.row0, t.rows, (int32_t)part_rows, (int32_t)parts,
+                                  out->seqs[t.seq].token0, {}});
         }
         for (int64_t k = 0; k < parts; ++k) {
             taps_plan_item i{};
-            i.seq = t.seq, i.row0 = t.row0, i.narrow = t.narrow;
+            i.seq = t.seq, i.row0 = t.row0, i.kind = t.kind;
+            const taps_plan_seq &q = out->seqs[t.seq];
+            i.token0 = q.token0, i.rows = q.rows, i.first_pos = q.first_pos, i.page0 = q.page0;
             i.lo = (int32_t)std::max<int64_t>(t.lo, start + 128 * (tiles * k / parts));
             i.hi = (int32_t)std::min<int64_t>(t.hi, start + 128 * (tiles * (k + 1) / parts));
             i.part = parts > 1 ? (int32_t)(part_rows + k * t.rows) : -1;
@@ -240,12 +257,15 @@ taps_status lay_out(const taps_paged_batch *b, uint32_t cus, Layout *out) {
         if (parts > 1) part_rows += (uint64_t)parts * t.rows;
         if (part_rows >= (1ull << 31)) return fail(TAPS_ERR_ARG, "too many rows are split");
     }
-    // dear items first, so that the last to start are cheap
+    // kind by kind, and dear items first, so that the last to start are cheap
+    const auto order = [](const taps_plan_item &i) {
+        return std::make_pair(i.kind, -(Strip::cost_of(i.kind, i.hi - i.lo) >> 8));
+    };
     std::stable_sort(out->items.begin(), out->items.end(),
-                     [](const taps_plan_item &x, const taps_plan_item &y) {
-                         return (x.hi - x.lo) * (x.narrow ? 2ll : 1ll) / 512 >
-                                (y.hi - y.lo) * (y.narrow ? 2ll : 1ll) / 512;
+                     [&](const taps_plan_item &x, const taps_plan_item &y) {
+                         return order(x) < order(y);
                      });
+    for (const taps_plan_item &i : out->items) h.n_wide += i.kind == kWide;
     if (out->items.size() * b->kv_heads >= (1ull << 31) || b->kv_heads > 65535)
         return fail(TAPS_ERR_ARG, "too many workgroups");
 
@@ -487,6 +507,9 @@ taps_status taps_attend(uint32_t dtype, const void *plan, const void *plan_devic
         if (!aligned(all[i]->data, 16) || (cache && all[i]->stride[0] % 8) || all[i]->stride[1] % 8 ||
             all[i]->stride[2] % 8)
             return fail(TAPS_ERR_ARG, "%s: rows do not start at multiples of 16 bytes", names[i]);
+        // 16 slots' offsets are held in 32 bits
+        if (cache && (all[i]->stride[2] < 0 || all[i]->stride[2] >= (1 << 26)))
+            return fail(TAPS_ERR_ARG, "%s: slots are 2^26 elements or more apart", names[i]);
     }
     if (!aligned(lse, 4)) return fail(TAPS_ERR_ARG, "lse is not aligned to its elements");
     const uint64_t need = workspace_of(*h);
@@ -503,7 +526,6 @@ taps_status taps_attend(uint32_t dtype, const void *plan, const void *plan_devic
     p.part_o = (float *)workspace;
     p.part_ml = (float *)((char *)workspace +
                           up16((uint64_t)h->part_rows * h->kv_heads * h->head_dim * 4));
-    p.seqs = (const taps_plan_seq *)(dev + h->seqs_at);
     p.pages = (const int32_t *)(dev + h->pages_at);
     p.items = (const taps_plan_item *)(dev + h->items_at);
     p.joins = (const taps_plan_join *)(dev + h->joins_at);
@@ -513,7 +535,7 @@ taps_status taps_attend(uint32_t dtype, const void *plan, const void *plan_devic
     p.k_slot = 2 * k_cache->stride[2];
     p.v_page = 2 * v_cache->stride[0], p.v_head = 2 * v_cache->stride[1];
     p.v_slot = 2 * v_cache->stride[2];
-    p.n_items = h->n_items, p.n_joins = h->n_joins, p.join_rounds = h->join_rounds;
+    p.n_items = h->n_items, p.n_wide = h->n_wide, p.n_joins = h->n_joins, p.join_rounds = h->join_rounds;
     p.q_heads = h->q_heads, p.kv_heads = h->kv_heads, p.group = h->q_heads / h->kv_heads;
     p.dim = h->head_dim;
     p.page_log2 = h->page_log2, p.causal = h->causal, p.window = h->window;

@@ -14,10 +14,9 @@
 
 constexpr uint32_t kPlanMagic = 0x54415031;
 
-// Query rows of a workgroup that shares key tiles between its wavefronts, and
-// of one whose wavefronts share the rows (taps_attend.hip).  A row is a pair of
-// a token and one of the query heads of a key head.
-constexpr int kWideRows = 128, kNarrowRows = 32;
+// Query rows of the kinds of items (taps_attend.hip).  A row is a pair of a
+// token and one of the query heads of a key head.
+constexpr int kWideRows = 256, kBlockRows = 128, kNarrowRows = 32;
 // Keys of a tile of either.
 constexpr int kWideKeys = 64, kNarrowKeys = 32;
 
@@ -26,14 +25,15 @@ struct taps_plan_header {
     uint64_t bytes;
     uint32_t tokens, q_heads, kv_heads, head_dim;
     uint32_t page_log2, n_pages, causal, window;
-    uint32_t n_items, n_joins;
+    uint32_t n_items, n_joins;   // items: the first n_wide are wide
     uint32_t part_rows;       // rows of partial results over all split pieces
     uint32_t max_positions;   // largest position of a new token, plus one
     uint32_t appendable;      // every sequence has kv_lens >= q_lens
     uint32_t join_rounds;     // workgroups that the rows of a join are spread over, at most
+    uint32_t n_wide, reserved;
+    uint32_t zeros[4];        // what attention reads for keys that are not there
     // byte offsets of the arrays
     uint64_t seqs_at, tokens_at, pages_at, items_at, joins_at;
-    uint32_t zeros[4];   // what attention reads for keys that are not there
 };
 static_assert(offsetof(taps_plan_header, zeros) % 16 == 0, "read 16 bytes at a time");
 
@@ -52,18 +52,23 @@ struct taps_plan_token {
 };
 
 // One workgroup of attention per item and key head.
+enum { kWide, kBlock, kNarrow };
+
 struct taps_plan_item {
     int32_t seq, row0;    // rows row0 .. of the sequence
     int32_t lo, hi;       // keys lo .. hi - 1
-    int32_t narrow;       // kNarrowRows rows, wavefronts split the keys
+    int32_t kind;
     int32_t part;         // first row of partial results, or -1: the item is its rows' only one
+    // the sequence's, so that nothing waits for a second look-up
+    int32_t token0, rows, first_pos, page0;
     int32_t reserved[2];
 };
 
 // Rows whose keys were split: `parts` pieces of `rows` rows each.
 struct taps_plan_join {
     int32_t seq, row0, rows, part, parts;
-    int32_t reserved[3];
+    int32_t token0;
+    int32_t reserved[2];
 };
 
 // Groups of lanes that share a row's pieces in k_join: 1, 2, 4 or 8 of a workgroup's 8.
@@ -113,14 +118,13 @@ struct taps_attend_launch {
     char *out;
     float *lse;
     float *part_o, *part_ml;   // [part_rows][kv_heads][dim], [part_rows][kv_heads][2]
-    const taps_plan_seq *seqs;
     const int32_t *pages;
     const taps_plan_item *items;
     const taps_plan_join *joins;
     // strides in bytes
     int64_t q_token, q_head, o_token, o_head;
     int64_t k_page, k_head, k_slot, v_page, v_head, v_slot;
-    uint32_t n_items, n_joins, join_rounds, q_heads, kv_heads, group, dim;
+    uint32_t n_items, n_wide, n_joins, join_rounds, q_heads, kv_heads, group, dim;
     uint32_t page_log2, causal, window;
     float scale;
 };

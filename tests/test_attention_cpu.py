@@ -45,7 +45,8 @@ class Header(C.Structure):
     _fields_ = [("magic", C.c_uint32), ("n_seqs", C.c_uint32), ("bytes", C.c_uint64)] + \
         [(n, C.c_uint32) for n in ("tokens", "q_heads", "kv_heads", "head_dim", "page_log2",
                                    "n_pages", "causal", "window", "n_items", "n_joins",
-                                   "part_rows", "max_positions", "appendable", "reserved")] + \
+                                   "part_rows", "max_positions", "appendable", "join_rounds",
+                                   "n_wide", "reserved")] + [("zeros", C.c_uint32 * 4)] + \
         [(n, C.c_uint64) for n in ("seqs_at", "tokens_at", "pages_at", "items_at", "joins_at")]
 
 
@@ -56,7 +57,7 @@ def parts(p):
     def words(at, n, k):
         return raw[at:at + 4 * n * k].view(np.int32).reshape(n, k)
     return (h, words(h.seqs_at, h.n_seqs, 8), words(h.tokens_at, h.tokens, 2),
-            words(h.items_at, h.n_items, 8), words(h.joins_at, h.n_joins, 8))
+            words(h.items_at, h.n_items, 12), words(h.joins_at, h.n_joins, 8))
 
 
 @pytest.mark.parametrize("seed", range(60))
@@ -77,11 +78,14 @@ def test_plan_covers_every_visible_pair_once(seed):
              q_heads=group * kv_heads, units=r.choice((1, 16, 256, 100000)))
     h, seqs, tokens, items, joins = parts(p)
     assert h.bytes == p._host.numel() and h.tokens == sum(q_lens)
+    kinds = items[:, 4].tolist()   # 0: 256 rows, 1: 128, 2: 32
+    assert kinds == sorted(kinds) and h.n_wide == kinds.count(0)
+    assert list(h.zeros) == [0] * 4
     covered = {}
     used = np.zeros(h.part_rows, dtype=bool)
-    for seq, row0, lo, hi, narrow, part, *_ in items.tolist():
-        rows = min(32 if narrow else 128, q_lens[seq] * group - row0)
-        assert rows > 0 and row0 % (32 if narrow else 128) == 0
+    for seq, row0, lo, hi, kind, part, *_ in items.tolist():
+        rows = min((256, 128, 32)[kind], q_lens[seq] * group - row0)
+        assert rows > 0 and row0 % (256, 128, 32)[kind] == 0
         covered.setdefault((seq, row0, rows), []).append((lo, hi, part))
         if part >= 0:
             assert not used[part:part + rows].any() and part + rows <= h.part_rows

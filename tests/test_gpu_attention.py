@@ -362,6 +362,14 @@ ATTEND = [
     ([1, 200], [3000, 2600], 4, 1, 64, 16, {"units": 4096, "window": 2000}),
     ([140], [2000], 2, 2, 96, 16, {"units": 4096, "causal": False}),
     ([20, 3, 300], [5, 0, 900], 4, 2, 128, 16, {"units": 1}),
+    # enough rows for one unit to be worth the largest strips
+    ([300, 520], [300, 700], 4, 2, 128, 64, {"units": 1}),
+    ([600], [1100], 4, 2, 96, 16, {"units": 1, "window": 130}),
+    ([400, 1], [300, 50], 8, 2, 80, 32, {"units": 1}),
+    ([700], [90], 4, 2, 64, 16, {"units": 1, "causal": False}),
+    ([520, 600], [600, 600], 2, 2, 64, 16, {"units": 1, "kv_starts": [333, 600]}),
+    ([260, 257], [260, 321], 4, 4, 128, 16, {"units": 1}),
+    ([1030], [2100], 1, 1, 40, 128, {"units": 1, "window": 600}),
 ]
 
 
@@ -446,6 +454,31 @@ def test_attend_large_scores():
                 torch.from_numpy(k).to(dtype).cuda()
         out, lse = A.taps_attend(q, *caches, plan, lse=True)
         attend_check(spec, q, rising, out, lse, 0.125, dtype)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F16])
+def test_attend_many_small_numerators(dtype):
+    """One key above thousands whose numerators lie below the smallest normal 16-bit numbers, and
+    together weigh as much as it does; the key comes first, last or between."""
+    n, dim, page = 9000, 64, 64
+    g = gen_of(8)
+    for q_len, at in ((1, 0), (1, n - 1), (40, 4000), (40, 0)):
+        k = torch.zeros(n, 1, dim, dtype=dtype)
+        v = torch.randn(n, 1, dim, generator=g).to(dtype)
+        q = torch.zeros(q_len, 1, dim, dtype=dtype)
+        q[:, 0, 0] = 8.0
+        k[:, 0, 0] = -10.75 + 0.25 * torch.randint(0, 3, (n,), generator=g).to(dtype)
+        k[at, 0, 0] = 0
+        pages, n_pages = page_table(random.Random(2), [n], page)
+        caches = [cache_of("heads", n_pages, 1, page, dim, dtype) for _ in range(2)]
+        j = torch.arange(n)
+        for c, x in zip(caches, (k, v)):
+            c[torch.from_numpy(pages[0]).long()[j // page].cuda(), :, (j % page).cuda()] = x.cuda()
+        spec = ([q_len], [n], 1, 1, dim, page, {})
+        plan = A.PagedPlan([q_len], [n], pages, n_pages=n_pages, page_size=page, q_heads=1,
+                           kv_heads=1, head_dim=dim)
+        out, lse = A.taps_attend(q.cuda(), *caches, plan, lse=True)   # scale 1/8: scores as in k
+        attend_check(spec, q, [(R.f64(k), R.f64(v))], out, lse, 0.125, dtype)
 
 
 def test_attend_far_offsets():
