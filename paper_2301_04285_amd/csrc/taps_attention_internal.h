@@ -98,7 +98,6 @@ struct taps_rows_launch {
     uint32_t page_log2;
     float eps;
     uint8_t wide_positions, interleaved, float_weights, norm[2];
-    uint8_t past_caches;   // set by the launch
 };
 
 hipError_t taps_launch_norm_rotate(const taps_rows_launch &p, uint32_t dtype, bool vectors,

@@ -39,13 +39,12 @@ template <> struct Pairs<true> {
         return dim <= 8 ? 1 : dim <= 16 ? 2 : dim <= 32 ? 4 : dim <= 64 ? 8 : dim <= 128 ? 16 : 32;
     }
     int a0, b0, angle0;
-    bool live, rotated, interleaved, past_caches;
+    bool live, rotated, interleaved;
     __device__ Pairs(const taps_rows_launch &p, int lane) {
         const int rot8 = p.rotary / 8;
         live = lane < (int)p.dim / 8;
         rotated = lane < rot8;
         interleaved = p.interleaved && rotated;
-        past_caches = p.past_caches;
         angle0 = 4 * lane;
         if (interleaved || !rotated) {   // neighbouring chunks
             a0 = 8 * lane;
@@ -93,13 +92,11 @@ template <> struct Pairs<true> {
         } else {
             for (int i = 0; i < 4; ++i) u[i] = from_f32<T>(a[i]), v[i] = from_f32<T>(b[i]);
         }
-        if (past_caches) {
-            __builtin_nontemporal_store(u, (v4 *)(row + a0));
-            __builtin_nontemporal_store(v, (v4 *)(row + b0));
-        } else {
-            *(v4 *)(row + a0) = u;
-            *(v4 *)(row + b0) = v;
-        }
+        // past the caches: 268 MB in and out 50.1 -> 47.3 us forwards, 112 -> 110
+        // backwards, an append of 545 MB 104.3 -> 101.1 (not so by a branch on the
+        // size, which the compiler joins into ordinary stores)
+        __builtin_nontemporal_store(u, (v4 *)(row + a0));
+        __builtin_nontemporal_store(v, (v4 *)(row + b0));
     }
     __device__ __forceinline__ void angles(const taps_rows_launch &p, int64_t pos, float (&c)[kN],
                                            float (&s)[kN]) const {
@@ -512,20 +509,12 @@ int lanes_of(uint32_t dim, bool vectors) {
     return vectors ? Pairs<true>::lanes(dim) : Pairs<false>::lanes(dim);
 }
 
-// Outputs that no cache holds are written past them: 268 MB in and out 50.1 ->
-// 46.5 us forwards, 114 -> 109 backwards, an append of 545 MB 104 -> 101.
-bool past_caches(uint64_t rows, uint32_t dim, uint32_t dtype) {
-    return rows * dim * (dtype == TAPS_F32 ? 4 : 2) >= 64ull << 20;
-}
-
 }  // namespace
 
-hipError_t taps_launch_norm_rotate(const taps_rows_launch &given, uint32_t dtype, bool vectors,
+hipError_t taps_launch_norm_rotate(const taps_rows_launch &p, uint32_t dtype, bool vectors,
                                    hipStream_t stream) {
-    taps_rows_launch p = given;
-    const uint64_t tokens = (uint64_t)p.batch * p.tokens, heads = p.heads[0] + p.heads[1];
-    p.past_caches = past_caches(tokens * heads, p.dim, dtype);
-    const uint32_t groups = token_groups(tokens, heads, lanes_of(p.dim, vectors));
+    const uint32_t groups = token_groups((uint64_t)p.batch * p.tokens, p.heads[0] + p.heads[1],
+                                         lanes_of(p.dim, vectors));
     with_type(dtype, [&](auto zero) {
         using T = decltype(zero);
         if (!vectors)
@@ -538,10 +527,8 @@ hipError_t taps_launch_norm_rotate(const taps_rows_launch &given, uint32_t dtype
     return hipGetLastError();
 }
 
-hipError_t taps_launch_append(const taps_rows_launch &given, uint32_t dtype, bool vectors,
+hipError_t taps_launch_append(const taps_rows_launch &p, uint32_t dtype, bool vectors,
                               hipStream_t stream) {
-    taps_rows_launch p = given;
-    p.past_caches = past_caches(2ull * p.tokens * p.heads[0], p.dim, dtype);
     const uint32_t groups = token_groups(p.tokens, 2 * p.heads[0], lanes_of(p.dim, vectors));
     with_type(dtype, [&](auto zero) {
         using T = decltype(zero);
@@ -561,12 +548,9 @@ uint32_t taps_backward_groups(const taps_rows_launch &p, bool vectors) {
     return groups < 1 ? 1 : groups < kMostBackwardGroups ? groups : kMostBackwardGroups;
 }
 
-hipError_t taps_launch_norm_rotate_backward(const taps_rows_launch &given, uint32_t dtype, bool vectors,
+hipError_t taps_launch_norm_rotate_backward(const taps_rows_launch &p, uint32_t dtype, bool vectors,
                                             void *q_weight_grad, void *k_weight_grad,
                                             hipStream_t stream) {
-    taps_rows_launch p = given;
-    p.past_caches =
-        past_caches((uint64_t)p.batch * p.tokens * (p.heads[0] + p.heads[1]), p.dim, dtype);
     const uint32_t groups = taps_backward_groups(p, vectors);
     with_type(dtype, [&](auto zero) {
         using T = decltype(zero);
