@@ -26,6 +26,7 @@
 // Where a sequence's keys are split over several items, each leaves its
 // unnormalised result, maximum and sum, and k_join adds them up.
 #include "taps_attention_internal.h"
+#include "taps_lanes.h"
 
 namespace {
 
@@ -110,7 +111,7 @@ template <int D> struct Tile {
 constexpr int max_of(int a, int b) { return a > b ? a : b; }
 template <int D> constexpr int narrow_bytes() {
     return max_of(kWaves * Tile<D>::bytes(kNarrowKeys), kWaves * kNarrowRows * (D + 4) * 4) +
-           kWaves * kNarrowRows * 2 * 4;
+           kWaves * kNarrowRows * 2 * 4 + kNarrowRows * 4;
 }
 
 // The LDS address of a generic pointer to LDS.
@@ -120,19 +121,19 @@ __device__ __forceinline__ uint32_t lds_at(const char *p) {
 
 // 16 bytes a lane from memory to LDS at `lds` + 16 lane, past the registers.
 // The compiler does not see the load: wait_loads() before the barrier that
-// hands the tile over.
+// hands the tile over.  It keeps nothing in m0 (LDS instructions do not read it on gfx9).
 __device__ __forceinline__ void load_to_lds(const char *from, uint32_t lds) {
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off"
                  :
                  : "s"(lds), "v"(from)
-                 : "memory", "m0");
+                 : "memory");
 }
 // The same from a uniform address and an offset a lane.
 __device__ __forceinline__ void load_to_lds(const char *from, uint32_t offset, uint32_t lds) {
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2"
                  :
                  : "s"(lds), "v"(offset), "s"(from)
-                 : "memory", "m0");
+                 : "memory");
 }
 // (the builtin, unlike an instruction in asm, tells the compiler too that no
 // load of its own is under way, or it would wait again inside the loop)
@@ -343,6 +344,16 @@ template <class T, int D> struct Rows {
         __builtin_amdgcn_s_setprio(0);
     }
 
+    // Whether this lane's part of its row's result is not finite.
+    __device__ __forceinline__ bool broken() const {
+        float sum = 0.f;
+#pragma unroll
+        for (int b = 0; b < kBlocks; ++b)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) sum += o[b][i] * 0.f;
+        return sum != sum;
+    }
+
     static __device__ __forceinline__ s16x4 transposed(const char *at) {
         return __builtin_amdgcn_ds_read_tr16_b64_v4i16(
             (__attribute__((address_space(3))) s16x4 *)at);
@@ -374,14 +385,57 @@ __device__ __forceinline__ void store_lse(const taps_attend_launch &p, const tap
         l == 0.f ? kMinusInf : m * p.scale + __builtin_amdgcn_logf(l) * kLn2;
 }
 
-// Writes the result of a wavefront's 32 rows; `row` is this lane's.
+// A row's result once more, by all lanes of a wavefront with two columns each:
+// only the keys that it sees are touched.  In the matrix products the numerator of a
+// hidden key, 0, meets that key's values, which another row of the tile sees; if one
+// is infinite or NaN, so is the product.  m and l do not depend on values.
 template <class T, int D>
-__device__ __forceinline__ void finish(const taps_attend_launch &p, const taps_plan_item &item,
-                                       uint32_t head, const Rows<T, D> &rows, int row, int lane) {
+__device__ __forceinline__ void redo_row(const taps_attend_launch &p, const taps_plan_item &item,
+                                         uint32_t head, int row, float m, float l, int lane) {
+    typedef T v2 __attribute__((ext_vector_type(2)));
+    const int token = row / (int)p.group, sub = row - token * (int)p.group, d = 2 * lane;
+    const int pos = item.first_pos + token;
+    int first = item.lo, last = item.hi - 1;
+    if (p.causal) {
+        last = min(last, pos);
+        if (p.window) first = max(first, pos - (int)p.window + 1);
+    }
+    const bool live = d < (int)p.dim;
+    const float c = p.scale * kLog2e, shift = m == kMinusInf ? 0.f : m * c;
+    v2 q = {};
+    if (live)
+        q = *(const v2 *)(p.q + (int64_t)(item.token0 + token) * p.q_token +
+                          (int64_t)(head * p.group + sub) * p.q_head + 2 * d);
+    float o[2] = {0.f, 0.f};
+    for (int j = first; j <= last; ++j) {
+        const int64_t page = p.pages[item.page0 + (j >> p.page_log2)];
+        const int64_t slot = j & ((1 << p.page_log2) - 1);
+        v2 k = {}, v = {};
+        if (live) {
+            k = *(const v2 *)(p.k_cache + head * p.k_head + page * p.k_page + slot * p.k_slot + 2 * d);
+            v = *(const v2 *)(p.v_cache + head * p.v_head + page * p.v_page + slot * p.v_slot + 2 * d);
+        }
+        const float s = row_sum<64>((float)q[0] * (float)k[0] + (float)q[1] * (float)k[1]);
+        const float e = __builtin_amdgcn_exp2f(s * c - shift);
+        o[0] += e * (float)v[0], o[1] += e * (float)v[1];
+    }
+    if (!live) return;
+    if (item.part < 0) {
+        const float inv = l == 0.f ? 0.f : 1.f / l;
+        *(uint32_t *)(out_row<T>(p, item, head, row) + 2 * d) = pack2<T>(o[0] * inv, o[1] * inv);
+        if (d == 0) store_lse(p, item, head, row, m, l);
+    } else {
+        const int64_t at = (int64_t)(item.part + row - item.row0) * p.kv_heads + head;
+        p.part_o[at * p.dim + d] = o[0], p.part_o[at * p.dim + d + 1] = o[1];
+        if (d == 0) p.part_ml[2 * at] = m, p.part_ml[2 * at + 1] = l;
+    }
+}
+
+template <class T, int D>
+__device__ __forceinline__ void write_rows(const taps_attend_launch &p, const taps_plan_item &item,
+                                           uint32_t head, const Rows<T, D> &rows, int row, float l,
+                                           int half) {
     constexpr int kBlocks = D / 32;
-    const int half = lane >> 5;
-    const float l = half_sum(rows.l);
-    if (row >= item.rows) return;
     if (item.part < 0) {
         const float inv = l == 0.f ? 0.f : 1.f / l;
         char *out = out_row<T>(p, item, head, row);
@@ -408,6 +462,25 @@ __device__ __forceinline__ void finish(const taps_attend_launch &p, const taps_p
             }
         if (half == 0) p.part_ml[2 * at] = rows.m, p.part_ml[2 * at + 1] = l;
     }
+}
+
+// Writes the result of a wavefront's 32 rows; `row` is this lane's.
+template <class T, int D>
+__device__ __forceinline__ void finish(const taps_attend_launch &p, const taps_plan_item &item,
+                                       uint32_t head, const Rows<T, D> &rows, int row, int lane) {
+    const int half = lane >> 5;
+    const float l = half_sum(rows.l);
+    uint32_t again = 0;   // rows to redo: either half of their results is not finite
+    if (item.rows > (int)p.group) {   // rows of several tokens: one sees what another does not
+        const uint64_t broken = __ballot(row < item.rows && rows.broken());
+        again = (uint32_t)broken | (uint32_t)(broken >> 32);
+    }
+    if (row < item.rows && !(again >> (lane & 31) & 1))
+        write_rows(p, item, head, rows, row, l, half);
+    for (int r = 0; r < 32; ++r)
+        if (again >> r & 1)
+            redo_row<T, D>(p, item, head, __shfl(row, r, 64), __shfl(rows.m, r, 64),
+                           __shfl(l, r, 64), lane);
 }
 
 // The keys that all 32 rows from `row0` on see, of the item's: a tile outside
@@ -694,7 +767,7 @@ __device__ __forceinline__ void attend_narrow(const taps_attend_launch &p,
             __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
         }
     }
-    float *ml = (float *)(lds + narrow_bytes<D>() - kWaves * kNarrowRows * 2 * 4);
+    float *ml = (float *)(lds + narrow_bytes<D>() - (2 * kWaves + 1) * kNarrowRows * 4);
     const float l_wave = half_sum(rows.l);
     __syncthreads();   // the tiles are done with
     if (half == 0) {
@@ -720,21 +793,42 @@ __device__ __forceinline__ void attend_narrow(const taps_attend_launch &p,
     }
     __syncthreads();
     const int n_rows = min(kNarrowRows, item.rows - item.row0);
-    for (int k = threadIdx.x; k < n_rows * (D / 4); k += kThreads) {
-        const int r = k / (D / 4), d = 4 * (k % (D / 4));
-        if (d >= (int)p.dim) continue;
-        float top = kMinusInf, l = 0.f;
+    const auto result = [&](int r, int d) {
         f32x4 o = {};
 #pragma unroll
-        for (int w = 0; w < kWaves; ++w) {
-            top = fmaxf(top, ml[2 * (w * kNarrowRows + r)]);
+        for (int w = 0; w < kWaves; ++w)
             o += *(const f32x4 *)(sums + (w * kNarrowRows + r) * (D + 4) + d);
-        }
+        return o;
+    };
+    const auto statistics = [&](int r, float &top, float &l) {
+        top = kMinusInf, l = 0.f;
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w) top = fmaxf(top, ml[2 * (w * kNarrowRows + r)]);
 #pragma unroll
         for (int w = 0; w < kWaves; ++w) {
             const float mw = ml[2 * (w * kNarrowRows + r)], lw = ml[2 * (w * kNarrowRows + r) + 1];
             l += mw == kMinusInf ? lw : lw * __builtin_amdgcn_exp2f((mw - top) * c);
         }
+    };
+    int *again = (int *)(ml + 2 * kWaves * kNarrowRows);   // whether a row is to be redone
+    const bool several = item.rows > (int)p.group;
+    if (several) {
+        if (threadIdx.x < kNarrowRows) again[threadIdx.x] = 0;
+        __syncthreads();
+        for (int k = threadIdx.x; k < n_rows * (D / 4); k += kThreads) {
+            const int r = k / (D / 4);
+            const f32x4 o = result(r, 4 * (k % (D / 4))) * 0.f;
+            const float sum = o[0] + o[1] + o[2] + o[3];
+            if (sum != sum) again[r] = 1;
+        }
+        __syncthreads();
+    }
+    for (int k = threadIdx.x; k < n_rows * (D / 4); k += kThreads) {
+        const int r = k / (D / 4), d = 4 * (k % (D / 4));
+        if (d >= (int)p.dim || (several && again[r])) continue;
+        float top, l;
+        statistics(r, top, l);
+        const f32x4 o = result(r, d);
         if (item.part < 0) {
             const float inv = l == 0.f ? 0.f : 1.f / l;
             char *out = out_row<T>(p, item, head, item.row0 + r);
@@ -746,6 +840,12 @@ __device__ __forceinline__ void attend_narrow(const taps_attend_launch &p,
             *(f32x4 *)(p.part_o + at * p.dim + d) = o;
             if (d == 0) p.part_ml[2 * at] = top, p.part_ml[2 * at + 1] = l;
         }
+    }
+    for (int r = wave; several && r < n_rows; r += kWaves) {
+        if (!again[r]) continue;
+        float top, l;
+        statistics(r, top, l);
+        redo_row<T, D>(p, item, head, item.row0 + r, top, l, lane);
     }
 }
 

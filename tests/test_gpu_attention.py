@@ -481,6 +481,47 @@ def test_attend_many_small_numerators(dtype):
         attend_check(spec, q, [(R.f64(k), R.f64(v))], out, lse, 0.125, dtype)
 
 
+@pytest.mark.parametrize("dtype", [BF16, F16])
+@pytest.mark.parametrize("spec", [
+    ([4, 30], [4, 200], 4, 2, 128, 16, {}),                  # few rows, several tokens
+    ([70, 3], [70, 90], 2, 2, 64, 16, {"window": 20}),
+    ([140], [500], 2, 1, 96, 32, {"window": 65}),
+    ([300], [330], 4, 2, 128, 64, {"units": 1}),
+    ([300], [700], 4, 2, 80, 16, {"units": 1, "window": 100}),
+    ([40], [1500], 8, 2, 128, 64, {"units": 4096}),
+])
+def test_attend_infinities_and_nans(spec, dtype):
+    """Keys and values that are infinite or NaN, among the new tokens and before: they reach the
+    tokens that see them and no others."""
+    q_lens, kv_lens, q_heads, kv_heads, dim, page, options = spec
+    say(f"[gpu] attend infinities {spec} {dtype}")
+    q, caches, plan, kept = attend_case(spec, dtype)
+    pages, _ = page_table(random.Random(4), kv_lens, page)
+    rng = random.Random(5)
+    for s, (n, m) in enumerate(zip(q_lens, kv_lens)):
+        for which, value in ((1, math.nan), (1, math.inf), (1, -math.inf), (0, math.nan)):
+            j = m - 1 - rng.randrange(min(m, n + 40))   # a new token, or one just before them
+            h, d = rng.randrange(kv_heads), rng.randrange(dim)
+            caches[which][pages[s, j // page], h, j % page, d] = value
+            kept[s][which][j, h, d] = value
+    out, lse = A.taps_attend(q, *caches, plan, lse=True)
+    want_bad = clean = 0
+    at = 0
+    for s, (n, m) in enumerate(zip(q_lens, kv_lens)):
+        with np.errstate(invalid="ignore"):
+            want, bound, _, _ = R.attend(R.f64(q[at:at + n]), *kept[s], m - n, 0, True,
+                                         options.get("window", 0), dim ** -0.5, dtype)
+        got = R.f64(out[at:at + n])
+        bad = ~np.isfinite(want)
+        assert np.array_equal(bad, ~np.isfinite(got)), "not the same outputs are finite"
+        R.check(np.where(bad, 0, got), np.where(bad, 0, want), np.where(bad, 1, bound), "finite")
+        inf = np.isinf(want) & ~np.isnan(got)
+        assert np.array_equal(got[inf], want[inf])
+        want_bad, clean = want_bad + bad.sum(), clean + (~bad).sum()
+        at += n
+    assert want_bad and clean
+
+
 def test_attend_far_offsets():
     """Caches of more than 2^32 bytes and 2^31 elements, a sequence at their far end."""
     page, heads, dim, n_pages = 64, 8, 128, 40000   # 2.6e9 elements, 5.2e9 bytes each
