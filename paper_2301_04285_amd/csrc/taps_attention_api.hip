@@ -126,24 +126,57 @@ struct Layout {
     taps_plan_header head{};
 };
 
+// Pieces shorter than this are not made: a split costs a launch and a pass
+// over partial results, some 5 us, in which a workgroup takes about this many
+// keys (one token over 1024 keys of 16 heads: 11.3 us whole, 13.7 in four).
+constexpr int64_t kLeastPiece = 1024;
+
 // Query rows that share their keys' loads, before they are split over the keys.
 struct Strip {
     int32_t seq, row0, rows, lo, hi, kind;
     // what a key costs: a narrow item waits for its bytes, which come to a
     // compute unit at about half the rate at which the others work keys off
     int64_t cost() const { return cost_of(kind, hi - lo); }
+    // pieces of about `piece`: one 3 % above it is not cut again
+    int64_t parts(int64_t piece) const {
+        const int64_t n = (cost() + piece - 1 - piece / 32) / piece;
+        return std::max<int64_t>(1, std::min<int64_t>({n, (hi - lo) / kLeastPiece, 256}));
+    }
     static int64_t cost_of(int32_t kind, int64_t keys) { return keys * (kind == kNarrow ? 2 : 1); }
 };
 
-// Pieces shorter than this are not made: a split costs a launch and a pass
-// over partial results, some 5 us, in which a workgroup takes about this many
-// keys (one token over 1024 keys of 16 heads: 11.3 us whole, 13.7 in four).
-constexpr int64_t kLeastPiece = 1024;
-// Pieces per compute unit that a step is cut into.  Two narrow ones fill a
-// unit and their bytes set the time; wide ones do not all take the same time,
-// and with twice as many the last ones end sooner (512 tokens over 32768 keys:
-// 425 us at two a unit, 370 at four; two tokens over 131001: 187 and 192).
-constexpr int64_t kNarrowPieces = 2, kWidePieces = 4;
+// Pieces per compute unit that narrow items are cut into: two fill a unit, and
+// their bytes set the time (two tokens over 131001 keys: 187 us, 192 at four).
+constexpr int64_t kNarrowPieces = 2;
+
+// The other kinds run in rounds: all pieces of a round take about the same
+// time, and a last round that few pieces share costs as much as a full one.
+// So the length of a piece, in keys, is the one of those below at which the
+// rounds, and what a piece costs beyond its keys, come to the least (512 tokens
+// over 32768 keys, 64 wide strips: 249 us as 256 pieces, 297 as 392 and 331 as
+// 528; 1024 over 20000: 295 as 256 pieces, 378 as 560).
+constexpr int64_t kPieceCost = 256; // a piece's start, end and join, in keys
+constexpr int64_t kMostRounds = 8;  // lengths are tried that come to 1/2, 3/4 .. 8 rounds
+
+int64_t share_of(int64_t total, int64_t times, int64_t among) {
+    return (int64_t)std::min((double)total * (double)times / (double)among, 1e18) + 1;
+}
+
+int64_t piece_of(const std::vector<Strip> &strips, int32_t kind, int64_t slots, int64_t heads) {
+    int64_t total = 0;
+    for (const Strip &t : strips) total += t.kind == kind ? t.cost() : 0;
+    int64_t best = 1, least = INT64_MAX;
+    for (int64_t k = 2; k <= 4 * kMostRounds; ++k) {
+        const int64_t piece = std::max(share_of(total, 4 * heads, slots * k), kLeastPiece);
+        int64_t n = 0;
+        for (const Strip &t : strips)
+            if (t.kind == kind) n += t.parts(piece);
+        const int64_t rounds = (n * heads + slots - 1) / slots;
+        const int64_t cost = rounds * (total / std::max<int64_t>(n, 1) + kPieceCost);
+        if (cost < least) least = cost, best = piece;
+    }
+    return best;
+}
 
 // Rounds of wide items over the compute units, pieces counted, from which they are worth it.
 constexpr int64_t kWideRounds = 4;
@@ -228,13 +261,13 @@ taps_status lay_out(const taps_paged_batch *b, uint32_t cus, Layout *out) {
 
     int64_t total = 0;
     for (const Strip &t : strips) total += t.cost();
-    total *= b->kv_heads;
+    const int64_t heads = b->kv_heads;
+    const int64_t narrow = share_of(total, heads, cus * kNarrowPieces);
+    const int64_t wides = piece_of(strips, kWide, cus, heads);
+    const int64_t blocks = piece_of(strips, kBlock, 2 * (int64_t)cus, heads);
     uint64_t part_rows = 0;
     for (const Strip &t : strips) {
-        const int64_t keys = t.hi - t.lo;
-        const int64_t target = total / (cus * (t.kind == kNarrow ? kNarrowPieces : kWidePieces)) + 1;
-        int64_t parts = std::min((t.cost() + target - 1) / target, keys / kLeastPiece);
-        parts = std::max<int64_t>(1, std::min<int64_t>(parts, 256));
+        int64_t parts = t.parts(t.kind == kNarrow ? narrow : t.kind == kBlock ? blocks : wides);
         // whole tiles, counted from where the strip's first tile starts
         const int64_t start = t.lo & ~15, tiles = (t.hi - start + 127) / 128;
         parts = std::max<int64_t>(1, std::min(parts, tiles));
