@@ -484,15 +484,19 @@ __device__ __forceinline__ void finish(const taps_attend_launch &p, const taps_p
 }
 
 // The keys that all 32 rows from `row0` on see, of the item's: a tile outside
-// needs a mask.  (Tiles that no row of one wavefront sees are taken all the same,
-// masked: leaving them out costs the other tiles 64 register moves each.)
+// needs a mask.  A wavefront does nothing with the tiles from `end` on but load
+// its part of them: a branch within the loop costs the other tiles 64 register
+// moves each, a second loop behind it nothing (prompts of 2048: 364 -> 350 us,
+// 1024 of 16 heads of 64: 36 -> 33).
 struct Seen {
     int from, to;
+    int end;   // no row sees a key from here on
     __device__ __forceinline__ Seen(const taps_attend_launch &p, const taps_plan_item &item,
                                     int row0) {
-        from = item.lo, to = item.hi - 1;
+        from = item.lo, to = item.hi - 1, end = row0 < item.rows ? item.hi : item.lo;
         if (!p.causal) return;
         const int a = min(row0, item.rows - 1), b = min(row0 + 31, item.rows - 1);
+        end = min(end, item.first_pos + b / (int)p.group + 1);
         to = min(to, item.first_pos + a / (int)p.group);
         if (p.window) from = max(from, item.first_pos + b / (int)p.group - (int)p.window + 1);
     }
@@ -579,6 +583,7 @@ __global__ __launch_bounds__(kWideThreads, 2) void k_attend_wide(taps_attend_lau
         const Loader<D> loader(p, item, head, second, wave, lane);
         const char *k_lds = lds, *v_lds = lds + 3 * kPart;
         const int tiles = (item.hi - start + kWideKeys - 1) / kWideKeys;
+        const int used = min(max((seen.end - start + kWideKeys - 1) / kWideKeys, 1), tiles);
         const auto tile0 = [&](int i) { return start + i * kWideKeys; };
         const auto page_of = [&](int t0) {
             return page_at(p, pages, t0 + loader.key0, item.lo, item.hi);
@@ -606,7 +611,7 @@ __global__ __launch_bounds__(kWideThreads, 2) void k_attend_wide(taps_attend_lau
         wait_loads<0>();
         end_phase();
         if (!second) {
-            for (int i = 0; i < tiles; ++i, turn()) {
+            for (int i = 0; i < used; ++i, turn()) {
                 if (i)
                     rows.products(v_lds + b0 * kPart, y, k_lds + b1 * kPart, x, lane);
                 else
@@ -618,23 +623,44 @@ __global__ __launch_bounds__(kWideThreads, 2) void k_attend_wide(taps_attend_lau
                 wait(i + 2 < tiles);
                 end_phase();
             }
+            rows.spend(v_lds + b0 * kPart, y, lane);   // the last tile's
+            for (int i = used; i < tiles; ++i, turn()) {
+                end_phase();
+                if (i + 2 < tiles) loader.load(tile0(i + 2), page, k_lds + b0 * kPart);
+                page = page_of(tile0(i + 3));
+                wait(i + 2 < tiles);
+                end_phase();
+            }
         } else {
             end_phase();
             rows.score(k_lds, x, lane);
             end_phase();
-            for (int i = 1; i < tiles; ++i, turn()) {
+            int i = 1;
+            const auto begin = [&]() {
                 if (i + 1 < tiles) loader.load(tile0(i + 1), page, v_lds + b0 * kPart);
                 page = page_of(tile0(i + 2));
+            };
+            for (; i < used; ++i, turn()) {
+                begin();
                 soften(tile0(i - 1));
                 end_phase();
                 rows.products(v_lds + b1 * kPart, y, k_lds + b2 * kPart, x, lane);
                 wait(i + 1 < tiles);
                 end_phase();
             }
-            soften(tile0(tiles - 1));
-            b0 = b1;
+            begin();
+            soften(tile0(used - 1));
+            if (used < tiles) end_phase();
+            rows.spend(v_lds + b1 * kPart, y, lane);
+            for (; i < tiles; ++i, turn()) {
+                if (i > used) {
+                    begin();
+                    end_phase();
+                }
+                wait(i + 1 < tiles);
+                end_phase();
+            }
         }
-        rows.spend(v_lds + b0 * kPart, y, lane);   // the last tile's
     }
     finish(p, item, head, rows, row, lane);
 }
@@ -662,10 +688,11 @@ __device__ __forceinline__ void attend_block(const taps_attend_launch &p, const 
         v.load(start, page, lds + kPart);
         page = page_of(start + kWideKeys);
     }
-    for (int t0 = start; item.lo < item.hi && t0 < item.hi; t0 += kWideKeys, buffer ^= 1) {
-        const char *tile = lds + 2 * buffer * kPart, *next = lds + 2 * (buffer ^ 1) * kPart;
-        // one barrier a tile: the tile's loads have ended in every wavefront, and every
-        // wavefront is done with the other buffer
+    int t0 = start;
+    // one barrier a tile: the tile's loads have ended in every wavefront, and every
+    // wavefront is done with the other buffer
+    const auto begin = [&]() {
+        const char *next = lds + 2 * (buffer ^ 1) * kPart;
         wait_loads<0>();
         __syncthreads();
         if (t0 + kWideKeys < item.hi) {
@@ -673,12 +700,17 @@ __device__ __forceinline__ void attend_block(const taps_attend_launch &p, const 
             v.load(t0 + kWideKeys, page, next + kPart);
             page = page_of(t0 + 2 * kWideKeys);
         }
+    };
+    for (; t0 < min(item.hi, seen.end); t0 += kWideKeys, buffer ^= 1) {
+        const char *tile = lds + 2 * buffer * kPart;
+        begin();
         typename Rows<T, D>::template Scores<kWideKeys> x;
         typename Rows<T, D>::template Numerators<kWideKeys> y;
         rows.score(tile, x, lane);
         rows.soften(x, y, t0, seen.masks(t0, kWideKeys), c, lane);
         rows.spend(tile + kPart, y, lane);
     }
+    for (; t0 < item.hi; t0 += kWideKeys, buffer ^= 1) begin();   // the other wavefronts' tiles
     finish(p, item, head, rows, row, lane);
 }
 
