@@ -13,16 +13,18 @@
 // In the accumulator's layout a lane then holds 16 of a tile's 32 keys for
 // one query row: the softmax needs one exchange between the two halves of a
 // wavefront per tile, and P^T, rounded to the cache's type, is the second
-// product's operand as it lies in the registers.  V^T comes out of LDS by the transposing read
-// (four keys of one column per lane).  The order in which a product takes its keys is free, so
-// the second takes them as the first left them.
+// product's operand as it lies in the registers.  V^T comes out of LDS by the
+// transposing read (four keys of one column per lane).  The order in which a
+// product takes its keys is free, so the second takes them as the first left
+// them.
 //
-// Two kinds of items (workgroups of four wavefronts):
-//   wide    128 query rows, 32 a wavefront; all share tiles of 64 keys;
-//   narrow  up to 32 query rows; every wavefront takes every fourth tile of 32 keys, and the
-//           four results are joined in LDS.
-// The next tile is on its way while the present one is in use: straight to a
-// second buffer in LDS (wide), or in registers (narrow).
+// Three kinds of items, each a workgroup's:
+//   wide    256 query rows, 32 for each of eight wavefronts, tiles of 64 keys;
+//           the halves of the workgroup take products and softmax in turns;
+//   block   128 query rows, 32 for each of four wavefronts, tiles of 64 keys;
+//   narrow  up to 32 query rows; each of four wavefronts takes every fourth tile
+//           of 32 keys, and the four results are joined in LDS.
+// Tiles go straight from memory to LDS while the ones before them are in use.
 // Where a sequence's keys are split over several items, each leaves its
 // unnormalised result, maximum and sum, and k_join adds them up.
 #include "taps_attention_internal.h"
@@ -33,8 +35,9 @@ namespace {
 constexpr int kThreads = 256, kWaves = 4, kWideThreads = 2 * kWideRows;
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 constexpr float kMinusInf = -__builtin_inff();
-// A row's maximum is raised only when a tile's numerators (this lane's 16 or 32) add up to more than this: none exceeds it, far inside every
-// type's range, and most tiles neither look for their maximum nor touch the accumulators.
+// A row's maximum is raised only when a tile's numerators (this lane's 16 or 32)
+// add up to more than this: none exceeds it, far inside every type's range, and
+// most tiles neither look for their maximum nor touch the accumulators.
 constexpr float kMostSum = 4096.f;
 
 typedef float f32x16 __attribute__((ext_vector_type(16)));

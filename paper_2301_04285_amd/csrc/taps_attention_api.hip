@@ -119,8 +119,16 @@ taps_status check_norm_rotate(const taps_norm_rotate_args *a, taps_rows_launch *
 
 uint64_t up16(uint64_t v) { return (v + 15) & ~15ull; }
 
+struct Sequence {
+    int32_t token0;      // its first token
+    int32_t rows;        // query rows: q_len * (q_heads / kv_heads)
+    int32_t kv_start, kv_len;
+    int32_t first_pos;   // position of its first token
+    int32_t page0;       // its pages in the plan's array
+};
+
 struct Layout {
-    std::vector<taps_plan_seq> seqs;
+    std::vector<Sequence> seqs;
     std::vector<taps_plan_item> items;
     std::vector<taps_plan_join> joins;
     taps_plan_header head{};
@@ -178,7 +186,9 @@ int64_t piece_of(const std::vector<Strip> &strips, int32_t kind, int64_t slots, 
     return best;
 }
 
-// Rounds of wide items over the compute units, pieces counted, from which they are worth it.
+// Rounds of wide items over the compute units, pieces counted, from which they
+// are worth it (512 strips of 256 rows, prompts of 1024 with 16 heads of 64: 41 us
+// wide, 36 in blocks; 64 strips that 32768 keys make 2048 pieces of: 249 and 279).
 constexpr int64_t kWideRounds = 4;
 
 taps_status lay_out(const taps_paged_batch *b, uint32_t cus, Layout *out) {
@@ -216,7 +226,7 @@ taps_status lay_out(const taps_paged_batch *b, uint32_t cus, Layout *out) {
             if (n && first < kv) written.push_back(row[g]);
         if (kv < n) appendable = false;
         if (n) most = std::max(most, kv);
-        taps_plan_seq q{};
+        Sequence q{};
         q.token0 = (int32_t)tokens;
         q.rows = (int32_t)(n * group);
         q.kv_start = (int32_t)from, q.kv_len = (int32_t)kv;
@@ -233,17 +243,17 @@ taps_status lay_out(const taps_paged_batch *b, uint32_t cus, Layout *out) {
         return fail(TAPS_ERR_ARG, "page %d is to be written from two places of the page table",
                     *std::adjacent_find(written.begin(), written.end()));
 
-    // Strips of 256 rows read the fewest keys, where there are enough of them to
-    // keep every compute unit busy for a few rounds; else strips of 128.
+    // Strips of 256 rows read the fewest keys, where there are enough of them;
+    // else strips of 128.
     int64_t wide = 0;
-    for (const taps_plan_seq &q : out->seqs)
+    for (const Sequence &q : out->seqs)
         wide += q.rows / kWideRows * std::max<int64_t>(1, q.kv_len / kLeastPiece);
     const bool few = wide * b->kv_heads < kWideRounds * (int64_t)cus;
     for (uint32_t s = 0; s < b->n_seqs; ++s) {
-        const taps_plan_seq &q = out->seqs[s];
-        const int32_t kind = q.rows <= kNarrowRows           ? kNarrow
+        const Sequence &q = out->seqs[s];
+        const int32_t kind = q.rows <= kNarrowRows         ? kNarrow
                              : few || q.rows <= kBlockRows ? kBlock
-                                                             : kWide;
+                                                           : kWide;
         const int32_t step = kind == kNarrow ? kNarrowRows : kind == kBlock ? kBlockRows : kWideRows;
         for (int32_t r = 0; r < q.rows; r += step) {
             Strip t{(int32_t)s, r, std::min(step, q.rows - r), q.kv_start, q.kv_len, kind};
@@ -280,7 +290,7 @@ taps_status lay_out(const taps_paged_batch *b, uint32_t cus, Layout *out) {
         for (int64_t k = 0; k < parts; ++k) {
             taps_plan_item i{};
             i.seq = t.seq, i.row0 = t.row0, i.kind = t.kind;
-            const taps_plan_seq &q = out->seqs[t.seq];
+            const Sequence &q = out->seqs[t.seq];
             i.token0 = q.token0, i.rows = q.rows, i.first_pos = q.first_pos, i.page0 = q.page0;
             i.lo = (int32_t)std::max<int64_t>(t.lo, start + 128 * (tiles * k / parts));
             i.hi = (int32_t)std::min<int64_t>(t.hi, start + 128 * (tiles * (k + 1) / parts));
@@ -312,7 +322,6 @@ taps_status lay_out(const taps_paged_batch *b, uint32_t cus, Layout *out) {
     h.max_positions = (uint32_t)most;
     h.appendable = appendable;
     uint64_t at = up16(sizeof h);
-    h.seqs_at = at, at = up16(at + out->seqs.size() * sizeof(taps_plan_seq));
     h.tokens_at = at, at = up16(at + tokens * sizeof(taps_plan_token));
     h.pages_at = at, at = up16(at + pages * 4);
     h.items_at = at, at = up16(at + out->items.size() * sizeof(taps_plan_item));
@@ -329,7 +338,6 @@ uint64_t workspace_of(const taps_plan_header &h) {
 void write_plan(const taps_paged_batch *b, const Layout &l, char *to) {
     const taps_plan_header &h = l.head;
     memcpy(to, &h, sizeof h);
-    if (!l.seqs.empty()) memcpy(to + h.seqs_at, l.seqs.data(), l.seqs.size() * sizeof l.seqs[0]);
     if (!l.items.empty())
         memcpy(to + h.items_at, l.items.data(), l.items.size() * sizeof l.items[0]);
     if (!l.joins.empty())
@@ -338,7 +346,7 @@ void write_plan(const taps_paged_batch *b, const Layout &l, char *to) {
     auto *pages = (int32_t *)(to + h.pages_at);
     for (uint32_t s = 0; s < h.n_seqs; ++s) {
         const int32_t *row = b->pages + (uint64_t)s * b->pages_stride;
-        const taps_plan_seq &q = l.seqs[s];
+        const Sequence &q = l.seqs[s];
         const int64_t n_pages = ((int64_t)q.kv_len + b->page_size - 1) >> h.page_log2;
         for (int64_t g = 0; g < n_pages; ++g) *pages++ = row[g];
         for (int64_t p = (int64_t)q.kv_len - b->q_lens[s]; p < q.kv_len; ++p, ++token) {

@@ -8,7 +8,7 @@
 #include "taps_attention.h"
 
 // ---------------------------------------------------------------------------
-// plan of a step (taps_paged_plan): a header and five arrays, the same bytes
+// plan of a step (taps_paged_plan): a header and four arrays, the same bytes
 // on the host and on the device
 // ---------------------------------------------------------------------------
 
@@ -17,7 +17,7 @@ constexpr uint32_t kPlanMagic = 0x54415031;
 // Query rows of the kinds of items (taps_attend.hip).  A row is a pair of a
 // token and one of the query heads of a key head.
 constexpr int kWideRows = 256, kBlockRows = 128, kNarrowRows = 32;
-// Keys of a tile of either.
+// Keys of a tile: of wide and block items, and of narrow ones.
 constexpr int kWideKeys = 64, kNarrowKeys = 32;
 
 struct taps_plan_header {
@@ -33,25 +33,17 @@ struct taps_plan_header {
     uint32_t n_wide, reserved;
     uint32_t zeros[4];        // what attention reads for keys that are not there
     // byte offsets of the arrays
-    uint64_t seqs_at, tokens_at, pages_at, items_at, joins_at;
+    uint64_t tokens_at, pages_at, items_at, joins_at;
 };
 static_assert(offsetof(taps_plan_header, zeros) % 16 == 0, "read 16 bytes at a time");
-
-struct taps_plan_seq {
-    int32_t token0;      // its first token
-    int32_t rows;        // query rows: q_len * (q_heads / kv_heads)
-    int32_t kv_start, kv_len;
-    int32_t first_pos;   // position of its first token
-    int32_t page0;       // its pages in the pages array
-    int32_t reserved[2];
-};
 
 struct taps_plan_token {
     int32_t position;
     int32_t slot;   // page * page_size + slot; -1: not appended
 };
 
-// One workgroup of attention per item and key head.
+// One workgroup of attention per item and key head.  The kinds differ in rows
+// and in how a workgroup shares them out (taps_attend.hip).
 enum { kWide, kBlock, kNarrow };
 
 struct taps_plan_item {

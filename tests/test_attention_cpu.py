@@ -47,7 +47,7 @@ class Header(C.Structure):
                                    "n_pages", "causal", "window", "n_items", "n_joins",
                                    "part_rows", "max_positions", "appendable", "join_rounds",
                                    "n_wide", "reserved")] + [("zeros", C.c_uint32 * 4)] + \
-        [(n, C.c_uint64) for n in ("seqs_at", "tokens_at", "pages_at", "items_at", "joins_at")]
+        [(n, C.c_uint64) for n in ("tokens_at", "pages_at", "items_at", "joins_at")]
 
 
 def parts(p):
@@ -56,7 +56,7 @@ def parts(p):
 
     def words(at, n, k):
         return raw[at:at + 4 * n * k].view(np.int32).reshape(n, k)
-    return (h, words(h.seqs_at, h.n_seqs, 8), words(h.tokens_at, h.tokens, 2),
+    return (h, words(h.tokens_at, h.tokens, 2),
             words(h.items_at, h.n_items, 12), words(h.joins_at, h.n_joins, 8))
 
 
@@ -76,7 +76,7 @@ def test_plan_covers_every_visible_pair_once(seed):
     # lengths below the new tokens' leave no tokens to append: plans for attention alone
     p = plan(q_lens, kv_lens, kv_starts=starts, causal=causal, window=window, kv_heads=kv_heads,
              q_heads=group * kv_heads, units=r.choice((1, 16, 256, 100000)))
-    h, seqs, tokens, items, joins = parts(p)
+    h, tokens, items, joins = parts(p)
     assert h.bytes == p._host.numel() and h.tokens == sum(q_lens)
     kinds = items[:, 4].tolist()   # 0: 256 rows, 1: 128, 2: 32
     assert kinds == sorted(kinds) and h.n_wide == kinds.count(0)
