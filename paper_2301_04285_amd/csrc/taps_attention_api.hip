@@ -186,6 +186,47 @@ int64_t piece_of(const std::vector<Strip> &strips, int32_t kind, int64_t slots, 
     return best;
 }
 
+// The order in which items start: kind by kind.  Workgroups that run at the same
+// time should find each other's keys in the cache, and the last ones to start
+// should be cheap.  So the items of a sequence follow each other, its dear ones
+// first, up to the last sequences, which come to the time of one dear item on
+// every slot: of those the dear items come first, whatever their sequence
+// (prompts of 2048 of eight sequences, 32 heads: 350 us with all dear items first, 321
+// so, 321 by sequences alone; 20 of 100 to 700 tokens: 107, 108 and 119).
+// Narrow items share no keys: dear ones first.
+void in_order(std::vector<taps_plan_item> *items, int64_t cus, int64_t heads) {
+    const auto cost = [](const taps_plan_item &i) { return Strip::cost_of(i.kind, i.hi - i.lo); };
+    const auto dear = [&](const taps_plan_item &x, const taps_plan_item &y) {
+        return cost(x) >> 8 > cost(y) >> 8;
+    };
+    std::stable_sort(items->begin(), items->end(),
+                     [](const taps_plan_item &x, const taps_plan_item &y) {
+                         return std::make_pair(x.kind, x.seq) < std::make_pair(y.kind, y.seq);
+                     });
+    for (auto at = items->begin(); at != items->end();) {
+        const int32_t kind = at->kind;
+        const int64_t slots = kind == kWide ? cus : 2 * cus;
+        const auto end = std::find_if(at, items->end(),
+                                      [&](const taps_plan_item &i) { return i.kind != kind; });
+        int64_t sum = 0, most = 0;
+        auto rest = end;   // where the last sequences begin
+        while (rest != at && (kind == kNarrow || !sum || sum * heads < slots * most)) {
+            const int32_t seq = (rest - 1)->seq;
+            for (; rest != at && (rest - 1)->seq == seq; --rest)
+                sum += cost(*(rest - 1)), most = std::max(most, cost(*(rest - 1)));
+        }
+        while (at != rest) {
+            const int32_t seq = at->seq;
+            const auto next = std::find_if(at, rest,
+                                           [&](const taps_plan_item &i) { return i.seq != seq; });
+            std::stable_sort(at, next, dear);
+            at = next;
+        }
+        std::stable_sort(rest, end, dear);
+        at = end;
+    }
+}
+
 // Rounds of wide items over the compute units, pieces counted, from which they
 // are worth it (512 strips of 256 rows, prompts of 1024 with 16 heads of 64: 41 us
 // wide, 36 in blocks; 64 strips that 32768 keys make 2048 pieces of: 249 and 279).
@@ -300,14 +341,7 @@ taps_status lay_out(const taps_paged_batch *b, uint32_t cus, Layout *out) {
         if (parts > 1) part_rows += (uint64_t)parts * t.rows;
         if (part_rows >= (1ull << 31)) return fail(TAPS_ERR_ARG, "too many rows are split");
     }
-    // kind by kind, and dear items first, so that the last to start are cheap
-    const auto order = [](const taps_plan_item &i) {
-        return std::make_pair(i.kind, -(Strip::cost_of(i.kind, i.hi - i.lo) >> 8));
-    };
-    std::stable_sort(out->items.begin(), out->items.end(),
-                     [&](const taps_plan_item &x, const taps_plan_item &y) {
-                         return order(x) < order(y);
-                     });
+    in_order(&out->items, cus, heads);
     for (const taps_plan_item &i : out->items) h.n_wide += i.kind == kWide;
     if (out->items.size() * b->kv_heads >= (1ull << 31) || b->kv_heads > 65535)
         return fail(TAPS_ERR_ARG, "too many workgroups");
