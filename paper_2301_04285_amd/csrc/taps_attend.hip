@@ -970,7 +970,8 @@ __global__ __launch_bounds__(kThreads) void k_join(taps_attend_launch p) {
 }
 
 template <class T, int D> void launch_items(const taps_attend_launch &p, hipStream_t stream) {
-    if (p.n_wide) k_attend_wide<T, D><<<p.n_wide * p.kv_heads, kWideThreads, 0, stream>>>(p);
+    if constexpr (D > kWideAbove)
+        if (p.n_wide) k_attend_wide<T, D><<<p.n_wide * p.kv_heads, kWideThreads, 0, stream>>>(p);
     if (p.n_items > p.n_wide)
         k_attend<T, D><<<(p.n_items - p.n_wide) * p.kv_heads, kThreads, 0, stream>>>(p);
 }

@@ -227,10 +227,31 @@ void in_order(std::vector<taps_plan_item> *items, int64_t cus, int64_t heads) {
     }
 }
 
-// Rounds of wide items over the compute units, pieces counted, from which they
-// are worth it (512 strips of 256 rows, prompts of 1024 with 16 heads of 64: 41 us
-// wide, 36 in blocks; 64 strips that 32768 keys make 2048 pieces of: 249 and 279).
-constexpr int64_t kWideRounds = 4;
+// Whether sequences of more than 128 rows are cut into strips of 256 rows (wide
+// items), which read the fewest keys, or of 128.  Wide ones pay
+//   - for heads of more than kWideAbove, where two blocks fill a unit (eight prompts of
+//     2048, 32 heads of 64: 212 us wide, 177 in blocks; 512 tokens over 32768
+//     keys, 32 heads of 64 over 8: 170 and 174; of 96: 209 and 223);
+//   - if the keys they see keep the loop busy beside a workgroup's start and end,
+//     which nothing covers (32 heads of 96, prompts of 1024: 184 and 171, of 2048: 266
+//     and 264, of 8000: 396 and 404; of 128 and 2048: 319 and 325);
+//   - if there are some rounds of them over the units, pieces counted (4 sequences of
+//     2048, 4 heads of 128: 51 and 48).
+constexpr int64_t kWideKeysSeen = 1024, kWideRounds = 4;
+
+bool wide_pays(const taps_paged_batch *b, const std::vector<Sequence> &seqs, int64_t window,
+               int64_t cus) {
+    int64_t strips = 0, pieces = 0, keys = 0;
+    for (const Sequence &q : seqs) {
+        const int64_t n = q.rows / kWideRows, kv = q.kv_len - q.kv_start;
+        int64_t seen = b->causal ? kv - (q.kv_len - q.first_pos) / 2 : kv;   // on average
+        if (window) seen = std::min(seen, window);
+        strips += n, keys += n * seen;
+        pieces += n * std::max<int64_t>(1, kv / kLeastPiece);
+    }
+    return b->head_dim > kWideAbove && keys >= kWideKeysSeen * strips &&
+           pieces * b->kv_heads >= kWideRounds * cus;
+}
 
 taps_status lay_out(const taps_paged_batch *b, uint32_t cus, Layout *out) {
     taps_plan_header &h = out->head;
@@ -284,17 +305,12 @@ taps_status lay_out(const taps_paged_batch *b, uint32_t cus, Layout *out) {
         return fail(TAPS_ERR_ARG, "page %d is to be written from two places of the page table",
                     *std::adjacent_find(written.begin(), written.end()));
 
-    // Strips of 256 rows read the fewest keys, where there are enough of them;
-    // else strips of 128.
-    int64_t wide = 0;
-    for (const Sequence &q : out->seqs)
-        wide += q.rows / kWideRows * std::max<int64_t>(1, q.kv_len / kLeastPiece);
-    const bool few = wide * b->kv_heads < kWideRounds * (int64_t)cus;
+    const bool wide = wide_pays(b, out->seqs, h.window, cus);
     for (uint32_t s = 0; s < b->n_seqs; ++s) {
         const Sequence &q = out->seqs[s];
-        const int32_t kind = q.rows <= kNarrowRows         ? kNarrow
-                             : few || q.rows <= kBlockRows ? kBlock
-                                                           : kWide;
+        const int32_t kind = q.rows <= kNarrowRows          ? kNarrow
+                             : wide && q.rows > kBlockRows ? kWide
+                                                           : kBlock;
         const int32_t step = kind == kNarrow ? kNarrowRows : kind == kBlock ? kBlockRows : kWideRows;
         for (int32_t r = 0; r < q.rows; r += step) {
             Strip t{(int32_t)s, r, std::min(step, q.rows - r), q.kv_start, q.kv_len, kind};

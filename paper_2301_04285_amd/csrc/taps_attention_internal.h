@@ -17,6 +17,8 @@ constexpr uint32_t kPlanMagic = 0x54415031;
 // Query rows of the kinds of items (taps_attend.hip).  A row is a pair of a
 // token and one of the query heads of a key head.
 constexpr int kWideRows = 256, kBlockRows = 128, kNarrowRows = 32;
+// Only plans for heads of more have wide items.
+constexpr uint32_t kWideAbove = 64;
 // Keys of a tile: of wide and block items, and of narrow ones.
 constexpr int kWideKeys = 64, kNarrowKeys = 32;
 
