@@ -130,13 +130,13 @@ typedef struct {
 /* Lays a step out for taps_cache_append and taps_attend: every token's slot,
  * and the work of attention cut into pieces of like size for `cus` compute
  * units (0: 256).  A plan serves every layer of the step and any cache with
- * its page size, at least its pages and its heads.  `plan` is host memory, 16-byte aligned, of
- * *plan_bytes bytes (NULL: only the needed size is written); the caller
- * copies it to the device and passes both copies on, unchanged.
- * *workspace_bytes is what taps_attend needs.  TAPS_ERR_ARG also for a page
- * number outside 0 .. n_pages - 1 where a key is or is to be written, for
- * lengths above 2^30, 2^31 or more tokens or slots in all, and if a page is to be written
- * from two places of the page table.
+ * its page size, at least its pages and its heads.  `plan` is host memory,
+ * 16-byte aligned, of *plan_bytes bytes (NULL: only the needed size is
+ * written); the caller copies it to the device and passes both copies on,
+ * unchanged.  *workspace_bytes is what taps_attend needs.  TAPS_ERR_ARG also
+ * for a page number outside 0 .. n_pages - 1 where a key is or is to be
+ * written, for lengths above 2^30, 2^31 or more tokens or slots in all, and if
+ * a page is to be written from two places of the page table.
  * A sequence with kv_lens < q_lens can be attended (tokens at negative
  * positions see nothing), not appended. */
 taps_status taps_paged_plan(const taps_paged_batch *batch, uint32_t cus, void *plan,

@@ -24,7 +24,8 @@
 //   block   128 query rows, 32 for each of four wavefronts, tiles of 64 keys;
 //   narrow  up to 32 query rows; each of four wavefronts takes every fourth tile
 //           of 32 keys, and the four results are joined in LDS.
-// Tiles go straight from memory to LDS while the ones before them are in use.
+// Tiles of the first two go straight from memory to LDS while the ones before
+// them are in use; those of narrow items wait in registers.
 // Where a sequence's keys are split over several items, each leaves its
 // unnormalised result, maximum and sum, and k_join adds them up.
 #include "taps_attention_internal.h"
@@ -280,6 +281,9 @@ template <class T, int D> struct Rows {
         }
         l += sum;
     }
+    // They are rounded for the product with the values, which takes operands of the
+    // cache's type only: an error of 2^-9 (bf16) or 2^-12 of each, independent of each
+    // other and no larger than the values' own.  Their sum is taken before, in 32 bits.
     template <int Keys>
     __device__ __forceinline__ float numerators(const Scores<Keys> &x, Numerators<Keys> &y,
                                                 float c) const {
@@ -558,10 +562,13 @@ template <int D> struct Loader {
 // of this one), and softmax.  While the first four wavefronts, one on each SIMD,
 // are in one of them, the others are in the other, so that the matrix cores
 // have a wavefront of their own at any time and a tile's loads serve twice the
-// rows of a block item: 512 tokens over 32768 keys of 8 heads of 128, four query
-// heads each, 366 -> 327 us (890 TFLOP/s in the kernel; with the loads, the
-// exponentials and the reads of LDS taken out in turns it gains 17, 12 and 12 %, with all of them
-// it runs at the rate of a large matrix product).
+// rows of a block item.
+// Bound by the matrix cores at the clocks that they leave (some 1.8 of 2.4 GHz): 512
+// tokens over 32768 keys, 32 heads of 128 over 8, 247 us here, 1110 TFLOP/s (279 in
+// blocks); eight sequences of 2048 tokens, 32 heads, not causal, take 0.21 us a
+// key, 1280 TFLOP/s, and 90 us besides, for starting, reading queries and writing
+// results eight times on every unit.  One workgroup a unit that loads its next
+// item's tiles and queries while it ends the last takes no less (364 and 360 us).
 template <class T, int D>
 __global__ __launch_bounds__(kWideThreads, 2) void k_attend_wide(taps_attend_launch p) {
     constexpr int kPart = kWideKeys * Tile<D>::kRow;   // a tile's K, or its V
@@ -578,7 +585,7 @@ __global__ __launch_bounds__(kWideThreads, 2) void k_attend_wide(taps_attend_lau
     rows.start(p, item, head, row, lane);
     const Seen seen(p, item, row0);
     if (item.lo < item.hi) {
-        // Both halves use all tiles; the first loads K, the other V.  K of tile i is read in phases
+        // Both halves use all tiles that they see; the first loads K, the other V.  K of tile i is read in phases
         // 2 i and 2 i + 1, V in the two after them.  Three tiles of each are kept: K of tile i + 2
         // is loaded in phase 2 i + 1, V of tile i + 1 in phase 2 i.
         typename Rows<T, D>::template Scores<kWideKeys> x;
@@ -594,8 +601,8 @@ __global__ __launch_bounds__(kWideThreads, 2) void k_attend_wide(taps_attend_lau
         const auto soften = [&](int t0) {
             rows.soften(x, y, t0, seen.masks(t0, kWideKeys), c, lane);
         };
-        // buffers: of tiles i - 1, i, i + 1 in the first half's loop, i - 2, i - 1, i in the other's;
-        // the oldest is loaded anew
+        // buffers: of tiles i - 1, i, i + 1 in the first half's loop, i - 2, i - 1, i in the
+        // other's; the oldest is loaded anew
         int b0 = 2, b1 = 0, b2 = 1;
         const auto turn = [&]() {
             const int b = b0;
@@ -668,8 +675,11 @@ __global__ __launch_bounds__(kWideThreads, 2) void k_attend_wide(taps_attend_lau
     finish(p, item, head, rows, row, lane);
 }
 
-// 128 query rows, 32 a wavefront, two workgroups to a unit.  Tiles of 64 keys in
-// two buffers, one loaded while the other is in use.
+// 128 query rows, 32 a wavefront, two workgroups to a unit (three for heads of up to
+// 64), which fill each other's gaps.  Tiles of 64 keys in two buffers, one loaded
+// while the other is in use.  Eight prompts of 1024, 16 heads of 64: 33 us, of which
+// the products alone would take 13 and the bytes 14; short rounds with a start and
+// an end each bound it.  (Four wavefronts a SIMD, with 128 registers: 49 for 37.)
 template <class T, int D>
 __device__ __forceinline__ void attend_block(const taps_attend_launch &p, const taps_plan_item &item,
                                              uint32_t head, char *lds) {
@@ -717,7 +727,10 @@ __device__ __forceinline__ void attend_block(const taps_attend_launch &p, const 
     finish(p, item, head, rows, row, lane);
 }
 
-// Up to 32 query rows: every wavefront has all of them and its own keys.
+// Up to 32 query rows: every wavefront has all of them and its own keys, so that
+// a unit has eight tiles on their way at any time.  Bytes bound it: 64 tokens over 2 to
+// 4000 keys each, 32 heads of 128 over 8, 104 us and 5 for the join, 5.3 TB/s; two
+// over 131001, 183 and 5, 5.9 TB/s.
 template <class T, int D>
 __device__ __forceinline__ void attend_narrow(const taps_attend_launch &p,
                                               const taps_plan_item &item, uint32_t head, char *lds) {
@@ -983,7 +996,8 @@ template <class T> hipError_t launch(const taps_attend_launch &p, hipStream_t st
         launch_items<T, 96>(p, stream);
     else
         launch_items<T, 128>(p, stream);
-    if (p.n_joins) k_join<T><<<dim3(p.n_joins, p.kv_heads, p.join_rounds), kThreads, 0, stream>>>(p);
+    if (p.n_joins)
+        k_join<T><<<dim3(p.n_joins, p.kv_heads, p.join_rounds), kThreads, 0, stream>>>(p);
     return hipGetLastError();
 }
 

