@@ -60,7 +60,7 @@ def parts(p):
             words(h.items_at, h.n_items, 12), words(h.joins_at, h.n_joins, 8))
 
 
-@pytest.mark.parametrize("seed", range(60))
+@pytest.mark.parametrize("seed", range(75))
 def test_plan_covers_every_visible_pair_once(seed):
     """Every row is in one strip; the pieces of a strip follow each other over exactly the keys
     that any of its rows sees; partial results do not overlap and fit the workspace."""
@@ -68,6 +68,9 @@ def test_plan_covers_every_visible_pair_once(seed):
     n = r.randint(1, 5)
     q_lens = [r.choice((0, 1, 1, 2, 7, 40, 300)) for _ in range(n)]
     kv_lens = [r.choice((0, 1, 15, 16, 17, 64, 129, 1000, 5000)) for _ in range(n)]
+    if seed >= 60:   # strips of 256 rows
+        q_lens, kv_lens = [300] + q_lens, [r.choice((5000, 9001))] + kv_lens
+        n += 1
     starts = [r.choice((0, 0, r.randint(0, k))) for k in kv_lens]
     causal = r.random() < 0.8
     window = r.choice((0, 0, 1, 16, 100, 2 ** 31)) if causal else 0
@@ -75,7 +78,8 @@ def test_plan_covers_every_visible_pair_once(seed):
     group = r.choice((1, 3, 4, 16))
     # lengths below the new tokens' leave no tokens to append: plans for attention alone
     p = plan(q_lens, kv_lens, kv_starts=starts, causal=causal, window=window, kv_heads=kv_heads,
-             q_heads=group * kv_heads, units=r.choice((1, 16, 256, 100000)))
+             q_heads=group * kv_heads, head_dim=128 if seed >= 60 else 64,
+             units=1 + seed % 3 if seed >= 60 else r.choice((1, 16, 256, 100000)))
     h, tokens, items, joins = parts(p)
     assert h.bytes == p._host.numel() and h.tokens == sum(q_lens)
     kinds = items[:, 4].tolist()   # 0: 256 rows, 1: 128, 2: 32
@@ -116,7 +120,7 @@ def test_plan_covers_every_visible_pair_once(seed):
             part, k = joined[s, row0, rows]
             assert k == len(pieces) and [x[2] for x in pieces] == [part + i * rows
                                                                     for i in range(k)]
-    assert p.workspace_bytes >= h.part_rows * kv_heads * (64 * 4 + 8)
+    assert p.workspace_bytes >= h.part_rows * kv_heads * ((128 if seed >= 60 else 64) * 4 + 8)
     at = 0
     for s in range(n):
         for pos in range(kv_lens[s] - q_lens[s], kv_lens[s]):

@@ -373,6 +373,25 @@ ATTEND = [
 ]
 
 
+# enough rows and keys for a few units to be worth strips of 256 rows
+WIDE = [
+    ([300, 520], [2300, 2700], 4, 2, 128, 64, {"units": 1}),
+    ([600], [3100], 4, 2, 96, 16, {"units": 1, "window": 1100}),
+    ([400, 1], [2300, 50], 8, 2, 80, 32, {"units": 1}),
+    ([700], [1500], 4, 2, 128, 16, {"units": 1, "causal": False}),
+    ([520, 600, 300], [6000, 2600, 2600], 8, 2, 72, 16,
+     {"units": 1, "kv_starts": [333, 2600, 2590]}),                    # one sequence sees no key
+    ([260, 257], [1500, 1321], 4, 4, 128, 16, {"units": 1}),
+    ([1030], [2100], 1, 1, 128, 128, {"units": 1}),
+    ([200, 300], [150, 2900], 8, 2, 128, 64, {"units": 1}),            # tokens before the first key
+    ([300], [9000], 8, 2, 128, 64, {"units": 16}),                     # split over the keys
+]
+
+
+def wide_items(plan):
+    return int(plan._host.numpy()[72:76].view(np.int32)[0])   # n_wide of the plan's header
+
+
 def attend_case(spec, dtype, layout="heads", seed=4):
     """(q, caches, plan, keys and values in 64 bits per sequence); slots that hold no key, or one
     before the sequence's start, hold NaN."""
@@ -411,10 +430,11 @@ def attend_check(spec, q, kept, out, lse, scale, dtype):
 
 
 @pytest.mark.parametrize("dtype", [BF16, F16])
-@pytest.mark.parametrize("spec", ATTEND)
+@pytest.mark.parametrize("spec", ATTEND + WIDE)
 def test_attend(spec, dtype):
     say(f"[gpu] attend {spec} {dtype}")
     q, caches, plan, kept = attend_case(spec, dtype)
+    assert wide_items(plan) or spec not in WIDE
     out, lse = A.taps_attend(q, *caches, plan, lse=True)
     torch.cuda.synchronize()
     attend_check(spec, q, kept, out, lse, spec[4] ** -0.5, dtype)
@@ -489,6 +509,8 @@ def test_attend_many_small_numerators(dtype):
     ([300], [330], 4, 2, 128, 64, {"units": 1}),
     ([300], [700], 4, 2, 80, 16, {"units": 1, "window": 100}),
     ([40], [1500], 8, 2, 128, 64, {"units": 4096}),
+    ([300], [1700], 4, 2, 128, 64, {"units": 1}),            # 256 rows an item
+    ([300], [2900], 4, 2, 80, 16, {"units": 1, "window": 1500}),
 ])
 def test_attend_infinities_and_nans(spec, dtype):
     """Keys and values that are infinite or NaN, among the new tokens and before: they reach the
