@@ -134,10 +134,13 @@ struct Layout {
     taps_plan_header head{};
 };
 
-// Pieces shorter than this are not made: a split costs a launch and a pass
-// over partial results, some 5 us, in which a workgroup takes about this many
-// keys (one token over 1024 keys of 16 heads: 11.3 us whole, 13.7 in four).
-constexpr int64_t kLeastPiece = 1024;
+// Shorter pieces are not made: a split costs a launch and a pass over partial
+// results, some 5 us for few rows, in which a narrow item takes about this many
+// keys (one token over 1024 keys of 16 heads: 11.3 us whole, 13.7 in four) and a
+// block half as many (256 tokens over 1500, 16 heads of 64: 25.5 us whole, 19.5 so).
+constexpr int64_t kLeastNarrow = 1024, kLeastPiece = 512;
+
+int64_t least_piece(int32_t kind) { return kind == kNarrow ? kLeastNarrow : kLeastPiece; }
 
 // Query rows that share their keys' loads, before they are split over the keys.
 struct Strip {
@@ -148,7 +151,7 @@ struct Strip {
     // pieces of about `piece`: one 3 % above it is not cut again
     int64_t parts(int64_t piece) const {
         const int64_t n = (cost() + piece - 1 - piece / 32) / piece;
-        return std::max<int64_t>(1, std::min<int64_t>({n, (hi - lo) / kLeastPiece, 256}));
+        return std::max<int64_t>(1, std::min<int64_t>({n, (hi - lo) / least_piece(kind), 256}));
     }
     static int64_t cost_of(int32_t kind, int64_t keys) { return keys * (kind == kNarrow ? 2 : 1); }
 };
@@ -157,30 +160,47 @@ struct Strip {
 // their bytes set the time (two tokens over 131001 keys: 187 us, 192 at four).
 constexpr int64_t kNarrowPieces = 2;
 
-// The other kinds run in rounds: all pieces of a round take about the same
-// time, and a last round that few pieces share costs as much as a full one.
-// So the length of a piece, in keys, is the one of those below at which the
-// rounds, and what a piece costs beyond its keys, come to the least (512 tokens
-// over 32768 keys, 64 wide strips: 249 us as 256 pieces, 297 as 392 and 331 as
-// 528; 1024 over 20000: 295 as 256 pieces, 378 as 560).
-constexpr int64_t kPieceCost = 256; // a piece's start, end and join, in keys
-constexpr int64_t kMostRounds = 8;  // lengths are tried that come to 1/2, 3/4 .. 8 rounds
+// The other kinds: the length of a piece, in keys, is the one of those below at
+// which the step should end first.  Pieces of like length run in rounds over the
+// units, and a last round that few share costs as much as a full one; others,
+// dear ones first, fill the gaps.  Nothing ends before its longest piece.  Two
+// blocks on a unit take longer than one alone.
+//   512 tokens over 32768 keys, 64 wide strips: 249 us as 256 pieces, 297 as 392,
+//   331 as 528;
+//   4 prompts of 2048, 4 heads, 256 blocks: 49 us whole, 40 as 480 pieces;
+//   prompts of 700 and single tokens, 176 blocks: 26 us whole, 34 as 304 pieces.
+constexpr double kPieceCost = 256;   // a piece's start and end, in keys
+constexpr double kJoinCost = 600;    // the join's launch and pass, in keys
+constexpr double kCrowded = 1.6;     // a block's time beside another, by its time alone
+constexpr int64_t kMostRounds = 8;   // lengths are tried that come to 1/4, 1/2 .. 8 rounds
 
 int64_t share_of(int64_t total, int64_t times, int64_t among) {
     return (int64_t)std::min((double)total * (double)times / (double)among, 1e18) + 1;
 }
 
-int64_t piece_of(const std::vector<Strip> &strips, int32_t kind, int64_t slots, int64_t heads) {
-    int64_t total = 0;
-    for (const Strip &t : strips) total += t.kind == kind ? t.cost() : 0;
-    int64_t best = 1, least = INT64_MAX;
-    for (int64_t k = 2; k <= 4 * kMostRounds; ++k) {
-        const int64_t piece = std::max(share_of(total, 4 * heads, slots * k), kLeastPiece);
-        int64_t n = 0;
+int64_t piece_of(const std::vector<Strip> &strips, int32_t kind, int64_t cus, int64_t heads) {
+    const int64_t slots = kind == kWide ? cus : 2 * cus;
+    int64_t total = 0, all = 0;
+    for (const Strip &t : strips)
+        if (t.kind == kind) total += t.cost(), ++all;
+    int64_t best = 1;
+    double least = INFINITY;
+    for (int64_t k = 0; all && k <= 4 * kMostRounds; ++k) {   // at 0 nothing is cut
+        const int64_t share = k ? share_of(total, 4 * heads, slots * k) : total;
+        const int64_t piece = std::max(share, least_piece(kind));
+        int64_t n = 0, longest = 1;
         for (const Strip &t : strips)
-            if (t.kind == kind) n += t.parts(piece);
-        const int64_t rounds = (n * heads + slots - 1) / slots;
-        const int64_t cost = rounds * (total / std::max<int64_t>(n, 1) + kPieceCost);
+            if (t.kind == kind) {
+                const int64_t parts = t.parts(piece);
+                n += parts, longest = std::max(longest, t.cost() / parts);
+            }
+        const bool crowded = kind == kBlock && n * heads > cus;
+        const double mean = (double)total / n, rounds = (double)((n * heads + slots - 1) / slots);
+        const double span = std::max<double>(
+            longest, std::min(rounds * longest,
+                              (double)n * heads / slots * mean + mean * mean / longest));
+        const double cost = (crowded ? kCrowded : 1) * span + rounds * kPieceCost +
+                            (n > all ? kJoinCost : 0);
         if (cost < least) least = cost, best = piece;
     }
     return best;
@@ -247,7 +267,7 @@ bool wide_pays(const taps_paged_batch *b, const std::vector<Sequence> &seqs, int
         int64_t seen = b->causal ? kv - (q.kv_len - q.first_pos) / 2 : kv;   // on average
         if (window) seen = std::min(seen, window);
         strips += n, keys += n * seen;
-        pieces += n * std::max<int64_t>(1, kv / kLeastPiece);
+        pieces += n * std::max<int64_t>(1, kv / kWideKeysSeen);
     }
     return b->head_dim > kWideAbove && keys >= kWideKeysSeen * strips &&
            pieces * b->kv_heads >= kWideRounds * cus;
@@ -331,7 +351,7 @@ taps_status lay_out(const taps_paged_batch *b, uint32_t cus, Layout *out) {
     const int64_t heads = b->kv_heads;
     const int64_t narrow = share_of(total, heads, cus * kNarrowPieces);
     const int64_t wides = piece_of(strips, kWide, cus, heads);
-    const int64_t blocks = piece_of(strips, kBlock, 2 * (int64_t)cus, heads);
+    const int64_t blocks = piece_of(strips, kBlock, cus, heads);
     uint64_t part_rows = 0;
     for (const Strip &t : strips) {
         int64_t parts = t.parts(t.kind == kNarrow ? narrow : t.kind == kBlock ? blocks : wides);

@@ -65,9 +65,10 @@ struct taps_plan_join {
     int32_t reserved[2];
 };
 
-// Groups of lanes that share a row's pieces in k_join: 1, 2, 4 or 8 of a workgroup's 8.
+// Groups of lanes of a workgroup's 8 that share a row's pieces in k_join, which
+// takes four of a group's at once.
 __host__ __device__ inline int taps_join_across(int parts) {
-    return parts <= 1 ? 1 : parts <= 2 ? 2 : parts <= 4 ? 4 : 8;
+    return parts <= 4 ? 1 : parts <= 8 ? 2 : parts <= 16 ? 4 : 8;
 }
 
 // ---------------------------------------------------------------------------
