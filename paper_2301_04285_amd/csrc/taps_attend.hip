@@ -564,7 +564,7 @@ template <int D> struct Loader {
 // have a wavefront of their own at any time and a tile's loads serve twice the
 // rows of a block item.
 // Bound by the matrix cores at the clocks that they leave (some 1.8 of 2.4 GHz): 512
-// tokens over 32768 keys, 32 heads of 128 over 8, 247 us here, 1110 TFLOP/s (279 in
+// tokens over 32768 keys, 32 heads of 128 over 8, 243 us here, 1120 TFLOP/s (279 in
 // blocks); eight sequences of 2048 tokens, 32 heads, not causal, take 0.21 us a
 // key, 1280 TFLOP/s, and 90 us besides, for starting, reading queries and writing
 // results eight times on every unit.  One workgroup a unit that loads its next
