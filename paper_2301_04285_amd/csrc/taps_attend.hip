@@ -563,9 +563,11 @@ template <int D> struct Loader {
 // are in one of them, the others are in the other, so that the matrix cores
 // have a wavefront of their own at any time and a tile's loads serve twice the
 // rows of a block item.
-// Bound by the matrix cores at the clocks that they leave (some 1.8 of 2.4 GHz): 512
-// tokens over 32768 keys, 32 heads of 128 over 8, 243 us here, 1120 TFLOP/s (279 in
-// blocks); eight sequences of 2048 tokens, 32 heads, not causal, take 0.21 us a
+// 512 tokens over 32768 keys, 32 heads of 128 over 8: 243 us here, 1120 TFLOP/s (279
+// in blocks), the matrix cores busy for 55 % of the cycles at 1.9 GHz; the phases that
+// wait for each other take the rest.  The products alone, without loads, softmax and
+// reads of LDS, reach 1377 at the clocks that they leave, so a fifth is the most
+// there is to win.  Eight sequences of 2048 tokens, 32 heads, not causal, take 0.21 us a
 // key, 1280 TFLOP/s, and 90 us besides, for starting, reading queries and writing
 // results eight times on every unit.  One workgroup a unit that loads its next
 // item's tiles and queries while it ends the last takes no less (364 and 360 us).
