@@ -88,7 +88,7 @@ typedef struct {
  * overlap nothing.  first_position .. first_position + tokens - 1 must be
  * rows of the table (TAPS_ERR_ARG); a value of `positions` that is not one
  * makes that token's outputs NaN (in the gradients: those of its inputs and
- * of the weights). */
+ * of the weights); a table without rows is refused (TAPS_ERR_ARG). */
 taps_status taps_norm_rotate(const taps_norm_rotate_args *args, const taps_heads *q,
                              const taps_heads *k, const taps_heads *q_out, const taps_heads *k_out,
                              void *stream);

@@ -89,6 +89,9 @@ taps_status check_norm_rotate(const taps_norm_rotate_args *a, taps_rows_launch *
             return fail(TAPS_ERR_ARG, "position_bytes %u is neither 4 nor 8", a->position_bytes);
         if (!aligned(a->positions, a->position_bytes))
             return fail(TAPS_ERR_ARG, "positions is not aligned to its elements");
+        // the kernels read row 0 for a position that is no row of the table
+        if (a->rotary_dim && a->batch && a->tokens && !a->n_positions)
+            return fail(TAPS_ERR_ARG, "the table has no rows for positions");
     } else if (a->rotary_dim && a->batch && a->tokens &&
                (a->first_position < 0 || a->first_position > (int64_t)a->n_positions ||
                 a->tokens > a->n_positions - (uint64_t)a->first_position)) {
