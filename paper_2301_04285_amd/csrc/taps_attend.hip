@@ -689,6 +689,8 @@ __device__ __forceinline__ void attend_block(const taps_attend_launch &p, const 
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int32_t *pages = p.pages + item.page0;
     const int start = item.lo & ~15;
+    // no tile of an item without keys: its lo need not be a multiple of 16
+    const int hi = item.lo < item.hi ? item.hi : start;
     const float c = p.scale * kLog2e;
     const int row0 = item.row0 + 32 * wave, row = row0 + (lane & 31);
     Rows<T, D> rows;
@@ -697,7 +699,7 @@ __device__ __forceinline__ void attend_block(const taps_attend_launch &p, const 
     const Loader<D> k(p, item, head, false, wave, lane), v(p, item, head, true, wave, lane);
     const auto page_of = [&](int t0) { return page_at(p, pages, t0 + k.key0, item.lo, item.hi); };
     int page = 0, buffer = 0;
-    if (item.lo < item.hi) {
+    if (start < hi) {
         page = page_of(start);
         k.load(start, page, lds);
         v.load(start, page, lds + kPart);
@@ -710,13 +712,13 @@ __device__ __forceinline__ void attend_block(const taps_attend_launch &p, const 
         const char *next = lds + 2 * (buffer ^ 1) * kPart;
         wait_loads<0>();
         __syncthreads();
-        if (t0 + kWideKeys < item.hi) {
+        if (t0 + kWideKeys < hi) {
             k.load(t0 + kWideKeys, page, next);
             v.load(t0 + kWideKeys, page, next + kPart);
             page = page_of(t0 + 2 * kWideKeys);
         }
     };
-    for (; t0 < min(item.hi, seen.end); t0 += kWideKeys, buffer ^= 1) {
+    for (; t0 < min(hi, seen.end); t0 += kWideKeys, buffer ^= 1) {
         const char *tile = lds + 2 * buffer * kPart;
         begin();
         typename Rows<T, D>::template Scores<kWideKeys> x;
@@ -725,7 +727,7 @@ __device__ __forceinline__ void attend_block(const taps_attend_launch &p, const 
         rows.soften(x, y, t0, seen.masks(t0, kWideKeys), c, lane);
         rows.spend(tile + kPart, y, lane);
     }
-    for (; t0 < item.hi; t0 += kWideKeys, buffer ^= 1) begin();   // the other wavefronts' tiles
+    for (; t0 < hi; t0 += kWideKeys, buffer ^= 1) begin();   // the other wavefronts' tiles
     finish(p, item, head, rows, row, lane);
 }
 
