@@ -19,8 +19,8 @@
 // pairs of every row it takes: `a` members in one chunk, `b` members in
 // another, so that the rotation needs no other lane, and the table's entries and
 // the weights are read once per token and kept.  Elements that are not rotated
-// form pairs of their own with cosine 1 and sine 0.  The norm's sum is the only
-// thing that crosses lanes.
+// are held in pairs too, but each stays as it is: a product with a sine of 0
+// would hand on infinities.  The norm's sum is the only thing that crosses lanes.
 #include "taps_attention_internal.h"
 #include "taps_lanes.h"
 
@@ -62,7 +62,7 @@ template <> struct Pairs<true> {
             b0 = a0 + p.rotary / 2;
         }
     }
-    __device__ __forceinline__ bool has(int) const { return live; }
+    __device__ __forceinline__ bool turns(int) const { return rotated; }
     template <class T> struct Raw {
         typedef T v4 __attribute__((ext_vector_type(4)));
         v4 u = {}, v = {};
@@ -139,6 +139,7 @@ template <> struct Pairs<false> {
             if (ib[i] >= (int)p.dim) ib[i] = -1;
         }
     }
+    __device__ __forceinline__ bool turns(int i) const { return ang[i] >= 0; }
     template <class T> struct Raw {
         T a[kN], b[kN];
     };
@@ -256,8 +257,8 @@ __global__ __launch_bounds__(kThreads) void k_norm_rotate(taps_rows_launch p) {
             for (int i = 0; i < N; ++i) {
                 const float na = a[i] * rstd * (side ? wa[1][i] : wa[0][i]);
                 const float nb = bb[i] * rstd * (side ? wb[1][i] : wb[0][i]);
-                a[i] = na * c[i] - nb * s[i];
-                bb[i] = nb * c[i] + na * s[i];
+                a[i] = pairs.turns(i) ? na * c[i] - nb * s[i] : na;
+                bb[i] = pairs.turns(i) ? nb * c[i] + na * s[i] : nb;
             }
             // a position off the table: what is not rotated is NaN too
             if (!good)
@@ -310,8 +311,8 @@ __global__ __launch_bounds__(kThreads) void k_append(taps_rows_launch p) {
                 }
                 for (int i = 0; i < N; ++i) {
                     const float na = a[i] * rstd * wa[i], nb = b[i] * rstd * wb[i];
-                    a[i] = na * c[i] - nb * s[i];
-                    b[i] = nb * c[i] + na * s[i];
+                    a[i] = pairs.turns(i) ? na * c[i] - nb * s[i] : na;
+                    b[i] = pairs.turns(i) ? nb * c[i] + na * s[i] : nb;
                 }
             }
             pairs.store((T *)p.dst[side] + page * p.dst_stride[side][0] +
@@ -364,9 +365,10 @@ __global__ __launch_bounds__(kThreads) void k_norm_rotate_backward(taps_rows_lau
                 pairs.unpack(raw_g[u], ya, yb);
                 pairs.unpack(raw_x[u], a, bb);
                 for (int i = 0; i < N; ++i) {   // h = R^T g
-                    const float v = ya[i] * c[i] + yb[i] * s[i];
-                    yb[i] = yb[i] * c[i] - ya[i] * s[i];
-                    ya[i] = v;
+                    const float va = ya[i] * c[i] + yb[i] * s[i];
+                    const float vb = yb[i] * c[i] - ya[i] * s[i];
+                    ya[i] = pairs.turns(i) ? va : ya[i];
+                    yb[i] = pairs.turns(i) ? vb : yb[i];
                 }
                 if (!good)
                     for (int i = 0; i < N; ++i) ya[i] = yb[i] = __builtin_nanf("");

@@ -70,3 +70,96 @@ def test_tokens_without_keys_and_many_heads(dim, causal):
         assert A.taps_attend(sq, nans, nans, spoil).isnan().all()
         out, lse = A.taps_attend(q, nans, nans, plan, lse=True)
         assert (out == 0).all() and (lse == -math.inf).all()
+
+
+# ---------------------------------------------------------------------------
+# elements that are not rotated
+# ---------------------------------------------------------------------------
+
+def same_specials(got, want, bound, what):
+    """Infinite and NaN where the definition is, finite elsewhere and within the bound."""
+    got = R.f64(got)
+    odd = ~np.isfinite(want)
+    assert np.array_equal(np.where(odd, got, 0), np.where(odd, want, 0), equal_nan=True), what
+    R.check(np.where(odd, 0, got), np.where(odd, 0, want), np.where(odd, 0, bound), what)
+
+
+PARTS = [   # dim, rotary, interleaved: by fours of elements, and element by element
+    (128, 64, False), (128, 64, True), (96, 48, True), (64, 0, False), (8, 0, False),
+    (36, 18, False), (37, 10, True), (101, 50, False), (7, 0, False), (256, 2, True),
+]
+
+
+def with_specials(x, rotary):
+    """Every unrotated element in turn, and sign, has an infinity or a NaN in some row."""
+    dim = x.shape[-1]
+    rows = x.view(-1, dim)
+    values = (math.inf, -math.inf, math.nan)
+    for r in range(min(len(rows), dim - rotary)):
+        rows[r, rotary + (r * 5 + 1) % (dim - rotary)] = values[r % 3]
+    return x
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("spec", PARTS)
+def test_unrotated_elements_stay(spec, dtype):
+    """An infinite or NaN element that is not rotated reaches no other element of its head,
+    forwards, backwards and on the way to a cache; without a rotation and a norm keys are
+    copied."""
+    dim, rotary, interleaved = spec
+    say(f"[gpu] unrotated {spec} {dtype}")
+    tokens, heads = 40, 3
+    g = gen_of(21)
+    x = with_specials(randn(g, 1, tokens, heads, dim, dtype=dtype), rotary)
+    table = A.rotation_table(tokens, rotary) if rotary else None
+    cos, sin = np.zeros((1, tokens, 0)), np.zeros((1, tokens, 0))
+    if rotary:
+        cos, sin = (R.f64(table)[None, :, i] for i in range(2))
+    y, bound = R.norm_rotate(R.f64(x), None, cos, sin, interleaved, 1e-6, dtype)
+    out, _ = A.taps_norm_rotate(x, None, None, None, table, interleaved=interleaved)
+    same_specials(out, y, bound, "output")
+    dx, b, _, _ = R.norm_rotate_gradients(R.f64(x), R.f64(x), None, cos, sin, interleaved, 1e-6,
+                                          dtype, None)
+    grads = A.taps_norm_rotate_backward(x, None, x, None, None, None, table,
+                                        interleaved=interleaved)
+    same_specials(grads[0], dx, b, "gradient")
+    page = 16
+    caches = [torch.zeros(3, heads, page, dim, dtype=dtype, device="cuda") for _ in range(2)]
+    plan = A.PagedPlan([tokens], [tokens], [[2, 0, 1]], n_pages=3, page_size=page, q_heads=heads,
+                       kv_heads=heads, head_dim=dim)
+    A.taps_cache_append(x[0], x[0], *caches, plan, table=table, interleaved=interleaved)
+    left = [c[[2, 0, 1]].transpose(1, 2).flatten(0, 1)[:tokens] for c in caches]
+    same_specials(left[0], y[0], bound[0], "key")
+    assert np.array_equal(R.f64(left[1]), R.f64(x[0]), equal_nan=True)
+    if not rotary:
+        assert np.array_equal(R.f64(left[0]), R.f64(x[0]), equal_nan=True)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("spec", PARTS[:3] + PARTS[5:8])
+def test_unrotated_elements_stay_with_a_norm(spec, dtype):
+    """The norm of a row with an infinity is infinite: that element becomes NaN and its
+    neighbours 0.  An infinite gradient reaches its own element's weight gradient alone."""
+    dim, rotary, interleaved = spec
+    say(f"[gpu] unrotated, normed {spec} {dtype}")
+    g = gen_of(22)
+    x = randn(g, 1, 5, 2, dim, dtype=dtype)
+    grad = randn(g, 1, 5, 2, dim, dtype=dtype)
+    w = (1 + 0.3 * torch.randn(dim, generator=g)).to(dtype).cuda()
+    table = A.rotation_table(5, rotary)
+    cos, sin = (R.f64(table)[None, :, i] for i in range(2))
+    bad = x.clone()
+    bad[0, 2, 1, rotary + 1] = math.inf
+    with np.errstate(invalid="ignore"):
+        y, bound = R.norm_rotate(R.f64(bad), R.f64(w), cos, sin, interleaved, 1e-6, dtype)
+    out, _ = A.taps_norm_rotate(bad, None, w, None, table, interleaved=interleaved)
+    same_specials(out, y, np.nan_to_num(bound), "output")
+    grad[0, 3, 0, rotary + 2] = -math.inf
+    grad[0, 4, 1, dim - 1] = math.inf
+    with np.errstate(invalid="ignore"):
+        _, _, dw, bw = R.norm_rotate_gradients(R.f64(grad), R.f64(x), R.f64(w), cos, sin,
+                                               interleaved, 1e-6, dtype, dtype)
+    got = A.taps_norm_rotate_backward(grad, None, x, None, w, None, table,
+                                      interleaved=interleaved)[2]
+    assert np.isinf(dw).sum() == 2
+    same_specials(got, dw, bw, "weight gradient")
