@@ -36,10 +36,20 @@ namespace {
 constexpr int kThreads = 256, kWaves = 4, kWideThreads = 2 * kWideRows;
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 constexpr float kMinusInf = -__builtin_inff();
+// Numerators are held as kLift exp(scale q.k - m), sums of them too; it cancels.
+// fp16 has its smallest normal number at 2^-14 and nothing below 2^-25, so there
+// the maximum's is placed at 2^10: keys that far below it still count, where many of
+// them together outweigh it.  bf16 has the exponents of 32 bits.
 // A row's maximum is raised only when a tile's numerators (this lane's 16 or 32)
-// add up to more than this: none exceeds it, far inside every type's range, and
-// most tiles neither look for their maximum nor touch the accumulators.
-constexpr float kMostSum = 4096.f;
+// add up to more than kMostSum: none exceeds it, inside the type's range, equal
+// ones do not reach it, and most tiles neither look for their maximum nor touch
+// the accumulators.
+template <class T> constexpr float kLift = 1.f;
+template <class T> constexpr float kLiftLog2 = 0.f;
+template <class T> constexpr float kMostSum = 4096.f;
+template <> constexpr float kLift<_Float16> = 1024.f;
+template <> constexpr float kLiftLog2<_Float16> = 10.f;
+template <> constexpr float kMostSum<_Float16> = 61440.f;
 
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
@@ -262,8 +272,8 @@ template <class T, int D> struct Rows {
                     x.s[n][i] = at + (32 * n + 8 * (i / 4) + i % 4) < seen ? x.s[n][i] : kMinusInf;
         }
         float sum = numerators(x, y, c);
-        // the first keys, and scores above the maximum by kSlack or more
-        if (__any(m == kMinusInf || sum > kMostSum)) {
+        // the first keys, and scores too far above the maximum
+        if (__any(m == kMinusInf || sum > kMostSum<T>)) {
             float most = x.s[0][0];
 #pragma unroll
             for (int n = 0; n < Keys / 32; ++n)
@@ -282,12 +292,13 @@ template <class T, int D> struct Rows {
         l += sum;
     }
     // They are rounded for the product with the values, which takes operands of the
-    // cache's type only: an error of 2^-9 (bf16) or 2^-12 of each, independent of each
-    // other and no larger than the values' own.  Their sum is taken before, in 32 bits.
+    // cache's type only: an error of up to 2^-8 (bf16) or 2^-11 of each, independent of
+    // each other and no larger than the values' own, and in fp16 of 2^-35 of the largest
+    // for those below 2^-24 of it.  Their sum is taken before, in 32 bits.
     template <int Keys>
     __device__ __forceinline__ float numerators(const Scores<Keys> &x, Numerators<Keys> &y,
                                                 float c) const {
-        const float shift = m == kMinusInf ? 0.f : m * c;
+        const float shift = m == kMinusInf ? 0.f : m * c - kLiftLog2<T>;
         float sum[2] = {0.f, 0.f};
 #pragma unroll
         for (int n = 0; n < Keys / 32; ++n)
@@ -384,12 +395,13 @@ __device__ __forceinline__ char *out_row(const taps_attend_launch &p, const taps
            (int64_t)(head * p.group + sub) * p.o_head;
 }
 
+template <class T>
 __device__ __forceinline__ void store_lse(const taps_attend_launch &p, const taps_plan_item &s,
                                           uint32_t head, int row, float m, float l) {
     if (!p.lse) return;
     const int token = row / (int)p.group, sub = row - token * (int)p.group;
     p.lse[(int64_t)(s.token0 + token) * p.q_heads + head * p.group + sub] =
-        l == 0.f ? kMinusInf : m * p.scale + __builtin_amdgcn_logf(l) * kLn2;
+        l == 0.f ? kMinusInf : m * p.scale + __builtin_amdgcn_logf(l / kLift<T>) * kLn2;
 }
 
 // A row's result once more, by all lanes of a wavefront with two columns each:
@@ -408,7 +420,7 @@ __device__ __forceinline__ void redo_row(const taps_attend_launch &p, const taps
         if (p.window) first = max(first, pos - (int)p.window + 1);
     }
     const bool live = d < (int)p.dim;
-    const float c = p.scale * kLog2e, shift = m == kMinusInf ? 0.f : m * c;
+    const float c = p.scale * kLog2e, shift = m == kMinusInf ? 0.f : m * c - kLiftLog2<T>;
     v2 q = {};
     if (live)
         q = *(const v2 *)(p.q + (int64_t)(item.token0 + token) * p.q_token +
@@ -430,7 +442,7 @@ __device__ __forceinline__ void redo_row(const taps_attend_launch &p, const taps
     if (item.part < 0) {
         const float inv = l == 0.f ? 0.f : 1.f / l;
         *(uint32_t *)(out_row<T>(p, item, head, row) + 2 * d) = pack2<T>(o[0] * inv, o[1] * inv);
-        if (d == 0) store_lse(p, item, head, row, m, l);
+        if (d == 0) store_lse<T>(p, item, head, row, m, l);
     } else {
         const int64_t at = (int64_t)(item.part + row - item.row0) * p.kv_heads + head;
         p.part_o[at * p.dim + d] = o[0], p.part_o[at * p.dim + d + 1] = o[1];
@@ -455,7 +467,7 @@ __device__ __forceinline__ void write_rows(const taps_attend_launch &p, const ta
                                  pack2<T>(rows.o[b][4 * i + 2] * inv, rows.o[b][4 * i + 3] * inv)};
                 if (d < (int)p.dim) *(u32x2 *)(out + 2 * d) = v;
             }
-        if (half == 0) store_lse(p, item, head, row, rows.m, l);
+        if (half == 0) store_lse<T>(p, item, head, row, rows.m, l);
     } else {
         const int64_t at = (int64_t)(item.part + row - item.row0) * p.kv_heads + head;
 #pragma unroll
@@ -886,7 +898,7 @@ __device__ __forceinline__ void attend_narrow(const taps_attend_launch &p,
             char *out = out_row<T>(p, item, head, item.row0 + r);
             const u32x2 v = {pack2<T>(o[0] * inv, o[1] * inv), pack2<T>(o[2] * inv, o[3] * inv)};
             *(u32x2 *)(out + 2 * d) = v;
-            if (d == 0) store_lse(p, item, head, item.row0 + r, top, l);
+            if (d == 0) store_lse<T>(p, item, head, item.row0 + r, top, l);
         } else {
             const int64_t at = (int64_t)(item.part + r) * p.kv_heads + head;
             *(f32x4 *)(p.part_o + at * p.dim + d) = o;
@@ -984,7 +996,7 @@ __global__ __launch_bounds__(kThreads) void k_join(taps_attend_launch p) {
         const u32x2 v = {pack2<T>(o[0] * inv, o[1] * inv), pack2<T>(o[2] * inv, o[3] * inv)};
         *(u32x2 *)(out + 2 * d) = v;
     }
-    if (d == 0) store_lse(p, item, head, join.row0 + r, m, l);
+    if (d == 0) store_lse<T>(p, item, head, join.row0 + r, m, l);
 }
 
 template <class T, int D> void launch_items(const taps_attend_launch &p, hipStream_t stream) {

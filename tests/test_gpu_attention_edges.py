@@ -163,3 +163,61 @@ def test_unrotated_elements_stay_with_a_norm(spec, dtype):
                                       interleaved=interleaved)[2]
     assert np.isinf(dw).sum() == 2
     same_specials(got, dw, bw, "weight gradient")
+
+
+# ---------------------------------------------------------------------------
+# weights far below a row's largest
+# ---------------------------------------------------------------------------
+
+@pytest.mark.parametrize("dtype", [BF16, F16])
+@pytest.mark.parametrize("spec", [
+    # tokens, keys, dim, where the largest weight is
+    (1, 1500, 64, 0), (1, 1500, 128, 1499), (3, 1500, 96, 700), (40, 1500, 64, 0),
+    (40, 1500, 128, 300), (300, 2300, 128, 0),   # the last in strips of 256 rows
+])
+def test_weights_far_below_the_largest(spec, dtype):
+    """One key whose value is 0 above thousands that lie e^-17 to e^-20 below: the result is
+    theirs.  Numerators of 16 bits reach 35 binary places below the largest."""
+    new, n, dim, at = spec
+    say(f"[gpu] attend far below {spec} {dtype}")
+    g = gen_of(31)
+    k = torch.zeros(n, 1, dim, dtype=dtype)
+    k[:, 0, 0] = -17 - 0.25 * torch.randint(0, 13, (n,), generator=g).to(dtype)
+    v = (1 + 0.25 * torch.randn(n, 1, dim, generator=g)).to(dtype)
+    k[at], v[at] = 0, 0
+    q = torch.zeros(new, 2, dim, dtype=dtype)
+    q[:, :, 0] = 8
+    pages = np.arange(-(-n // 16))[None]
+    plan = A.PagedPlan([new], [n], pages, n_pages=pages.size, page_size=16, q_heads=2, kv_heads=1,
+                       head_dim=dim, units=1)
+    out, lse = A.taps_attend(q.cuda(), paged(k, 16), paged(v, 16), plan, scale=0.125, lse=True)
+    want, bound, w_lse, b_lse = R.attend(R.f64(q), R.f64(k), R.f64(v), n - new, 0, True, 0, 0.125,
+                                         dtype)
+    if dtype is F16:
+        # that bound counts half a step of the smallest numbers, 2^-25, for every numerator, with
+        # the largest at 1; at 2^10 they are 2^10 times as many steps, and all else stays
+        seen = np.cumsum(np.abs(R.f64(v)), axis=0)[n - new:]   # by each token
+        bound = bound - (1 + R.ROUND[F16]) * 2.0 ** -25 * (1 - 2.0 ** -10) * seen
+        assert (bound > 0).all() and (bound < 0.05 * want).all()
+    R.check(out, want, bound, "result")
+    R.check(lse, w_lse, b_lse, "lse")
+
+
+@pytest.mark.parametrize("new", [1, 40, 300])
+def test_equal_weights_and_large_values(new):
+    """Nothing overflows where all numerators are as large as any, nor where scores rise slowly."""
+    n, dim = 3000, 128
+    for rise in (0.0, 0.004, 0.03):   # of a score, from key to key
+        k = torch.zeros(n, 1, dim, dtype=F16)
+        k[:, 0, 0] = torch.arange(n) * rise
+        v = torch.full((n, 1, dim), 60000.0, dtype=F16)
+        q = torch.zeros(new, 1, dim, dtype=F16)
+        q[:, 0, 0] = 8
+        pages = np.arange(-(-n // 16))[None]
+        plan = A.PagedPlan([new], [n], pages, n_pages=pages.size, page_size=16, q_heads=1,
+                           kv_heads=1, head_dim=dim, units=1)
+        out, lse = A.taps_attend(q.cuda(), paged(k, 16), paged(v, 16), plan, scale=0.125, lse=True)
+        want, bound, w_lse, b_lse = R.attend(R.f64(q), R.f64(k), R.f64(v), n - new, 0, True, 0,
+                                             0.125, F16)
+        R.check(out, want, bound, f"rise {rise}")
+        R.check(lse, w_lse, b_lse, f"lse, rise {rise}")
