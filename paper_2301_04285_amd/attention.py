@@ -317,7 +317,7 @@ _function = None
 def norm_rotate(q, k, q_weight, k_weight, table, positions=None, first=0, eps=1e-6,
                 interleaved=False):
     """``taps_norm_rotate`` for torch's autograd: gradients of q, k and the
-    weights come from ``taps_norm_rotate_backward``."""
+    weights come from ``taps_norm_rotate_backward``; they have none of their own."""
     global _function
     if _function is None:
         class NormRotate(torch.autograd.Function):
@@ -329,6 +329,7 @@ def norm_rotate(q, k, q_weight, k_weight, table, positions=None, first=0, eps=1e
                 return taps_norm_rotate(q, k, q_weight, k_weight, table, positions, **how)
 
             @staticmethod
+            @torch.autograd.function.once_differentiable
             def backward(ctx, dq_out, dk_out):
                 q, k, q_weight, k_weight, table, positions = ctx.saved_tensors
 

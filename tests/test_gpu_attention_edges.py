@@ -221,3 +221,22 @@ def test_equal_weights_and_large_values(new):
                                              0.125, F16)
         R.check(out, want, bound, f"rise {rise}")
         R.check(lse, w_lse, b_lse, f"lse, rise {rise}")
+
+
+# ---------------------------------------------------------------------------
+# gradients
+# ---------------------------------------------------------------------------
+
+def test_gradients_of_gradients_raise():
+    """They are not computed; a penalty on a gradient must not lose its term silently."""
+    g = gen_of(41)
+    q = randn(g, 1, 5, 2, 64, dtype=F32).requires_grad_()
+    w = randn(g, 64, dtype=F32).requires_grad_()
+    table = A.rotation_table(5, 64)
+    out, _ = A.norm_rotate(q, None, w, None, table)
+    (first,) = torch.autograd.grad(out.square().sum(), q, create_graph=True)
+    with pytest.raises(RuntimeError, match="once_differentiable"):
+        first.square().sum().backward()
+    out, _ = A.norm_rotate(q, None, w, None, table)
+    (same,) = torch.autograd.grad(out.square().sum(), q)
+    assert torch.equal(first, same) and not same.requires_grad
