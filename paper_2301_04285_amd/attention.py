@@ -11,7 +11,9 @@ operators that run one device's share of an attention block.
 Argument marshalling only: every step runs in ``libtaps_attention.so``.  If
 the library is missing the calls raise -- there is no other implementation to
 fall back to.  Outputs and workspaces come from torch's allocator, on the
-stream that the call runs on (``stream``, or the current one).
+stream that the call runs on (``stream``, or the current one).  Torch's autograd
+follows ``norm_rotate`` alone: a backward pass through the new outputs of another
+call raises, and what a call writes to tensors it is given has no history.
 """
 from __future__ import annotations
 
@@ -195,6 +197,28 @@ def _on(stream, make):
         return make()
 
 
+class _NoGradient(torch.autograd.Function):
+    """Hands on the outputs of a call as a function of its inputs that has no gradient."""
+
+    @staticmethod
+    def forward(ctx, said, outputs, *inputs):
+        ctx.said = said
+        return outputs
+
+    @staticmethod
+    def backward(ctx, *grads):
+        raise RuntimeError(ctx.said)
+
+
+def _no_gradient(said: str, outputs, inputs):
+    """``outputs``, which raise in a backward pass if one of the inputs asks for it: left without
+    a history they would pass for constants there."""
+    for t in inputs:
+        if t is not None and t.requires_grad and torch.is_grad_enabled():
+            return _NoGradient.apply(said, outputs, *inputs)
+    return outputs
+
+
 def rotation_table(n_positions: int, rotary_dim: int, base: float = 10000.0, device="cuda"):
     """Cosines and sines of position x base^(-2 i / rotary_dim) as a 32-bit tensor
     [n_positions, 2, rotary_dim // 2], angles computed in 64 bits."""
@@ -266,14 +290,16 @@ def taps_norm_rotate(q, k, q_weight, k_weight, table, positions=None, first=0, e
     rank = len(shape)
     kh = None if k is None else _heads(k, "k", device, dtype, k.shape, rank)
     qh = _heads(q, "q", device, dtype, shape, rank)
-    if out is None:   # dense even where q and k are slices of one projection
-        out = _on(stream, lambda: (_like(q), None if k is None else _like(k)))
-    q_out, k_out = out
+    q_out, k_out = out if out is not None else \
+        _on(stream, lambda: (_like(q), None if k is None else _like(k)))   # dense, of slices too
     _check(load().taps_norm_rotate(
         C.byref(args), qh, kh, _heads(q_out, "out[0]", device, dtype, shape, rank),
         None if k is None else _heads(k_out, "out[1]", device, dtype, k.shape, rank),
         _stream(stream)), "taps_norm_rotate")
-    return q_out, k_out
+    if out is not None:
+        return q_out, k_out
+    return _no_gradient("taps_norm_rotate has no gradient: call norm_rotate", (q_out, k_out),
+                        (q, k, q_weight, k_weight))
 
 
 def taps_norm_rotate_backward(dq_out, dk_out, q, k, q_weight, k_weight, table, positions=None,
@@ -488,6 +514,7 @@ def taps_attend(q, k_cache, v_cache, plan: PagedPlan, scale=None, out=None, lse=
     vh = _cache(v_cache, "v_cache", plan, device, dtype)
     n = plan.workspace_bytes
     sums = workspace = None
+    given = out
     if out is None:
         out = _on(stream, lambda: _like(q))
     if lse:
@@ -500,4 +527,6 @@ def taps_attend(q, k_cache, v_cache, plan: PagedPlan, scale=None, out=None, lse=
         _heads(out, "out", device, dtype, shape, 3),
         None if sums is None else sums.data_ptr(),
         None if workspace is None else workspace.data_ptr(), n, raw), "taps_attend")
+    if given is None:
+        out, sums = _no_gradient("taps_attend has no gradient", (out, sums), (q, k_cache, v_cache))
     return (out, sums) if lse else out

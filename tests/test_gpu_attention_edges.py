@@ -240,3 +240,35 @@ def test_gradients_of_gradients_raise():
     out, _ = A.norm_rotate(q, None, w, None, table)
     (same,) = torch.autograd.grad(out.square().sum(), q)
     assert torch.equal(first, same) and not same.requires_grad
+
+
+def test_calls_without_a_gradient_say_so():
+    g = gen_of(42)
+    q, k = (randn(g, 5, 2, 64) for _ in range(2))
+    w = randn(g, 64)
+    table = A.rotation_table(5, 64)
+    cache = randn(g, 1, 2, 16, 64)
+    plan = A.PagedPlan([5], [5], [[0]], n_pages=1, page_size=16, q_heads=2, kv_heads=2, head_dim=64)
+    want = A.taps_norm_rotate(q, k, w, w, table)
+    want_out, want_lse = A.taps_attend(q, cache, cache, plan, lse=True)
+    assert not any(t.requires_grad for t in (*want, want_out, want_lse))
+    for which in range(3):
+        args = [q.clone(), k.clone(), w.clone()]
+        args[which].requires_grad_()
+        for t, x in zip(A.taps_norm_rotate(*args, w, table), want):
+            assert torch.equal(t, x)
+            with pytest.raises(RuntimeError, match="call norm_rotate"):
+                t.sum().backward()
+        with torch.no_grad():
+            assert not any(t.requires_grad for t in A.taps_norm_rotate(*args, w, table))
+    for which in range(3):
+        args = [q.clone(), cache.clone(), cache.clone()]
+        args[which].requires_grad_()
+        out, lse = A.taps_attend(*args, plan, lse=True)
+        assert torch.equal(out, want_out) and torch.equal(lse, want_lse)
+        for t in (out, lse, A.taps_attend(*args, plan)):
+            with pytest.raises(RuntimeError, match="taps_attend has no gradient"):
+                t.sum().backward()
+        mine = torch.empty_like(q)
+        assert A.taps_attend(*args, plan, out=mine) is mine and not mine.requires_grad
+        assert torch.equal(mine, want_out)
