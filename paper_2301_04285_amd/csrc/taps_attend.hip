@@ -125,7 +125,7 @@ template <int D> struct Tile {
 constexpr int max_of(int a, int b) { return a > b ? a : b; }
 template <int D> constexpr int narrow_bytes() {
     return max_of(kWaves * Tile<D>::bytes(kNarrowKeys), kWaves * kNarrowRows * (D + 4) * 4) +
-           kWaves * kNarrowRows * 2 * 4 + kNarrowRows * 4;
+           kWaves * kNarrowRows * 2 * 4;
 }
 
 // The LDS address of a generic pointer to LDS.
@@ -256,21 +256,24 @@ template <class T, int D> struct Rows {
         }
     }
 
-    // Hides the keys this row does not see (t0: the first key's number) and
-    // makes the numerators from the maximum as it is; only where their sum shows
-    // that it lies too far below a score is it raised and are they made anew.
-    // `c` = scale log2 e.
+    // Hides the keys this row does not see (t0: the first key's number).
+    template <int Keys>
+    __device__ __forceinline__ void hide(Scores<Keys> &x, int t0, int lane) const {
+        const uint32_t seen = max(last - first + 1, 0), at = t0 + 4 * (lane >> 5) - first;
+#pragma unroll
+        for (int n = 0; n < Keys / 32; ++n)
+#pragma unroll
+            for (int i = 0; i < 16; ++i)
+                x.s[n][i] = at + (32 * n + 8 * (i / 4) + i % 4) < seen ? x.s[n][i] : kMinusInf;
+    }
+
+    // Hides keys where a tile needs it and makes the numerators from the maximum
+    // as it is; only where their sum shows that it lies too far below a score is
+    // it raised and are they made anew.  `c` = scale log2 e.
     template <int Keys>
     __device__ __forceinline__ void soften(Scores<Keys> &x, Numerators<Keys> &y, int t0, bool masked,
                                            float c, int lane) {
-        if (masked) {
-            const uint32_t seen = max(last - first + 1, 0), at = t0 + 4 * (lane >> 5) - first;
-#pragma unroll
-            for (int n = 0; n < Keys / 32; ++n)
-#pragma unroll
-                for (int i = 0; i < 16; ++i)
-                    x.s[n][i] = at + (32 * n + 8 * (i / 4) + i % 4) < seen ? x.s[n][i] : kMinusInf;
-        }
+        if (masked) hide(x, t0, lane);
         float sum = numerators(x, y, c);
         // the first keys, and scores too far above the maximum
         if (__any(m == kMinusInf || sum > kMostSum<T>)) {
@@ -404,52 +407,6 @@ __device__ __forceinline__ void store_lse(const taps_attend_launch &p, const tap
         l == 0.f ? kMinusInf : m * p.scale + __builtin_amdgcn_logf(l / kLift<T>) * kLn2;
 }
 
-// A row's result once more, by all lanes of a wavefront with two columns each:
-// only the keys that it sees are touched.  In the matrix products the numerator of a
-// hidden key, 0, meets that key's values, which another row of the tile sees; if one
-// is infinite or NaN, so is the product.  m and l do not depend on values.
-template <class T, int D>
-__device__ __forceinline__ void redo_row(const taps_attend_launch &p, const taps_plan_item &item,
-                                         uint32_t head, int row, float m, float l, int lane) {
-    typedef T v2 __attribute__((ext_vector_type(2)));
-    const int token = row / (int)p.group, sub = row - token * (int)p.group, d = 2 * lane;
-    const int pos = item.first_pos + token;
-    int first = item.lo, last = item.hi - 1;
-    if (p.causal) {
-        last = min(last, pos);
-        if (p.window) first = max(first, pos - (int)p.window + 1);
-    }
-    const bool live = d < (int)p.dim;
-    const float c = p.scale * kLog2e, shift = m == kMinusInf ? 0.f : m * c - kLiftLog2<T>;
-    v2 q = {};
-    if (live)
-        q = *(const v2 *)(p.q + (int64_t)(item.token0 + token) * p.q_token +
-                          (int64_t)(head * p.group + sub) * p.q_head + 2 * d);
-    float o[2] = {0.f, 0.f};
-    for (int j = first; j <= last; ++j) {
-        const int64_t page = p.pages[item.page0 + (j >> p.page_log2)];
-        const int64_t slot = j & ((1 << p.page_log2) - 1);
-        v2 k = {}, v = {};
-        if (live) {
-            k = *(const v2 *)(p.k_cache + head * p.k_head + page * p.k_page + slot * p.k_slot + 2 * d);
-            v = *(const v2 *)(p.v_cache + head * p.v_head + page * p.v_page + slot * p.v_slot + 2 * d);
-        }
-        const float s = row_sum<64>((float)q[0] * (float)k[0] + (float)q[1] * (float)k[1]);
-        const float e = __builtin_amdgcn_exp2f(s * c - shift);
-        o[0] += e * (float)v[0], o[1] += e * (float)v[1];
-    }
-    if (!live) return;
-    if (item.part < 0) {
-        const float inv = l == 0.f ? 0.f : 1.f / l;
-        *(uint32_t *)(out_row<T>(p, item, head, row) + 2 * d) = pack2<T>(o[0] * inv, o[1] * inv);
-        if (d == 0) store_lse<T>(p, item, head, row, m, l);
-    } else {
-        const int64_t at = (int64_t)(item.part + row - item.row0) * p.kv_heads + head;
-        p.part_o[at * p.dim + d] = o[0], p.part_o[at * p.dim + d + 1] = o[1];
-        if (d == 0) p.part_ml[2 * at] = m, p.part_ml[2 * at + 1] = l;
-    }
-}
-
 template <class T, int D>
 __device__ __forceinline__ void write_rows(const taps_attend_launch &p, const taps_plan_item &item,
                                            uint32_t head, const Rows<T, D> &rows, int row, float l,
@@ -483,25 +440,6 @@ __device__ __forceinline__ void write_rows(const taps_attend_launch &p, const ta
     }
 }
 
-// Writes the result of a wavefront's 32 rows; `row` is this lane's.
-template <class T, int D>
-__device__ __forceinline__ void finish(const taps_attend_launch &p, const taps_plan_item &item,
-                                       uint32_t head, const Rows<T, D> &rows, int row, int lane) {
-    const int half = lane >> 5;
-    const float l = half_sum(rows.l);
-    uint32_t again = 0;   // rows to redo: either half of their results is not finite
-    if (item.rows > (int)p.group) {   // rows of several tokens: one sees what another does not
-        const uint64_t broken = __ballot(row < item.rows && rows.broken());
-        again = (uint32_t)broken | (uint32_t)(broken >> 32);
-    }
-    if (row < item.rows && !(again >> (lane & 31) & 1))
-        write_rows(p, item, head, rows, row, l, half);
-    for (int r = 0; r < 32; ++r)
-        if (again >> r & 1)
-            redo_row<T, D>(p, item, head, __shfl(row, r, 64), __shfl(rows.m, r, 64),
-                           __shfl(l, r, 64), lane);
-}
-
 // The keys that all 32 rows from `row0` on see, of the item's: a tile outside
 // needs a mask.  A wavefront does nothing with the tiles from `end` on but load
 // its part of them: a branch within the loop costs the other tiles 64 register
@@ -513,7 +451,7 @@ struct Seen {
     __device__ __forceinline__ Seen(const taps_attend_launch &p, const taps_plan_item &item,
                                     int row0) {
         from = item.lo, to = item.hi - 1, end = row0 < item.rows ? item.hi : item.lo;
-        if (!p.causal) return;
+        if (!p.causal || item.rows <= (int)p.group) return;   // all rows see the item's keys
         const int a = min(row0, item.rows - 1), b = min(row0 + 31, item.rows - 1);
         end = min(end, item.first_pos + b / (int)p.group + 1);
         to = min(to, item.first_pos + a / (int)p.group);
@@ -522,7 +460,130 @@ struct Seen {
     __device__ __forceinline__ bool masks(int t0, int keys) const {
         return t0 < from || t0 + keys - 1 > to;
     }
+    // Whether one of the rows sees a key of the item that another does not.
+    __device__ __forceinline__ bool differ(const taps_plan_item &item) const {
+        return from > item.lo || to < min(item.hi, end) - 1;
+    }
 };
+
+// The rows of `again` once more, from tiles of 32 keys at t0, t0 + step ..  In the
+// matrix products the numerator of a key that a row does not see, 0, meets the key's
+// values, which another row of the tile sees; if one is infinite or NaN, so is the
+// product, and the row is found by that.  Where all rows see a tile nothing of the kind
+// can happen: those are taken as before, only from memory.  In the others the values
+// that a row does not see are made zeros, row by row.  m and l do not depend on values.
+// (A prompt of 2048, 8 heads of 128 over 4, whose first value is infinite, so that all
+// rows are done again: 249 us, 39 without; a row and a key at a time took 9.9 ms.)
+// Behind the kernels' other code: between it, it cost a lone token 0.7 us.
+template <class T, int D>
+__device__ __forceinline__ void redo(const taps_attend_launch &p, const taps_plan_item &item,
+                                     uint32_t head, Rows<T, D> &rows, uint32_t again,
+                                     const Seen &seen, int t0, int step, int lane) {
+    constexpr int kSteps = D / 16, kBlocks = D / 32;
+    using R = Rows<T, D>;
+    const int half = lane >> 5, lo = item.lo, hi = min(item.hi, seen.end), dim = p.dim;
+    const char *k_head = p.k_cache + (int64_t)head * p.k_head;
+    const char *v_head = p.v_cache + (int64_t)head * p.v_head;
+    const float c = p.scale * kLog2e;
+#pragma unroll
+    for (int b = 0; b < kBlocks; ++b) rows.o[b] = f32x16{};
+    for (; lo < hi && t0 < hi; t0 += step) {
+        // two groups of 16 keys; of one that lies outside, and of keys outside, the nearest inside
+        const char *k_at[2], *v_at[2];
+        int key0[2];
+#pragma unroll
+        for (int n = 0; n < 2; ++n) {
+            key0[n] = min(max(t0 + 16 * n, lo & ~15), (hi - 1) & ~15);
+            const Place at(p, k_head, v_head, page_at(p, p.pages + item.page0, key0[n], lo, hi),
+                           key0[n]);
+            k_at[n] = at.k, v_at[n] = at.v;
+        }
+        const auto in = [&](int key) { return key >= lo && key < hi; };
+        const auto slot_of = [&](int key, int n) {
+            return (uint32_t)(min(max(key, lo), hi - 1) - key0[n]);
+        };
+        typename R::template Scores<32> x;
+        typename R::template Numerators<32> y;
+        x.s[0] = f32x16{};
+        {
+            const int key = t0 + (lane & 31), n = (lane >> 4) & 1;
+            const char *row = (n ? k_at[1] : k_at[0]) +
+                              (n ? slot_of(key, 1) : slot_of(key, 0)) * (uint32_t)p.k_slot;
+#pragma unroll
+            for (int k = 0; k < kSteps; ++k) {
+                const int d = 16 * k + 8 * half;
+                s16x8 a = *(const s16x8 *)(row + 2 * (d < dim ? d : 0));
+                if (!in(key) || d >= dim) a = s16x8{};
+                x.s[0] = Mfma<T>::run(a, rows.q[k], x.s[0]);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+        }
+        rows.hide(x, t0, lane);
+        rows.numerators(x, y, c);
+        const bool masked = seen.masks(t0, 32);
+#pragma unroll
+        for (int b = 0; b < kBlocks; ++b) {
+            const int d = 32 * b + (lane & 31);
+            s16x8 v[2];   // column d of the keys of the numerators
+            // this path is rare and the kernels' registers are few: no address is kept, no load moved
+            uint32_t slot = (uint32_t)p.v_slot;
+            asm volatile("" : "+s"(slot));
+#pragma unroll
+            for (int n = 0; n < 2; ++n)
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    const int key = t0 + 16 * n + 8 * (e / 4) + 4 * half + e % 4;
+                    const short u = *(const short *)(v_at[n] + slot_of(key, n) * slot +
+                                                     2 * (d < dim ? d : 0));
+                    v[n][e] = in(key) && d < dim ? u : (short)0;
+                    if (e % 4 == 3) __builtin_amdgcn_sched_barrier(0);
+                }
+            if (!masked) {
+#pragma unroll
+                for (int n = 0; n < 2; ++n)
+                    rows.o[b] = Mfma<T>::run(v[n], __builtin_bit_cast(s16x8, y.p[n]), rows.o[b]);
+                continue;
+            }
+            for (uint32_t left = again; left; left &= left - 1) {
+                const int r = __builtin_ctz(left);
+                const int first = __shfl(rows.first, r, 64), last = __shfl(rows.last, r, 64);
+                f32x16 o = {};
+#pragma unroll
+                for (int n = 0; n < 2; ++n) {
+                    s16x8 w;
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) {
+                        const int key = t0 + 16 * n + 8 * (e / 4) + 4 * half + e % 4;
+                        w[e] = key >= first && key <= last ? v[n][e] : (short)0;
+                    }
+                    o = Mfma<T>::run(w, __builtin_bit_cast(s16x8, y.p[n]), o);
+                }
+#pragma unroll
+                for (int i = 0; i < 16; ++i)
+                    rows.o[b][i] = (lane & 31) == r ? rows.o[b][i] + o[i] : rows.o[b][i];
+            }
+        }
+    }
+}
+
+// Hands the results of a wavefront's 32 rows to write(), for some lanes' rows at a
+// time; `row` is this lane's, `l` the sum of both its halves, t0 and step the
+// wavefront's tiles (32 keys each) in the item.
+template <class T, int D, class F>
+__device__ __forceinline__ void finish(const taps_attend_launch &p, const taps_plan_item &item,
+                                       uint32_t head, Rows<T, D> &rows, const Seen &seen, int row,
+                                       float l, int t0, int step, int lane, F &&write) {
+    uint32_t again = 0;   // rows to redo: either half of their results is not finite, by values
+    if (seen.differ(item)) {
+        const uint64_t broken = __ballot(row < item.rows && l == l && rows.broken());
+        again = (uint32_t)broken | (uint32_t)(broken >> 32);
+    }
+    const bool mine = again >> (lane & 31) & 1;
+    if (!mine) write();
+    if (__builtin_expect(again == 0, 1)) return;
+    redo(p, item, head, rows, again, seen, t0, step, lane);
+    if (mine) write();
+}
 
 // Loads to LDS: a wavefront takes 16 of a tile's 64 keys, of K or of V.  Keys
 // outside lo .. hi - 1 and columns beyond the head come from a block of zeros in
@@ -686,7 +747,10 @@ __global__ __launch_bounds__(kWideThreads, 2) void k_attend_wide(taps_attend_lau
             }
         }
     }
-    finish(p, item, head, rows, row, lane);
+    const float l = half_sum(rows.l);
+    finish(p, item, head, rows, seen, row, l, start, 32, lane, [&]() {
+        if (row < item.rows) write_rows(p, item, head, rows, row, l, lane >> 5);
+    });
 }
 
 // 128 query rows, 32 a wavefront, two workgroups to a unit (three for heads of up to
@@ -740,7 +804,10 @@ __device__ __forceinline__ void attend_block(const taps_attend_launch &p, const 
         rows.spend(tile + kPart, y, lane);
     }
     for (; t0 < hi; t0 += kWideKeys, buffer ^= 1) begin();   // the other wavefronts' tiles
-    finish(p, item, head, rows, row, lane);
+    const float l = half_sum(rows.l);
+    finish(p, item, head, rows, seen, row, l, start, 32, lane, [&]() {
+        if (row < item.rows) write_rows(p, item, head, rows, row, l, lane >> 5);
+    });
 }
 
 // Up to 32 query rows: every wavefront has all of them and its own keys, so that
@@ -831,7 +898,7 @@ __device__ __forceinline__ void attend_narrow(const taps_attend_launch &p,
             __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
         }
     }
-    float *ml = (float *)(lds + narrow_bytes<D>() - (2 * kWaves + 1) * kNarrowRows * 4);
+    float *ml = (float *)(lds + narrow_bytes<D>() - 2 * kWaves * kNarrowRows * 4);
     const float l_wave = half_sum(rows.l);
     __syncthreads();   // the tiles are done with
     if (half == 0) {
@@ -843,7 +910,8 @@ __device__ __forceinline__ void attend_narrow(const taps_attend_launch &p,
 #pragma unroll
     for (int w = 0; w < kWaves; ++w) m = fmaxf(m, ml[2 * (w * kNarrowRows + (lane & 31))]);
     float *sums = (float *)lds;   // [wave][row][D + 4]
-    {
+    const Seen seen(p, item, item.row0);
+    const auto leave = [&]() {
         const float by = rows.m == kMinusInf ? 0.f : __builtin_amdgcn_exp2f((rows.m - m) * c);
         float *at = sums + (wave * kNarrowRows + (lane & 31)) * (D + 4);
 #pragma unroll
@@ -854,7 +922,9 @@ __device__ __forceinline__ void attend_narrow(const taps_attend_launch &p,
                                  rows.o[b][4 * i + 2] * by, rows.o[b][4 * i + 3] * by};
                 *(f32x4 *)(at + 32 * b + 8 * i + 4 * half) = v;
             }
-    }
+    };
+    finish(p, item, head, rows, seen, item.row0 + (lane & 31), l_wave, start + kNarrowKeys * wave,
+           kWaves * kNarrowKeys, lane, leave);
     __syncthreads();
     const int n_rows = min(kNarrowRows, item.rows - item.row0);
     const auto result = [&](int r, int d) {
@@ -874,22 +944,9 @@ __device__ __forceinline__ void attend_narrow(const taps_attend_launch &p,
             l += mw == kMinusInf ? lw : lw * __builtin_amdgcn_exp2f((mw - top) * c);
         }
     };
-    int *again = (int *)(ml + 2 * kWaves * kNarrowRows);   // whether a row is to be redone
-    const bool several = item.rows > (int)p.group;
-    if (several) {
-        if (threadIdx.x < kNarrowRows) again[threadIdx.x] = 0;
-        __syncthreads();
-        for (int k = threadIdx.x; k < n_rows * (D / 4); k += kThreads) {
-            const int r = k / (D / 4);
-            const f32x4 o = result(r, 4 * (k % (D / 4))) * 0.f;
-            const float sum = o[0] + o[1] + o[2] + o[3];
-            if (sum != sum) again[r] = 1;
-        }
-        __syncthreads();
-    }
     for (int k = threadIdx.x; k < n_rows * (D / 4); k += kThreads) {
         const int r = k / (D / 4), d = 4 * (k % (D / 4));
-        if (d >= (int)p.dim || (several && again[r])) continue;
+        if (d >= (int)p.dim) continue;
         float top, l;
         statistics(r, top, l);
         const f32x4 o = result(r, d);
@@ -904,12 +961,6 @@ __device__ __forceinline__ void attend_narrow(const taps_attend_launch &p,
             *(f32x4 *)(p.part_o + at * p.dim + d) = o;
             if (d == 0) p.part_ml[2 * at] = top, p.part_ml[2 * at + 1] = l;
         }
-    }
-    for (int r = wave; several && r < n_rows; r += kWaves) {
-        if (!again[r]) continue;
-        float top, l;
-        statistics(r, top, l);
-        redo_row<T, D>(p, item, head, item.row0 + r, top, l, lane);
     }
 }
 

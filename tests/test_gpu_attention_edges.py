@@ -272,3 +272,84 @@ def test_calls_without_a_gradient_say_so():
         mine = torch.empty_like(q)
         assert A.taps_attend(*args, plan, out=mine) is mine and not mine.requires_grad
         assert torch.equal(mine, want_out)
+
+
+# ---------------------------------------------------------------------------
+# infinite and NaN values that many rows see
+# ---------------------------------------------------------------------------
+
+def _values_case(new, n, heads, dim, page, dtype, options, seed=51):
+    g = gen_of(seed)
+    k, v = (torch.randn(n, heads, dim, generator=g).to(dtype) for _ in range(2))
+    q = randn(g, new, 2 * heads, dim, dtype=dtype)
+    pages = np.arange(-(-n // page))[None]
+    plan = A.PagedPlan([new], [n], pages, n_pages=pages.size, page_size=page, q_heads=2 * heads,
+                       kv_heads=heads, head_dim=dim, **options)
+    return q, k, v, plan
+
+
+@pytest.mark.parametrize("dtype", [BF16, F16])
+@pytest.mark.parametrize("spec", [
+    # new tokens, keys, heads, dim, page, options
+    (4, 3001, 1, 128, 16, {}),                                  # narrow items, in pieces
+    (7, 700, 2, 40, 16, {"window": 90}),
+    (150, 150, 2, 64, 16, {}),
+    (90, 333, 2, 96, 32, {"window": 70}),
+    (200, 2000, 1, 128, 64, {"units": 4096}),                   # in pieces
+    (300, 2700, 1, 128, 64, {"units": 1}),                      # 256 rows an item
+    (300, 2900, 1, 80, 16, {"units": 1, "window": 1500}),
+    (130, 400, 2, 64, 16, {"causal": False}),
+    (60, 200, 2, 72, 16, {"kv_starts": [33]}),
+])
+@pytest.mark.parametrize("where", ["first", "everywhere", "a column"])
+def test_infinite_values_that_many_rows_see(spec, dtype, where):
+    new, n, heads, dim, page, options = spec
+    say(f"[gpu] attend infinite values {spec} {dtype} {where}")
+    q, k, v, plan = _values_case(*spec[:5], dtype, options)
+    start = options.get("kv_starts", [0])[0]
+    if where == "first":
+        v[start, :, 3], v[start, :, dim - 1] = math.inf, math.nan
+    elif where == "everywhere":
+        at = torch.rand(v.shape, generator=gen_of(5)) < 3e-3
+        v[at] = math.inf
+        v[torch.rand(v.shape, generator=gen_of(6)) < 1e-3] = math.nan
+    else:
+        v[:, 0, 5] = -math.inf
+    out, lse = A.taps_attend(q, paged(k, page), paged(v, page), plan, lse=True)
+    with np.errstate(invalid="ignore"):
+        want, bound, w_lse, b_lse = R.attend(
+            R.f64(q), R.f64(k), R.f64(v), n - new, start, options.get("causal", True),
+            options.get("window", 0), dim ** -0.5, dtype)
+    got, odd = R.f64(out), ~np.isfinite(want)
+    assert odd.any() or (where == "first" and "window" in options)   # there no row sees it
+    assert np.array_equal(odd, ~np.isfinite(got)), "not the same outputs are finite"
+    # an infinity whose weight is below the type's range may be NaN
+    assert np.array_equal(got[odd & ~np.isnan(got)], want[odd & ~np.isnan(got)])
+    assert np.isnan(got[np.isnan(want)]).all()
+    R.check(np.where(odd, 0, got), np.where(odd, 0, want), np.where(odd, 0, bound), "finite")
+    R.check(lse, w_lse, b_lse, "lse")
+
+
+@pytest.mark.parametrize("new,n", [(2048, 2048), (512, 16384), (4, 16384)])
+def test_infinite_values_cost_a_few_passes(new, n):
+    """A value that has overflowed early in a document, and all of them: rows that are done again
+    take the time of a few passes, not that of a key at a time (hundreds)."""
+    q, k, v, plan = _values_case(new, n, 4, 128, 64, BF16, {})
+    kc, vc = paged(k, 64), paged(v, 64)
+    cases = [vc, vc.clone(), torch.full_like(vc, math.nan)]
+    cases[1][0, :, 2, 7] = math.inf
+    times = []
+    for c in cases:
+        A.taps_attend(q, kc, c, plan)
+        best = math.inf
+        for _ in range(3):
+            a, b = (torch.cuda.Event(enable_timing=True) for _ in range(2))
+            a.record()
+            A.taps_attend(q, kc, c, plan)
+            b.record()
+            b.synchronize()
+            best = min(best, a.elapsed_time(b) * 1e3)
+        times.append(best)
+    say(f"[gpu] attend {new} over {n}: {times[0]:.0f} us, one infinite value {times[1]:.0f}, "
+        f"all NaN {times[2]:.0f}")
+    assert max(times[1:]) < 20 * times[0] + 100
