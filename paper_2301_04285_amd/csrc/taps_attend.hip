@@ -226,7 +226,7 @@ template <class T, int D> struct Rows {
             q[k] = s16x8{};
             if (real && d < (int)p.dim) q[k] = *(const s16x8 *)(at + 2 * d);
         }
-        m = kMinusInf;
+        m = real ? kMinusInf : 0.f;   // a row that is not there never raises it
         l = 0.f;
 #pragma unroll
         for (int b = 0; b < kBlocks; ++b) o[b] = f32x16{};
@@ -827,10 +827,8 @@ __device__ __forceinline__ void attend_narrow(const taps_attend_launch &p,
     const int half = lane >> 5;
     Rows<T, D> rows;
     rows.start(p, item, head, item.row0 + (lane & 31), lane);
+    const Seen seen(p, item, item.row0);
     {
-        const int last_row = min(item.row0 + kNarrowRows, item.rows) - 1;
-        // one token's rows all see the item's keys; several tokens' need masks
-        const bool one = item.row0 / (int)p.group == last_row / (int)p.group || !p.causal;
         char *tile = lds + wave * Tile<D>::bytes(kNarrowKeys);
         // The next tile, two groups of 16 keys, waits in registers; keys outside lo .. hi - 1 are
         // loaded from an end of that range and become zeros on the way to LDS, as do columns
@@ -887,7 +885,7 @@ __device__ __forceinline__ void attend_narrow(const taps_attend_launch &p,
                 page0 = page_at(p, pages, t0 + 2 * kStep, lo, hi);
                 page1 = page_at(p, pages, t0 + 2 * kStep + 16, lo, hi);
             }
-            const bool masked = !one || t0 < lo || t0 + kNarrowKeys > hi;
+            const bool masked = seen.masks(t0, kNarrowKeys);
             typename Rows<T, D>::template Scores<kNarrowKeys> x;
             typename Rows<T, D>::template Numerators<kNarrowKeys> y;
             rows.score(tile, x, lane);
@@ -910,7 +908,6 @@ __device__ __forceinline__ void attend_narrow(const taps_attend_launch &p,
 #pragma unroll
     for (int w = 0; w < kWaves; ++w) m = fmaxf(m, ml[2 * (w * kNarrowRows + (lane & 31))]);
     float *sums = (float *)lds;   // [wave][row][D + 4]
-    const Seen seen(p, item, item.row0);
     const auto leave = [&]() {
         const float by = rows.m == kMinusInf ? 0.f : __builtin_amdgcn_exp2f((rows.m - m) * c);
         float *at = sums + (wave * kNarrowRows + (lane & 31)) * (D + 4);

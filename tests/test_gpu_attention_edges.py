@@ -353,3 +353,28 @@ def test_infinite_values_cost_a_few_passes(new, n):
     say(f"[gpu] attend {new} over {n}: {times[0]:.0f} us, one infinite value {times[1]:.0f}, "
         f"all NaN {times[2]:.0f}")
     assert max(times[1:]) < 20 * times[0] + 100
+
+
+@pytest.mark.parametrize("dim", [64, 128])
+def test_a_few_tokens_take_a_tokens_time(dim):
+    """Rows that pad a wavefront do not send it into the path that raises maxima, nor do tiles that
+    all rows see: four tokens of one head over keys in one piece take what one takes."""
+    n = 16384
+    g = gen_of(61)
+    k, v = (paged(torch.randn(n, 8, dim, generator=g).to(BF16), 64) for _ in range(2))
+    pages = np.arange(n // 64)[None]
+    plans = [A.PagedPlan([new], [n], pages, n_pages=pages.size, page_size=64, q_heads=8, kv_heads=8,
+                         head_dim=dim, units=1) for new in (1, 4)]
+    q = randn(g, 4, 8, dim)
+    times = [math.inf, math.inf]
+    for _ in range(10):
+        for i, new in enumerate((1, 4)):
+            a, b = (torch.cuda.Event(enable_timing=True) for _ in range(2))
+            a.record()
+            for _ in range(5):
+                A.taps_attend(q[:new], k, v, plans[i])
+            b.record()
+            b.synchronize()
+            times[i] = min(times[i], a.elapsed_time(b) * 200)
+    say(f"[gpu] attend 1 and 4 tokens over {n}, heads of {dim}: {times[0]:.1f} and {times[1]:.1f} us")
+    assert times[1] < 1.2 * times[0]
