@@ -967,7 +967,7 @@ __global__ __launch_bounds__(kThreads, 2) void k_attend(taps_attend_launch p) {
     __shared__ __attribute__((aligned(16))) char lds[max_of(narrow_bytes<D>(),
                                                             2 * Tile<D>::bytes(kWideKeys))];
     const uint32_t head = blockIdx.x % p.kv_heads;
-    const taps_plan_item item = p.items[p.n_wide + blockIdx.x / p.kv_heads];
+    const taps_plan_item item = p.items[blockIdx.x / p.kv_heads];
     if (item.kind == kBlock)
         attend_block<T, D>(p, item, head, lds);
     else
@@ -1047,11 +1047,22 @@ __global__ __launch_bounds__(kThreads) void k_join(taps_attend_launch p) {
     if (d == 0) store_lse<T>(p, item, head, join.row0 + r, m, l);
 }
 
-template <class T, int D> void launch_items(const taps_attend_launch &p, hipStream_t stream) {
+// Launches of as many of n items as a grid's dimension, fewer than 2^32 threads, holds.
+template <class F>
+void in_slices(taps_attend_launch p, uint32_t n, int threads, F &&launch_slice) {
+    const uint32_t most = max(0xffffffffu / threads / p.kv_heads, 1u);
+    for (; n; n -= min(n, most), p.items += most) launch_slice(p, min(n, most) * p.kv_heads);
+}
+
+template <class T, int D> void launch_items(taps_attend_launch p, hipStream_t stream) {
     if constexpr (D > kWideAbove)
-        if (p.n_wide) k_attend_wide<T, D><<<p.n_wide * p.kv_heads, kWideThreads, 0, stream>>>(p);
-    if (p.n_items > p.n_wide)
-        k_attend<T, D><<<(p.n_items - p.n_wide) * p.kv_heads, kThreads, 0, stream>>>(p);
+        in_slices(p, p.n_wide, kWideThreads, [&](const taps_attend_launch &s, uint32_t groups) {
+            k_attend_wide<T, D><<<groups, kWideThreads, 0, stream>>>(s);
+        });
+    p.items += p.n_wide;
+    in_slices(p, p.n_items - p.n_wide, kThreads, [&](const taps_attend_launch &s, uint32_t groups) {
+        k_attend<T, D><<<groups, kThreads, 0, stream>>>(s);
+    });
 }
 
 template <class T> hipError_t launch(const taps_attend_launch &p, hipStream_t stream) {

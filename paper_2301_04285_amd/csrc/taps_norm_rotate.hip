@@ -27,6 +27,13 @@
 namespace {
 
 constexpr int kThreads = 256;
+// Workgroups in the first dimension of a launch, which holds fewer than 2^32
+// threads; the second dimension numbers rows of as many.
+constexpr uint32_t kGridRow = 1u << 22;
+__device__ __forceinline__ uint32_t workgroup() { return blockIdx.y * kGridRow + blockIdx.x; }
+dim3 grid_of(uint32_t groups) {
+    return groups <= kGridRow ? dim3(groups) : dim3(kGridRow, (groups + kGridRow - 1) / kGridRow);
+}
 // Rows that a group of lanes has on their way at once.
 constexpr int kAtOnce = 4;
 
@@ -221,7 +228,7 @@ __global__ __launch_bounds__(kThreads) void k_norm_rotate(taps_rows_launch p) {
     const uint32_t heads = p.heads[0] + p.heads[1];
     const Split split(heads, Lanes);
     const uint32_t group = threadIdx.x / Lanes;
-    const uint32_t token = blockIdx.x * split.tokens + group / split.across;
+    const uint32_t token = workgroup() * split.tokens + group / split.across;
     if (token >= p.batch * p.tokens) return;   // whole groups leave; sums stay inside a group
     const uint32_t b = token / p.tokens, t = token % p.tokens;
     const P pairs(p, threadIdx.x % Lanes);
@@ -276,7 +283,7 @@ __global__ __launch_bounds__(kThreads) void k_append(taps_rows_launch p) {
     const uint32_t heads = 2 * p.heads[0];
     const Split split(heads, Lanes);
     const uint32_t group = threadIdx.x / Lanes;
-    const uint32_t t = blockIdx.x * split.tokens + group / split.across;
+    const uint32_t t = workgroup() * split.tokens + group / split.across;
     if (t >= p.tokens) return;
     const taps_plan_token place = p.plan_tokens[t];
     if (place.slot < 0) return;
@@ -498,10 +505,10 @@ hipError_t taps_launch_norm_rotate(const taps_rows_launch &p, uint32_t dtype, bo
     with_type(dtype, [&](auto zero) {
         using T = decltype(zero);
         if (!vectors)
-            k_norm_rotate<T, false, 64><<<groups, kThreads, 0, stream>>>(p);
+            k_norm_rotate<T, false, 64><<<grid_of(groups), kThreads, 0, stream>>>(p);
         else
             with_lanes(p.dim, [&](auto n) {
-                k_norm_rotate<T, true, decltype(n)::value><<<groups, kThreads, 0, stream>>>(p);
+                k_norm_rotate<T, true, decltype(n)::value><<<grid_of(groups), kThreads, 0, stream>>>(p);
             });
     });
     return hipGetLastError();
@@ -513,10 +520,10 @@ hipError_t taps_launch_append(const taps_rows_launch &p, uint32_t dtype, bool ve
     with_type(dtype, [&](auto zero) {
         using T = decltype(zero);
         if (!vectors)
-            k_append<T, false, 64><<<groups, kThreads, 0, stream>>>(p);
+            k_append<T, false, 64><<<grid_of(groups), kThreads, 0, stream>>>(p);
         else
             with_lanes(p.dim, [&](auto n) {
-                k_append<T, true, decltype(n)::value><<<groups, kThreads, 0, stream>>>(p);
+                k_append<T, true, decltype(n)::value><<<grid_of(groups), kThreads, 0, stream>>>(p);
             });
     });
     return hipGetLastError();

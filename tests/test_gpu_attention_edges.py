@@ -378,3 +378,55 @@ def test_a_few_tokens_take_a_tokens_time(dim):
             times[i] = min(times[i], a.elapsed_time(b) * 200)
     say(f"[gpu] attend 1 and 4 tokens over {n}, heads of {dim}: {times[0]:.1f} and {times[1]:.1f} us")
     assert times[1] < 1.2 * times[0]
+
+
+# ---------------------------------------------------------------------------
+# more workgroups than one dimension of a launch holds threads for
+# ---------------------------------------------------------------------------
+
+def test_norm_of_many_tokens():
+    """2^24 workgroups of 256 threads: the same as in calls of fewer tokens."""
+    tokens, heads, dim = (1 << 24) + 3, 4, 7
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(71)
+    q = torch.randn(tokens, heads, dim, generator=gen, device="cuda", dtype=BF16)
+    w = torch.randn(dim, generator=gen, device="cuda", dtype=BF16)
+    say(f"[gpu] norm of {tokens} tokens")
+    out, _ = A.taps_norm_rotate(q, None, w, None, None)
+    for a in range(0, tokens, 5_000_000):
+        part, _ = A.taps_norm_rotate(q[a:a + 5_000_000], None, w, None, None)
+        assert torch.equal(out[a:a + 5_000_000], part)
+
+
+def test_append_of_many_tokens():
+    tokens, heads, dim, page = (1 << 24) + 3, 2, 7, 4096
+    n_pages = -(-tokens // page)
+    k, v = (torch.arange(tokens * heads * dim, device="cuda").remainder(m).view(tokens, heads, dim)
+            .to(BF16) for m in (251, 241))
+    caches = [torch.zeros(n_pages, page, heads, dim, dtype=BF16, device="cuda") for _ in range(2)]
+    say(f"[gpu] append of {tokens} tokens")
+    plan = A.PagedPlan([tokens], [tokens], np.arange(n_pages)[None], n_pages=n_pages, page_size=page,
+                       q_heads=heads, kv_heads=heads, head_dim=dim)
+    A.taps_cache_append(k, v, *(c.transpose(1, 2) for c in caches), plan)
+    assert torch.equal(caches[0].flatten(0, 1)[:tokens], k)
+    assert torch.equal(caches[1].flatten(0, 1)[:tokens], v)
+
+
+def test_attention_of_many_items():
+    """A token and 128 heads of each of 2^17 + 1 sequences, two of which have keys."""
+    seqs, heads, dim = (1 << 17) + 1, 128, 8
+    g = gen_of(73)
+    k, v = (randn(g, 2, heads, 16, dim) for _ in range(2))
+    kv = np.zeros(seqs, dtype=np.int32)
+    kv[[5, seqs - 1]] = 9, 16
+    pages = np.zeros((seqs, 1), dtype=np.int32)
+    pages[5] = 1
+    q = torch.zeros(seqs, heads, dim, dtype=BF16, device="cuda")
+    q[[5, seqs - 1]] = randn(g, 2, heads, dim)
+    say(f"[gpu] attend {seqs} sequences of {heads} heads")
+    how = {"n_pages": 2, "page_size": 16, "q_heads": heads, "kv_heads": heads, "head_dim": dim}
+    out = A.taps_attend(q, k, v, A.PagedPlan([1] * seqs, kv, pages, **how))
+    want = A.taps_attend(q[[5, seqs - 1]], k, v, A.PagedPlan([1, 1], [9, 16], [[1], [0]], **how))
+    assert torch.equal(out[[5, seqs - 1]], want) and want.isfinite().all()
+    out[[5, seqs - 1]] = 0
+    assert (out == 0).all()
