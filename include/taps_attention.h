@@ -167,8 +167,8 @@ taps_status taps_cache_append(const taps_append_args *args, const void *plan,
  *   lse    device float [tokens][q_heads] or NULL: log of the sum of
  *          exp(scale q k) of every token and head.
  *   workspace  device, 16-byte aligned, workspace_bytes as the plan said.
- * Every data pointer must be 16-byte aligned and every stride used a multiple
- * of 8; a cache's slots must be less than 2^26 elements apart. */
+ * Every data pointer must be 16-byte aligned and every stride of an axis longer
+ * than one a multiple of 8; a cache's slots must be less than 2^26 elements apart. */
 taps_status taps_attend(uint32_t dtype, const void *plan, const void *plan_device,
                         const taps_heads *q, const taps_heads *k_cache, const taps_heads *v_cache,
                         float scale, const taps_heads *out, float *lse, void *workspace,

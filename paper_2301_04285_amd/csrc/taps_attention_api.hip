@@ -620,8 +620,12 @@ taps_status taps_attend(uint32_t dtype, const void *plan, const void *plan_devic
     for (int i = 0; i < 4; ++i) {
         const bool cache = i == 1 || i == 2;
         if (!all[i] || !all[i]->data) return fail(TAPS_ERR_ARG, "%s is NULL", names[i]);
-        if (!aligned(all[i]->data, 16) || (cache && all[i]->stride[0] % 8) || all[i]->stride[1] % 8 ||
-            all[i]->stride[2] % 8)
+        // an axis of one is not stepped along
+        const uint32_t lengths[3] = {cache ? h->n_pages : 1, cache ? h->kv_heads : h->tokens,
+                                     cache ? 2 : h->q_heads};
+        bool fits = aligned(all[i]->data, 16);
+        for (int k = 0; k < 3; ++k) fits = fits && (lengths[k] < 2 || all[i]->stride[k] % 8 == 0);
+        if (!fits)
             return fail(TAPS_ERR_ARG, "%s: rows do not start at multiples of 16 bytes", names[i]);
         // 16 slots' offsets are held in 32 bits
         if (cache && (all[i]->stride[2] < 0 || all[i]->stride[2] >= (1 << 26)))

@@ -430,3 +430,30 @@ def test_attention_of_many_items():
     assert torch.equal(out[[5, seqs - 1]], want) and want.isfinite().all()
     out[[5, seqs - 1]] = 0
     assert (out == 0).all()
+
+
+# ---------------------------------------------------------------------------
+# strides
+# ---------------------------------------------------------------------------
+
+def test_strides_of_axes_of_one_are_not_used():
+    """One token, one head, one page: how far the next would be does not matter."""
+    g = gen_of(81)
+
+    def odd(t, axis):   # the same tensor with a stride of 8 n + 3 where its length is 1
+        assert t.shape[axis] == 1
+        strides = list(t.stride())
+        strides[axis] = strides[axis] * 2 + 3
+        return t.as_strided(t.shape, strides)
+    q, one_head = randn(g, 1, 8, 64), randn(g, 5, 1, 64)
+    cache, v = (randn(g, 3, 8, 16, 64) for _ in range(2))
+    plan = A.PagedPlan([1], [40], [[2, 0, 1]], n_pages=3, page_size=16, q_heads=8, kv_heads=8,
+                       head_dim=64)
+    want = A.taps_attend(q, cache, v, plan)
+    assert torch.equal(A.taps_attend(odd(q, 0), cache, v, plan), want)
+    out = odd(torch.empty_like(q), 0)
+    assert torch.equal(A.taps_attend(q, cache, v, plan, out=out), want)
+    page, pv = (randn(g, 1, 1, 16, 64) for _ in range(2))
+    plan = A.PagedPlan([5], [9], [[0]], n_pages=1, page_size=16, q_heads=1, kv_heads=1, head_dim=64)
+    want = A.taps_attend(one_head, page, pv, plan)
+    assert torch.equal(A.taps_attend(odd(one_head, 1), odd(page, 0), odd(odd(pv, 0), 1), plan), want)
