@@ -189,6 +189,22 @@ def _table(table, dim: int, device: int):
 _like = torch.empty_like   # of every way to an output the shortest
 
 
+def _output(t, rank: int):
+    """(a new tensor like ``t``, its Heads).  After overlapping rows (a sliding window over tokens)
+    empty_like may not keep a head's elements together."""
+    out = _like(t)
+    s = out.stride()
+    if s[-1] != 1:
+        out = torch.empty(t.shape, dtype=t.dtype, device=t.device)
+        s = out.stride()
+    if rank == 3:
+        return out, Heads(out.data_ptr(), 0, s[0], s[1])
+    return out, Heads(out.data_ptr(), s[0], s[1], s[2])
+
+
+_NO_OUTPUT = None, None
+
+
 def _on(stream, make):
     """New tensors belong to the stream that fills them."""
     if stream is None:
@@ -213,9 +229,10 @@ class _NoGradient(torch.autograd.Function):
 def _no_gradient(said: str, outputs, inputs):
     """``outputs``, which raise in a backward pass if one of the inputs asks for it: left without
     a history they would pass for constants there."""
-    for t in inputs:
-        if t is not None and t.requires_grad and torch.is_grad_enabled():
-            return _NoGradient.apply(said, outputs, *inputs)
+    if torch.is_grad_enabled():
+        for t in inputs:
+            if t is not None and t.requires_grad:
+                return _NoGradient.apply(said, outputs, *inputs)
     return outputs
 
 
@@ -290,12 +307,15 @@ def taps_norm_rotate(q, k, q_weight, k_weight, table, positions=None, first=0, e
     rank = len(shape)
     kh = None if k is None else _heads(k, "k", device, dtype, k.shape, rank)
     qh = _heads(q, "q", device, dtype, shape, rank)
-    q_out, k_out = out if out is not None else \
-        _on(stream, lambda: (_like(q), None if k is None else _like(k)))   # dense, of slices too
-    _check(load().taps_norm_rotate(
-        C.byref(args), qh, kh, _heads(q_out, "out[0]", device, dtype, shape, rank),
-        None if k is None else _heads(k_out, "out[1]", device, dtype, k.shape, rank),
-        _stream(stream)), "taps_norm_rotate")
+    if out is None:   # dense even where q and k are slices of one projection
+        (q_out, qoh), (k_out, koh) = _on(
+            stream, lambda: (_output(q, rank), _NO_OUTPUT if k is None else _output(k, rank)))
+    else:
+        q_out, k_out = out
+        qoh = _heads(q_out, "out[0]", device, dtype, shape, rank)
+        koh = None if k is None else _heads(k_out, "out[1]", device, dtype, k.shape, rank)
+    _check(load().taps_norm_rotate(C.byref(args), qh, kh, qoh, koh, _stream(stream)),
+           "taps_norm_rotate")
     if out is not None:
         return q_out, k_out
     return _no_gradient("taps_norm_rotate has no gradient: call norm_rotate", (q_out, k_out),
@@ -315,22 +335,20 @@ def taps_norm_rotate_backward(dq_out, dk_out, q, k, q_weight, k_weight, table, p
     rank = len(shape)
     qh = _heads(q, "q", device, dtype, shape, rank)
     gqh = _heads(dq_out, "dq_out", device, dtype, shape, rank)
-    kh = gkh = dkh = None
+    kh = gkh = None
     if k is not None:
         kh = _heads(k, "k", device, dtype, k.shape, rank)
         gkh = _heads(dk_out, "dk_out", device, dtype, k.shape, rank)
     size = WORKSPACE_PER_ELEMENT * shape[-1]
 
     def make():
-        return (_like(q), None if k is None else _like(k),
+        return (_output(q, rank), _NO_OUTPUT if k is None else _output(k, rank),
                 None if q_weight is None else _like(q_weight),
                 None if k_weight is None else _like(k_weight),
                 torch.empty(size, dtype=torch.uint8, device=q.device))
-    dq, dk, dqw, dkw, workspace = _on(stream, make)
-    if k is not None:
-        dkh = _heads(dk, "dk", device, dtype, k.shape, rank)
+    (dq, dqh), (dk, dkh), dqw, dkw, workspace = _on(stream, make)
     _check(load().taps_norm_rotate_backward(
-        C.byref(args), gqh, gkh, qh, kh, _heads(dq, "dq", device, dtype, shape, rank), dkh,
+        C.byref(args), gqh, gkh, qh, kh, dqh, dkh,
         None if dqw is None else dqw.data_ptr(), None if dkw is None else dkw.data_ptr(),
         workspace.data_ptr(), C.byref(C.c_uint64(size)), _stream(stream)),
         "taps_norm_rotate_backward")
@@ -516,15 +534,16 @@ def taps_attend(q, k_cache, v_cache, plan: PagedPlan, scale=None, out=None, lse=
     sums = workspace = None
     given = out
     if out is None:
-        out = _on(stream, lambda: _like(q))
+        out, oh = _on(stream, lambda: _output(q, 3))
+    else:
+        oh = _heads(out, "out", device, dtype, shape, 3)
     if lse:
         sums = _on(stream, lambda: torch.empty(shape[:2], dtype=torch.float32, device=q.device))
     if n:
         workspace = _on(stream, lambda: torch.empty(n, dtype=torch.uint8, device=q.device))
     _check(load().taps_attend(
         code, *plan.pointers(stream, raw, device), qh, kh, vh,
-        plan.head_dim ** -0.5 if scale is None else scale,
-        _heads(out, "out", device, dtype, shape, 3),
+        plan.head_dim ** -0.5 if scale is None else scale, oh,
         None if sums is None else sums.data_ptr(),
         None if workspace is None else workspace.data_ptr(), n, raw), "taps_attend")
     if given is None:

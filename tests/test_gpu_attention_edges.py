@@ -457,3 +457,25 @@ def test_strides_of_axes_of_one_are_not_used():
     plan = A.PagedPlan([5], [9], [[0]], n_pages=1, page_size=16, q_heads=1, kv_heads=1, head_dim=64)
     want = A.taps_attend(one_head, page, pv, plan)
     assert torch.equal(A.taps_attend(odd(one_head, 1), odd(page, 0), odd(odd(pv, 0), 1), plan), want)
+
+
+def test_overlapping_tokens():
+    """Queries that are a sliding window over one long row, by eight elements and by one."""
+    g = gen_of(82)
+    long, w, grad = randn(g, 1000), randn(g, 64), randn(g, 9, 4, 64)
+    table = A.rotation_table(9, 64)
+    cache, v = (randn(g, 1, 4, 16, 64) for _ in range(2))
+    plan = A.PagedPlan([9], [9], [[0]], n_pages=1, page_size=16, q_heads=4, kv_heads=4, head_dim=64)
+    for by in (8, 1):
+        q = long.as_strided((9, 4, 64), (by, 72, 1))
+        dense = q.contiguous()
+        out, _ = A.taps_norm_rotate(q, None, w, None, table)
+        assert torch.equal(out, A.taps_norm_rotate(dense, None, w, None, table)[0])
+        got = A.taps_norm_rotate_backward(grad, None, q, None, w, None, table)
+        want = A.taps_norm_rotate_backward(grad, None, dense, None, w, None, table)
+        # not the same path: rows that start anywhere are read element by element
+        b = 2 * R.ROUND[BF16] * want[0].abs().max() + 2e-5 * want[0].abs().max()
+        assert (got[0] - want[0]).abs().max() <= b
+        if by == 8:
+            assert torch.equal(A.taps_attend(q, cache, v, plan),
+                               A.taps_attend(dense, cache, v, plan))
