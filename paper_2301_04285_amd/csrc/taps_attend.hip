@@ -135,19 +135,19 @@ __device__ __forceinline__ uint32_t lds_at(const char *p) {
 
 // 16 bytes a lane from memory to LDS at `lds` + 16 lane, past the registers.
 // The compiler does not see the load: wait_loads() before the barrier that
-// hands the tile over.  It keeps nothing in m0 (LDS instructions do not read it on gfx9).
+// hands the tile over.
 __device__ __forceinline__ void load_to_lds(const char *from, uint32_t lds) {
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off"
                  :
                  : "s"(lds), "v"(from)
-                 : "memory");
+                 : "m0", "memory");
 }
 // The same from a uniform address and an offset a lane.
 __device__ __forceinline__ void load_to_lds(const char *from, uint32_t offset, uint32_t lds) {
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2"
                  :
                  : "s"(lds), "v"(offset), "s"(from)
-                 : "memory");
+                 : "m0", "memory");
 }
 // (the builtin, unlike an instruction in asm, tells the compiler too that no
 // load of its own is under way, or it would wait again inside the loop)
