@@ -161,7 +161,7 @@ taps_status taps_cache_append(const taps_append_args *args, const void *plan,
 
 /* out = softmax(scale q k^T) v over the keys each token sees; query head h
  * reads key head h / (q_heads / kv_heads).  A token that sees no key gets
- * zeros, and -inf in lse.
+ * zeros, and -inf in lse; one that sees only keys with scores of -inf gets NaN in both.
  *   dtype  TAPS_BF16 or TAPS_F16, of q, the cache and out.
  *   scale  positive and finite.
  *   lse    device float [tokens][q_heads] or NULL: log of the sum of

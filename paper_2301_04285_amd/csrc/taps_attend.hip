@@ -36,6 +36,9 @@ namespace {
 constexpr int kThreads = 256, kWaves = 4, kWideThreads = 2 * kWideRows;
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 constexpr float kMinusInf = -__builtin_inff();
+// The maximum of a row that sees keys whose scores are all -inf; -inf is that of one
+// that sees no key.
+constexpr float kNoScore = -3.402823466e38f;
 // Numerators are held as kLift exp(scale q.k - m), sums of them too; it cancels.
 // fp16 has its smallest normal number at 2^-14 and nothing below 2^-25, so there
 // the maximum's is placed at 2^10: keys that far below it still count, where many of
@@ -301,7 +304,7 @@ template <class T, int D> struct Rows {
     template <int Keys>
     __device__ __forceinline__ float numerators(const Scores<Keys> &x, Numerators<Keys> &y,
                                                 float c) const {
-        const float shift = m == kMinusInf ? 0.f : m * c - kLiftLog2<T>;
+        const float shift = m <= kNoScore ? 0.f : m * c - kLiftLog2<T>;
         float sum[2] = {0.f, 0.f};
 #pragma unroll
         for (int n = 0; n < Keys / 32; ++n)
@@ -365,6 +368,12 @@ template <class T, int D> struct Rows {
         __builtin_amdgcn_s_setprio(0);
     }
 
+    // The sum of its row's numerators, of both lanes; ends the statistics.
+    __device__ __forceinline__ float total() {
+        const float sum = half_sum(l);
+        if (sum == 0.f && m == kMinusInf && first <= last) m = kNoScore;
+        return sum;
+    }
     // Whether this lane's part of its row's result is not finite.
     __device__ __forceinline__ bool broken() const {
         float sum = 0.f;
@@ -398,13 +407,20 @@ __device__ __forceinline__ char *out_row(const taps_attend_launch &p, const taps
            (int64_t)(head * p.group + sub) * p.o_head;
 }
 
+// What turns a row's sum of numerators by values into its result.
+__device__ __forceinline__ float inverse(float m, float l) {
+    return l != 0.f ? 1.f / l : m == kMinusInf ? 0.f : __builtin_nanf("");
+}
+
 template <class T>
 __device__ __forceinline__ void store_lse(const taps_attend_launch &p, const taps_plan_item &s,
                                           uint32_t head, int row, float m, float l) {
     if (!p.lse) return;
     const int token = row / (int)p.group, sub = row - token * (int)p.group;
     p.lse[(int64_t)(s.token0 + token) * p.q_heads + head * p.group + sub] =
-        l == 0.f ? kMinusInf : m * p.scale + __builtin_amdgcn_logf(l / kLift<T>) * kLn2;
+        l != 0.f         ? m * p.scale + __builtin_amdgcn_logf(l / kLift<T>) * kLn2
+        : m == kMinusInf ? kMinusInf
+                         : __builtin_nanf("");
 }
 
 template <class T, int D>
@@ -413,7 +429,7 @@ __device__ __forceinline__ void write_rows(const taps_attend_launch &p, const ta
                                            int half) {
     constexpr int kBlocks = D / 32;
     if (item.part < 0) {
-        const float inv = l == 0.f ? 0.f : 1.f / l;
+        const float inv = inverse(rows.m, l);
         char *out = out_row<T>(p, item, head, row);
 #pragma unroll
         for (int b = 0; b < kBlocks; ++b)
@@ -747,7 +763,7 @@ __global__ __launch_bounds__(kWideThreads, 2) void k_attend_wide(taps_attend_lau
             }
         }
     }
-    const float l = half_sum(rows.l);
+    const float l = rows.total();
     finish(p, item, head, rows, seen, row, l, start, 32, lane, [&]() {
         if (row < item.rows) write_rows(p, item, head, rows, row, l, lane >> 5);
     });
@@ -804,7 +820,7 @@ __device__ __forceinline__ void attend_block(const taps_attend_launch &p, const 
         rows.spend(tile + kPart, y, lane);
     }
     for (; t0 < hi; t0 += kWideKeys, buffer ^= 1) begin();   // the other wavefronts' tiles
-    const float l = half_sum(rows.l);
+    const float l = rows.total();
     finish(p, item, head, rows, seen, row, l, start, 32, lane, [&]() {
         if (row < item.rows) write_rows(p, item, head, rows, row, l, lane >> 5);
     });
@@ -897,7 +913,7 @@ __device__ __forceinline__ void attend_narrow(const taps_attend_launch &p,
         }
     }
     float *ml = (float *)(lds + narrow_bytes<D>() - 2 * kWaves * kNarrowRows * 4);
-    const float l_wave = half_sum(rows.l);
+    const float l_wave = rows.total();
     __syncthreads();   // the tiles are done with
     if (half == 0) {
         ml[2 * (wave * kNarrowRows + lane)] = rows.m;
@@ -948,7 +964,7 @@ __device__ __forceinline__ void attend_narrow(const taps_attend_launch &p,
         statistics(r, top, l);
         const f32x4 o = result(r, d);
         if (item.part < 0) {
-            const float inv = l == 0.f ? 0.f : 1.f / l;
+            const float inv = inverse(top, l);
             char *out = out_row<T>(p, item, head, item.row0 + r);
             const u32x2 v = {pack2<T>(o[0] * inv, o[1] * inv), pack2<T>(o[2] * inv, o[3] * inv)};
             *(u32x2 *)(out + 2 * d) = v;
@@ -1038,7 +1054,7 @@ __global__ __launch_bounds__(kThreads) void k_join(taps_attend_launch p) {
         l += ls[g] * w;
         o += sums[g][threadIdx.x & 31] * w;
     }
-    const float inv = l == 0.f ? 0.f : 1.f / l;
+    const float inv = inverse(m, l);
     if (live) {
         char *out = out_row<T>(p, item, head, join.row0 + r);
         const u32x2 v = {pack2<T>(o[0] * inv, o[1] * inv), pack2<T>(o[2] * inv, o[3] * inv)};

@@ -479,3 +479,37 @@ def test_overlapping_tokens():
         if by == 8:
             assert torch.equal(A.taps_attend(q, cache, v, plan),
                                A.taps_attend(dense, cache, v, plan))
+
+
+# ---------------------------------------------------------------------------
+# scores of minus infinity
+# ---------------------------------------------------------------------------
+
+@pytest.mark.parametrize("dtype", [BF16, F16])
+@pytest.mark.parametrize("spec", [
+    # new tokens, keys, heads, dim, page, options
+    (1, 4, 2, 64, 16, {}), (3, 6, 1, 128, 16, {}), (9, 9, 2, 96, 16, {}), (150, 150, 2, 64, 16, {}),
+    (40, 4000, 1, 128, 64, {"units": 4096}),                    # in pieces
+    (1, 9000, 1, 64, 64, {"units": 4096}),
+    (2500, 2500, 1, 128, 64, {"units": 1}),                     # 256 rows an item
+])
+def test_scores_of_minus_infinity(spec, dtype):
+    """Keys whose scores are all -inf weigh nothing beside others; a row that sees no others has
+    no softmax and is NaN, unlike one that sees no key."""
+    new, n, heads, dim, page, options = spec
+    say(f"[gpu] attend scores of -inf {spec} {dtype}")
+    q, k, v, plan = _values_case(new, n, heads, dim, page, dtype, options)
+    q = q.abs()
+    dead = {1: n, 3: 4, 40: 3000, 2500: 70}.get(new, 5)   # so many keys from the first on
+    if n == 9000:
+        dead = 8999
+    k[:dead, :, 3] = -math.inf
+    out, lse = A.taps_attend(q, paged(k, page), paged(v, page), plan, lse=True)
+    gone = np.arange(n - new, n) < dead
+    assert out[torch.from_numpy(gone).cuda()].isnan().all()
+    assert lse[torch.from_numpy(gone).cuda()].isnan().all()
+    if not gone.all():
+        want, bound, w_lse, b_lse = R.attend(R.f64(q)[~gone], R.f64(k), R.f64(v),
+                                             max(n - new, dead), dead, True, 0, dim ** -0.5, dtype)
+        R.check(out[torch.from_numpy(~gone).cuda()], want, bound, "others")
+        R.check(lse[torch.from_numpy(~gone).cuda()], w_lse, b_lse, "lse of others")
