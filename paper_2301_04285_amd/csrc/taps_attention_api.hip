@@ -256,23 +256,30 @@ void in_order(std::vector<taps_plan_item> *items, int64_t cus, int64_t heads) {
 //     2048, 32 heads of 64: 212 us wide, 177 in blocks; 512 tokens over 32768
 //     keys, 32 heads of 64 over 8: 170 and 174; of 96: 209 and 223);
 //   - if the keys they see keep the loop busy beside a workgroup's start and end,
-//     which nothing covers (32 heads of 96, prompts of 1024: 184 and 171, of 2048: 266
-//     and 264, of 8000: 396 and 404; of 128 and 2048: 319 and 325);
+//     which nothing covers (32 heads of 128, eight prompts of 1024: 105 and 97, of 1900:
+//     301 and 295, of 2047: 322 and 328, of 2500: 455 and 478);
+//   - for heads of up to 96, if few of the keys are seen by some rows only, with
+//     which wavefronts wait for the strip's last one (32 heads of 96, prompts of 2048:
+//     269 to 289 and 264, two of 8000: 820 and 812; 4 chunks of 512 over 4096 keys, 32
+//     heads over 8: 101 and 108, one over 32768: 205 and 218);
 //   - if there are some rounds of them over the units, pieces counted (4 sequences of
 //     2048, 4 heads of 128: 51 and 48).
-constexpr int64_t kWideKeysSeen = 1024, kWideRounds = 4;
+constexpr int64_t kWideKeysSeen = 960, kWidePiece = 1024, kWideRounds = 4;
+constexpr uint32_t kDiagonalUpTo = 96;
 
 bool wide_pays(const taps_paged_batch *b, const std::vector<Sequence> &seqs, int64_t window,
                int64_t cus) {
-    int64_t strips = 0, pieces = 0, keys = 0;
+    int64_t strips = 0, pieces = 0, keys = 0, loaded = 0;
     for (const Sequence &q : seqs) {
         const int64_t n = q.rows / kWideRows, kv = q.kv_len - q.kv_start;
         int64_t seen = b->causal ? kv - (q.kv_len - q.first_pos) / 2 : kv;   // on average
-        if (window) seen = std::min(seen, window);
-        strips += n, keys += n * seen;
-        pieces += n * std::max<int64_t>(1, kv / kWideKeysSeen);
+        int64_t most = kv;
+        if (window) seen = std::min(seen, window), most = std::min(most, window + kWideRows);
+        strips += n, keys += n * seen, loaded += n * most;
+        pieces += n * std::max<int64_t>(1, kv / kWidePiece);
     }
     return b->head_dim > kWideAbove && keys >= kWideKeysSeen * strips &&
+           (b->head_dim > kDiagonalUpTo || 4 * keys >= 3 * loaded) &&
            pieces * b->kv_heads >= kWideRounds * cus;
 }
 

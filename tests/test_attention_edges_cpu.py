@@ -33,3 +33,23 @@ def test_positions_without_a_table_row_are_refused(size):
     assert "no rows" in A.last_error()
     a.tokens = 0   # nothing to look up
     assert L.taps_norm_rotate(C.byref(a), _heads(), NONE, _heads(), NONE, None) == taps.OK
+
+
+def _wide(q_len, kv_len, seqs, q_heads, kv_heads, dim):
+    """Strips of 256 rows of a step of like sequences, planned for 256 units."""
+    import numpy as np
+    n = -(-kv_len // 64)
+    p = A.PagedPlan([q_len] * seqs, [kv_len] * seqs, np.arange(seqs * n).reshape(seqs, n),
+                    n_pages=seqs * n, page_size=64, q_heads=q_heads, kv_heads=kv_heads, head_dim=dim,
+                    units=256, device=None)
+    return int(p._host.numpy()[72:76].view(np.int32)[0])   # n_wide of the plan's header
+
+
+def test_kinds_of_items():
+    """Lengths about each other are planned alike; heads of up to 96 take strips of 256 rows for
+    chunks late in a document only."""
+    for n in (1980, 2046, 2047, 2048, 2100):
+        assert _wide(n, n, 8, 32, 32, 128) and not _wide(n, n, 8, 32, 32, 64)
+        assert not _wide(n, n, 8, 32, 32, 96) and not _wide(n, n, 8, 32, 32, 80)
+    assert not _wide(1500, 1500, 8, 32, 32, 128)
+    assert _wide(512, 32768, 1, 32, 8, 96) and _wide(512, 4096, 4, 32, 8, 96)
