@@ -653,13 +653,15 @@ template <int D> struct Loader {
 // have a wavefront of their own at any time and a tile's loads serve twice the
 // rows of a block item.
 // 512 tokens over 32768 keys, 32 heads of 128 over 8: 243 us here, 1120 TFLOP/s (279
-// in blocks), the matrix cores busy for 55 % of the cycles at 1.9 GHz; the phases that
+// in blocks), the matrix cores busy for 58 % of the cycles at 1.9 GHz; the phases that
 // wait for each other take the rest.  The products alone, without loads, softmax and
 // reads of LDS, reach 1377 at the clocks that they leave, so a fifth is the most
 // there is to win.  Eight sequences of 2048 tokens, 32 heads, not causal, take 0.21 us a
-// key, 1280 TFLOP/s, and 90 us besides, for starting, reading queries and writing
-// results eight times on every unit.  One workgroup a unit that loads its next
-// item's tiles and queries while it ends the last takes no less (364 and 360 us).
+// key, 1280 TFLOP/s, and 90 us that do not grow with the keys.  Loading the next item's
+// first tiles and queries while the last ends wins none of those back (one workgroup
+// a unit that stays: 364 and 360 us).  Causal, a wavefront waits besides for the
+// tiles behind its last key that the strip's last one sees: 112 keys on average, a
+// tenth of the time for prompts of 2048.
 template <class T, int D>
 __global__ __launch_bounds__(kWideThreads, 2) void k_attend_wide(taps_attend_launch p) {
     constexpr int kPart = kWideKeys * Tile<D>::kRow;   // a tile's K, or its V

@@ -10,7 +10,7 @@
 // Each row is read once and written once: bytes bound these kernels.  64 heads of
 // 128 bf16 elements of 8192 tokens (a large copy does 4.9 TB/s, reads and writes
 // together):
-//   forwards   268 MB in  47 us  5.7 TB/s
+//   forwards   268 MB in  48 us  5.6 TB/s
 //   backwards  403 MB in 102 us  4.0 TB/s, and 6 us for the weights' gradients
 //   append     537 MB in 100 us  5.4 TB/s (16384 tokens of 32 heads, and values)
 // Few rows (one token of 32 heads of 64: 3.5 us) only wait for memory.
