@@ -476,9 +476,10 @@ struct Seen {
     __device__ __forceinline__ bool masks(int t0, int keys) const {
         return t0 < from || t0 + keys - 1 > to;
     }
-    // Whether one of the rows sees a key of the item that another does not.
+    // Whether one of the rows does not see a key of the item, which then may be in its
+    // tiles for the sake of another row, be it another wavefront's.
     __device__ __forceinline__ bool differ(const taps_plan_item &item) const {
-        return from > item.lo || to < min(item.hi, end) - 1;
+        return from > item.lo || to < item.hi - 1;
     }
 };
 

@@ -513,3 +513,28 @@ def test_scores_of_minus_infinity(spec, dtype):
                                              max(n - new, dead), dead, True, 0, dim ** -0.5, dtype)
         R.check(out[torch.from_numpy(~gone).cuda()], want, bound, "others")
         R.check(lse[torch.from_numpy(~gone).cuda()], w_lse, b_lse, "lse of others")
+
+
+@pytest.mark.parametrize("dtype", [BF16, F16])
+@pytest.mark.parametrize("new,n,heads,dim,options", [
+    (20, 20, 40, 64, {}), (9, 200, 32, 128, {}), (3, 70, 64, 96, {"window": 9}),
+    (40, 1500, 32, 128, {"units": 1}), (20, 3000, 40, 64, {"units": 4096}),
+])
+def test_infinite_values_and_many_heads(new, n, heads, dim, options, dtype):
+    """A wavefront whose rows are all of one token, beside others of later tokens: what those see
+    does not reach it."""
+    say(f"[gpu] attend infinite values, {heads} heads {new} {n} {dim} {dtype}")
+    g = gen_of(91)
+    k, v = (torch.randn(n, 1, dim, generator=g).to(dtype) for _ in range(2))
+    q = randn(g, new, heads, dim, dtype=dtype)
+    pages = np.arange(-(-n // 16))[None]
+    plan = A.PagedPlan([new], [n], pages, n_pages=pages.size, page_size=16, q_heads=heads,
+                       kv_heads=1, head_dim=dim, **options)
+    for j, value in ((1, math.inf), (new // 2, math.nan), (new - 2, -math.inf)):
+        v[n - 1 - j, 0, (5 * j) % dim] = value
+    out, lse = A.taps_attend(q, paged(k, 16), paged(v, 16), plan, lse=True)
+    with np.errstate(invalid="ignore"):
+        want, bound, w_lse, b_lse = R.attend(R.f64(q), R.f64(k), R.f64(v), n - new, 0, True,
+                                             options.get("window", 0), dim ** -0.5, dtype)
+    same_specials(out, want, np.nan_to_num(bound), "result")
+    R.check(lse, w_lse, b_lse, "lse")
