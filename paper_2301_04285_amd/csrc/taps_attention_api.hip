@@ -2,77 +2,19 @@
 // and launches.  Host code only sizes and checks.
 #include <algorithm>
 #include <cmath>
-#include <cstdarg>
-#include <cstdio>
 #include <cstring>
 #include <new>
 #include <vector>
 
-#include "taps_attention_internal.h"
+#include "taps_attention_checks.h"
+
+using namespace taps_checks;
 
 namespace {
-
-thread_local char g_last_error[512] = "";
-
-taps_status fail(taps_status st, const char *fmt, ...) {
-    va_list ap;
-    va_start(ap, fmt);
-    vsnprintf(g_last_error, sizeof g_last_error, fmt, ap);
-    va_end(ap);
-    return st;
-}
-
-taps_status launched(hipError_t err, const char *what) {
-    if (err == hipSuccess) return TAPS_OK;
-    return fail(TAPS_ERR_DEVICE, "%s: %s", what, hipGetErrorString(err));
-}
-
-uint32_t size_of(uint32_t dtype) { return dtype == TAPS_F32 ? 4 : 2; }
-
-bool aligned(const void *p, uint64_t bytes) { return ((uintptr_t)p & (bytes - 1)) == 0; }
 
 // ---------------------------------------------------------------------------
 // norm and rotation
 // ---------------------------------------------------------------------------
-
-taps_status check_types(uint32_t dtype, uint32_t weight_dtype, uint32_t dim, uint32_t rotary,
-                        float eps, const float *table) {
-    if (dtype > TAPS_F32) return fail(TAPS_ERR_ARG, "dtype %u is none", dtype);
-    if (weight_dtype != dtype && weight_dtype != TAPS_F32)
-        return fail(TAPS_ERR_ARG, "weight_dtype %u is neither dtype (%u) nor TAPS_F32", weight_dtype,
-                    dtype);
-    if (dim < 1 || dim > TAPS_MAX_HEAD_DIM)
-        return fail(TAPS_ERR_ARG, "head_dim %u outside 1..%u", dim, TAPS_MAX_HEAD_DIM);
-    if (rotary > dim || rotary % 2)
-        return fail(TAPS_ERR_ARG, "rotary_dim %u is odd or above head_dim %u", rotary, dim);
-    if (rotary && !table) return fail(TAPS_ERR_ARG, "rotary_dim is %u but table is NULL", rotary);
-    if (!aligned(table, 4)) return fail(TAPS_ERR_ARG, "table is not aligned to its elements");
-    if (!(eps >= 0.f) || std::isinf(eps)) return fail(TAPS_ERR_ARG, "eps is negative or not finite");
-    return TAPS_OK;
-}
-
-taps_status check_heads(const taps_heads *t, const char *what, uint32_t dtype) {
-    if (!t || !t->data) return fail(TAPS_ERR_ARG, "%s is NULL", what);
-    if (!aligned(t->data, size_of(dtype)))
-        return fail(TAPS_ERR_ARG, "%s is not aligned to its elements", what);
-    return TAPS_OK;
-}
-
-// Whether every row starts at a multiple of four elements.
-bool by_fours(const taps_heads &t, uint32_t dtype) {
-    return aligned(t.data, 4 * size_of(dtype)) && t.stride[0] % 4 == 0 && t.stride[1] % 4 == 0 &&
-           t.stride[2] % 4 == 0;
-}
-
-bool vectors_fit(uint32_t dim, uint32_t rotary, uint32_t weight_dtype, const void *w0, const void *w1,
-                 const float *table) {
-    const uint32_t w = 4 * size_of(weight_dtype);
-    return dim % 8 == 0 && rotary % 8 == 0 && aligned(w0, w) && aligned(w1, w) && aligned(table, 16);
-}
-
-void set_strides(int64_t (&to)[3], const taps_heads &t) {
-    for (int i = 0; i < 3; ++i) to[i] = t.stride[i];
-}
 
 taps_status check_norm_rotate(const taps_norm_rotate_args *a, taps_rows_launch *p) {
     if (!a) return fail(TAPS_ERR_ARG, "args is NULL");
@@ -119,8 +61,6 @@ taps_status check_norm_rotate(const taps_norm_rotate_args *a, taps_rows_launch *
 // ---------------------------------------------------------------------------
 // plans
 // ---------------------------------------------------------------------------
-
-uint64_t up16(uint64_t v) { return (v + 15) & ~15ull; }
 
 struct Sequence {
     int32_t token0;      // its first token
@@ -410,11 +350,6 @@ taps_status lay_out(const taps_paged_batch *b, uint32_t cus, Layout *out) {
     return TAPS_OK;
 }
 
-uint64_t workspace_of(const taps_plan_header &h) {
-    return up16((uint64_t)h.part_rows * h.kv_heads * h.head_dim * 4) +
-           up16((uint64_t)h.part_rows * h.kv_heads * 8);
-}
-
 void write_plan(const taps_paged_batch *b, const Layout &l, char *to) {
     const taps_plan_header &h = l.head;
     memcpy(to, &h, sizeof h);
@@ -437,15 +372,6 @@ void write_plan(const taps_paged_batch *b, const Layout &l, char *to) {
                                           (p & (b->page_size - 1)));
         }
     }
-}
-
-taps_status check_plan(const void *plan, const void *plan_device, const taps_plan_header **h) {
-    if (!plan || !plan_device) return fail(TAPS_ERR_ARG, "plan or plan_device is NULL");
-    if (!aligned(plan, 16) || !aligned(plan_device, 16))
-        return fail(TAPS_ERR_ARG, "plan or plan_device is not 16-byte aligned");
-    *h = (const taps_plan_header *)plan;
-    if ((*h)->magic != kPlanMagic) return fail(TAPS_ERR_ARG, "plan was not made by taps_paged_plan");
-    return TAPS_OK;
 }
 
 }  // namespace
@@ -612,62 +538,27 @@ taps_status taps_attend(uint32_t dtype, const void *plan, const void *plan_devic
                         const taps_heads *k_cache, const taps_heads *v_cache, float scale,
                         const taps_heads *out, float *lse, void *workspace,
                         uint64_t workspace_bytes, void *stream) {
-    if (dtype != TAPS_BF16 && dtype != TAPS_F16)
-        return fail(TAPS_ERR_ARG, "dtype %u is neither TAPS_BF16 nor TAPS_F16", dtype);
     const taps_plan_header *h;
-    if (taps_status st = check_plan(plan, plan_device, &h)) return st;
-    if (h->head_dim % 8 || h->head_dim > TAPS_MAX_ATTEND_DIM)
-        return fail(TAPS_ERR_ARG, "head_dim %u is not a multiple of 8 up to %u", h->head_dim,
-                    TAPS_MAX_ATTEND_DIM);
-    if (!(scale > 0.f) || std::isinf(scale))
-        return fail(TAPS_ERR_ARG, "scale is not positive and finite");
+    if (taps_status st = check_attend(dtype, plan, plan_device, scale, &h)) return st;
     if (!h->tokens) return TAPS_OK;
-    const taps_heads *const all[4] = {q, k_cache, v_cache, out};
-    static const char *const names[4] = {"q", "k_cache", "v_cache", "out"};
-    for (int i = 0; i < 4; ++i) {
-        const bool cache = i == 1 || i == 2;
-        if (!all[i] || !all[i]->data) return fail(TAPS_ERR_ARG, "%s is NULL", names[i]);
-        // an axis of one is not stepped along
-        const uint32_t lengths[3] = {cache ? h->n_pages : 1, cache ? h->kv_heads : h->tokens,
-                                     cache ? 2 : h->q_heads};
-        bool fits = aligned(all[i]->data, 16);
-        for (int k = 0; k < 3; ++k) fits = fits && (lengths[k] < 2 || all[i]->stride[k] % 8 == 0);
-        if (!fits)
-            return fail(TAPS_ERR_ARG, "%s: rows do not start at multiples of 16 bytes", names[i]);
+    if (taps_status st = check_rows(q, "q", h->tokens, h->q_heads)) return st;
+    const taps_heads *const caches[2] = {k_cache, v_cache};
+    for (int i = 0; i < 2; ++i) {
+        const char *const what = i ? "v_cache" : "k_cache";
+        if (taps_status st = check_rows(caches[i], what, h->kv_heads, 2, h->n_pages)) return st;
         // 16 slots' offsets are held in 32 bits
-        if (cache && (all[i]->stride[2] < 0 || all[i]->stride[2] >= (1 << 26)))
-            return fail(TAPS_ERR_ARG, "%s: slots are 2^26 elements or more apart", names[i]);
+        if (caches[i]->stride[2] < 0 || caches[i]->stride[2] >= (1 << 26))
+            return fail(TAPS_ERR_ARG, "%s: slots are 2^26 elements or more apart", what);
     }
-    if (!aligned(lse, 4)) return fail(TAPS_ERR_ARG, "lse is not aligned to its elements");
-    const uint64_t need = workspace_of(*h);
-    if (need && !workspace) return fail(TAPS_ERR_ARG, "workspace is NULL");
-    if (need > workspace_bytes)
-        return fail(TAPS_ERR_CAPACITY, "workspace of %llu bytes, %llu are needed",
-                    (unsigned long long)workspace_bytes, (unsigned long long)need);
-    if (!aligned(workspace, 16)) return fail(TAPS_ERR_ARG, "workspace is not 16-byte aligned");
+    if (taps_status st = check_rows(out, "out", h->tokens, h->q_heads)) return st;
+    if (taps_status st = check_results(*h, lse, workspace, workspace_bytes)) return st;
     taps_attend_launch p{};
-    const char *dev = (const char *)plan_device;
-    p.q = (const char *)q->data, p.out = (char *)out->data, p.lse = lse;
+    set_attend(&p, *h, plan_device, *q, scale, *out, lse, workspace);
     p.k_cache = (const char *)k_cache->data, p.v_cache = (const char *)v_cache->data;
-    p.zeros = dev + offsetof(taps_plan_header, zeros);
-    p.part_o = (float *)workspace;
-    p.part_ml = (float *)((char *)workspace +
-                          up16((uint64_t)h->part_rows * h->kv_heads * h->head_dim * 4));
-    p.pages = (const int32_t *)(dev + h->pages_at);
-    p.items = (const taps_plan_item *)(dev + h->items_at);
-    p.joins = (const taps_plan_join *)(dev + h->joins_at);
-    p.q_token = 2 * q->stride[1], p.q_head = 2 * q->stride[2];
-    p.o_token = 2 * out->stride[1], p.o_head = 2 * out->stride[2];
     p.k_page = 2 * k_cache->stride[0], p.k_head = 2 * k_cache->stride[1];
     p.k_slot = 2 * k_cache->stride[2];
     p.v_page = 2 * v_cache->stride[0], p.v_head = 2 * v_cache->stride[1];
     p.v_slot = 2 * v_cache->stride[2];
-    p.n_items = h->n_items, p.n_wide = h->n_wide;
-    p.n_joins = h->n_joins, p.join_rounds = h->join_rounds;
-    p.q_heads = h->q_heads, p.kv_heads = h->kv_heads, p.group = h->q_heads / h->kv_heads;
-    p.dim = h->head_dim;
-    p.page_log2 = h->page_log2, p.causal = h->causal, p.window = h->window;
-    p.scale = scale;
     return launched(taps_launch_attend(p, dtype, (hipStream_t)stream), "taps_attend");
 }
 

@@ -125,3 +125,5 @@ struct taps_attend_launch {
 };
 
 hipError_t taps_launch_attend(const taps_attend_launch &p, uint32_t dtype, hipStream_t stream);
+// Adds up the pieces of rows whose keys were split; nothing to do without any.
+hipError_t taps_launch_join(const taps_attend_launch &p, uint32_t dtype, hipStream_t stream);
