@@ -12,7 +12,8 @@ import sys
 from .build import ARCH, CSRC, HERE, INCLUDE, hipcc
 
 LIB = os.path.join(HERE, "libtaps_attention.so")
-SOURCES = ["taps_attention_api.hip", "taps_norm_rotate.hip", "taps_attend.hip"]
+SOURCES = ["taps_attention_api.hip", "taps_norm_rotate.hip", "taps_attend.hip", "taps_mx_api.hip",
+           "taps_mx.hip", "taps_mx_attend.hip"]
 
 
 def _commands(out: str) -> list:

@@ -1,0 +1,408 @@
+// taps_mx.hip -- the append to a cache in microscaling formats, and reading it back.
+//
+// A row is one head of one token's keys or values.  For a block of 32 elements with
+// the largest magnitude a, with e the smallest integer from -110 on with a <= L 2^e,
+//   code_i = nearest(x_i 2^-e),   x'_i = code_i 2^e.
+// a 2^-E <= L depends on a's exponent and mantissa alone: integer work on its bits.
+// The codes are the conversion instructions', which round to the nearest, the even one
+// of two, and take 2^e themselves.
+//
+// Eight elements a lane: four lanes are a block, and meet for its largest magnitude.
+// A rotated element's other half of the pair is in another lane (but for neighbouring
+// pairs); lanes hand them over through LDS, inside a wavefront.
+#include "taps_lanes.h"
+#include "taps_mx_device.h"
+#include "taps_mx_internal.h"
+
+namespace {
+
+constexpr int kThreads = 256;
+constexpr uint32_t kGridRow = 1u << 22;   // workgroups in a launch's first dimension
+__device__ __forceinline__ uint32_t workgroup() { return blockIdx.y * kGridRow + blockIdx.x; }
+dim3 grid_of(uint32_t groups) {
+    return groups <= kGridRow ? dim3(groups) : dim3(kGridRow, (groups + kGridRow - 1) / kGridRow);
+}
+
+// Elements of a lane, and lanes of a row: whole blocks, up to the next power of two.
+constexpr int kN = 8;
+int lanes_of(uint32_t dim) { return dim <= 32 ? 4 : dim <= 64 ? 8 : 16; }
+
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+
+template <class T> struct Raw {
+    typedef T v8 __attribute__((ext_vector_type(8)));
+    v8 x = {};
+};
+
+// Elements d .. d + 7 of a row of `dim`; zeros beyond it.
+template <class T, bool Vectors>
+__device__ __forceinline__ Raw<T> fetch(const T *row, int d, int dim) {
+    Raw<T> r;
+    if (Vectors) {
+        if (d < dim) r.x = *(const typename Raw<T>::v8 *)(row + d);
+    } else {
+#pragma unroll
+        for (int i = 0; i < kN; ++i)
+            if (d + i < dim) r.x[i] = row[d + i];
+    }
+    return r;
+}
+
+// cos and +-sin of a lane's elements, so that y = x cos + partner sin, and their partners'
+// places in the row; elements that are not rotated stay as they are.
+template <bool Vectors> struct Turn {
+    float c[kN], s[kN];
+    int d, half;        // first element; rotary / 2
+    bool any, all, near;   // some, all are rotated; pairs are neighbours
+    __device__ __forceinline__ Turn(const taps_mx_append_launch &p, int64_t position, int d0) {
+        d = d0, half = p.rotary / 2;
+        any = d < (int)p.rotary, all = d + kN <= (int)p.rotary;
+        near = p.interleaved;
+        const float *row = p.table + position * (int64_t)p.rotary;
+#pragma unroll
+        for (int i = 0; i < kN; ++i) c[i] = 1.f, s[i] = 0.f;
+        if (!any) return;
+        if (Vectors && !near) {   // four elements lie in one half of the pairs
+#pragma unroll
+            for (int g = 0; g < kN; g += 4) {
+                const bool b = d + g >= half;
+                const int angle = b ? d + g - half : d + g;
+                const f32x4 u = *(const f32x4 *)(row + angle), v = *(const f32x4 *)(row + half + angle);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) c[g + i] = u[i], s[g + i] = b ? v[i] : -v[i];
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < kN; ++i)
+                if (rotated(i)) {
+                    const bool b = near ? (d + i) & 1 : d + i >= half;
+                    const int angle = near ? (d + i) / 2 : b ? d + i - half : d + i;
+                    c[i] = row[angle];
+                    s[i] = b ? row[half + angle] : -row[half + angle];
+                }
+        }
+    }
+    __device__ __forceinline__ bool rotated(int i) const { return d + i < 2 * half; }
+    // Partners of elements i of this lane, from the row in LDS.
+    __device__ __forceinline__ void partners(const float *row, float (&y)[kN]) const {
+        if (Vectors) {
+#pragma unroll
+            for (int g = 0; g < kN; g += 4) {
+                const f32x4 u = *(const f32x4 *)(row + (d + g >= half ? d + g - half : d + g + half));
+#pragma unroll
+                for (int i = 0; i < 4; ++i) y[g + i] = u[i];
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < kN; ++i)
+                y[i] = rotated(i) ? row[d + i >= half ? d + i - half : d + i + half] : 0.f;
+        }
+    }
+};
+
+// 1 / sqrt(v) in 64 bits: the instruction's half precision and two steps of Newton's.
+__device__ __forceinline__ double inverse_root(double v) {
+    double y = __builtin_amdgcn_rsq(v);
+    if (v == 0.0 || v == __builtin_inf()) return y;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) y = y + 0.5 * y * __builtin_fma(-v * y, y, 1.0);
+    return y;
+}
+
+// Sum over groups of Lanes neighbouring lanes, in 64 bits.
+template <int Lanes> __device__ __forceinline__ double row_sum64(double v) {
+#pragma unroll
+    for (int m = 1; m < Lanes; m *= 2) v += __shfl_xor(v, m, 64);
+    return v;
+}
+
+// Largest of four neighbouring lanes.
+__device__ __forceinline__ uint32_t quad_max(uint32_t v) {
+    v = max(v, (uint32_t)__builtin_amdgcn_mov_dpp((int)v, 0xb1, 0xf, 0xf, true));   // 1 0 3 2
+    return max(v, (uint32_t)__builtin_amdgcn_mov_dpp((int)v, 0x4e, 0xf, 0xf, true));   // 2 3 0 1
+}
+
+// The scale byte of a block whose largest magnitude has these bits (finite).
+template <int Bits> __device__ __forceinline__ uint32_t scale_byte(uint32_t top) {
+    // L = 1.75 x 2^2, 1.8125 x 2^8
+    constexpr int kExponent = Bits == 4 ? 2 : 8;
+    constexpr uint32_t kMantissa = Bits == 4 ? 0x600000 : 0x680000;
+    const int e = (int)(top >> 23) - kExponent + ((top & 0x7fffff) > kMantissa);
+    return (uint32_t)max(e, 17);   // 2^-110
+}
+
+// Eight elements' codes: x 2^-e, rounded.
+template <int Bits>
+__device__ __forceinline__ void encode(const float (&x)[kN], float scale, uint32_t (&to)[kWords<Bits>]) {
+    if constexpr (Bits == 4) {
+        uint32_t w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(0u, x[0], x[1], scale, 0);
+        w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[2], x[3], scale, 1);
+        w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[4], x[5], scale, 2);
+        to[0] = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[6], x[7], scale, 3);
+    } else {
+        typedef short s16x2 __attribute__((ext_vector_type(2)));
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            s16x2 w = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(s16x2{}, x[4 * i], x[4 * i + 1], scale,
+                                                               false);
+            w = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(w, x[4 * i + 2], x[4 * i + 3], scale, true);
+            to[i] = __builtin_bit_cast(uint32_t, w);
+        }
+    }
+}
+
+// How a workgroup's groups of lanes share tokens and heads: `across` groups
+// take a token's heads in turns, the others take other tokens.
+struct Split {
+    uint32_t across, tokens;   // groups per token, tokens per workgroup
+    __host__ __device__ Split(uint32_t heads, int lanes) {
+        const uint32_t groups = kThreads / lanes;
+        across = groups;
+        while (across > 1 && across / 2 >= heads) across /= 2;
+        tokens = groups / across;
+    }
+};
+// Rows that a group of lanes has on their way at once.
+constexpr int kAtOnce = 4;
+
+template <class T, int Bits, bool Vectors, int Lanes>
+__global__ __launch_bounds__(kThreads) void k_mx_append(taps_mx_append_launch p) {
+    __shared__ __attribute__((aligned(16))) float lds[kThreads * kN];
+    const uint32_t heads = 2 * p.heads;
+    const Split split(heads, Lanes);
+    const uint32_t group = threadIdx.x / Lanes;
+    const uint32_t t = workgroup() * split.tokens + group / split.across;
+    if (t >= p.tokens) return;   // whole groups leave; sums and pairs stay inside a group
+    const taps_plan_token place = p.plan_tokens[t];
+    if (place.slot < 0) return;
+    const int64_t page = place.slot >> p.page_log2;
+    const int64_t slot = place.slot & ((1 << p.page_log2) - 1);
+    const int lane = threadIdx.x % Lanes, d = kN * lane, dim = p.dim;
+    const bool held = lane < 4 * (int)((p.dim + 31) / 32);   // codes of whole blocks
+    const Turn<Vectors> turn(p, place.position, d);
+    float *row = lds + group * Lanes * kN;
+    float w[kN];
+    if (p.weight) {
+        if (p.float_weight) {
+            const Raw<float> r = fetch<float, false>((const float *)p.weight, d, dim);
+#pragma unroll
+            for (int i = 0; i < kN; ++i) w[i] = r.x[i];
+        } else {
+            const Raw<T> r = fetch<T, false>((const T *)p.weight, d, dim);
+#pragma unroll
+            for (int i = 0; i < kN; ++i) w[i] = (float)r.x[i];
+        }
+    }
+    for (uint32_t h0 = group % split.across; h0 < heads; h0 += kAtOnce * split.across) {
+        Raw<T> raw[kAtOnce];
+#pragma unroll
+        for (int u = 0; u < kAtOnce; ++u) {
+            const uint32_t h = h0 + u * split.across;
+            if (h >= heads) break;
+            const bool v = h >= p.heads;
+            raw[u] = fetch<T, Vectors>(
+                (const T *)(v ? p.src[1] : p.src[0]) + t * (v ? p.src_stride[1][0] : p.src_stride[0][0]) +
+                    (v ? h - p.heads : h) * (v ? p.src_stride[1][1] : p.src_stride[0][1]),
+                d, dim);
+        }
+#pragma unroll
+        for (int u = 0; u < kAtOnce; ++u) {
+#pragma clang fp contract(off)
+            const uint32_t h = h0 + u * split.across;
+            if (h >= heads) break;
+            const bool v = h >= p.heads;
+            float x[kN];
+#pragma unroll
+            for (int i = 0; i < kN; ++i) x[i] = (float)raw[u].x[i];
+            if (!v && p.weight) {
+                double sum = 0.0;
+#pragma unroll
+                for (int i = 0; i < kN; ++i) sum = __builtin_fma((double)x[i], (double)x[i], sum);
+                const float rstd =
+                    (float)inverse_root(row_sum64<Lanes>(sum) / (double)dim + (double)p.eps);
+#pragma unroll
+                for (int i = 0; i < kN; ++i) x[i] = d + i < dim ? x[i] * rstd * w[i] : 0.f;
+            }
+            if (!v && p.rotary) {
+                float y[kN];
+                if (turn.near) {
+#pragma unroll
+                    for (int i = 0; i < kN; ++i) y[i] = x[i ^ 1];
+                } else {
+                    *(f32x4 *)(row + d) = f32x4{x[0], x[1], x[2], x[3]};
+                    *(f32x4 *)(row + d + 4) = f32x4{x[4], x[5], x[6], x[7]};
+                    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+                    __builtin_amdgcn_wave_barrier();
+                    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+                    if (turn.any) turn.partners(row, y);
+                    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+                    __builtin_amdgcn_wave_barrier();
+                    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+                }
+#pragma unroll
+                for (int i = 0; i < kN; ++i)
+                    if (turn.rotated(i)) {
+                        const float a = x[i] * turn.c[i], b = y[i] * turn.s[i];
+                        x[i] = a + b;
+                    }
+            }
+            uint32_t top = 0;
+#pragma unroll
+            for (int i = 0; i < kN; ++i)
+                top = max(top, __builtin_bit_cast(uint32_t, x[i]) & 0x7fffffff);
+            top = quad_max(top);
+            const bool finite = top < 0x7f800000;   // NaN's bits are the largest
+            top = min(top, __builtin_bit_cast(uint32_t, p.most));
+            const uint32_t byte = finite ? scale_byte<Bits>(top) : TAPS_MX_NAN;
+#pragma unroll
+            for (int i = 0; i < kN; ++i) x[i] = finite ? fminf(fmaxf(x[i], -p.most), p.most) : 0.f;
+            uint32_t code[kWords<Bits>];
+            encode<Bits>(x, mx_scale(finite ? byte : 127), code);
+            if (held) {
+                const taps_mx_place &c = p.cache[v];
+                const uint32_t hh = v ? h - p.heads : h;
+                char *to = c.codes + page * c.code_stride[0] + hh * c.code_stride[1] +
+                           slot * c.code_stride[2] + lane * Bits;
+                if constexpr (Bits == 4)
+                    *(uint32_t *)to = code[0];
+                else
+                    *(u32x2 *)to = u32x2{code[0], code[1]};
+                if (lane % 4 == 0)
+                    c.scales[page * c.scale_stride[0] + hh * c.scale_stride[1] +
+                             slot * c.scale_stride[2] + lane / 4] = (char)byte;
+            }
+        }
+    }
+}
+
+template <class T, int Bits, bool Vectors, int Lanes>
+__global__ __launch_bounds__(kThreads) void k_mx_read(taps_mx_read_launch p) {
+    const uint32_t heads = 2 * p.heads;
+    const Split split(heads, Lanes);
+    const uint32_t group = threadIdx.x / Lanes;
+    const uint32_t t = workgroup() * split.tokens + group / split.across;
+    if (t >= p.tokens) return;
+    int64_t at = p.wide_slots ? ((const int64_t *)p.slots)[t] : (int64_t)((const int32_t *)p.slots)[t];
+    const bool good = at >= 0 && at < p.n_slots;
+    if (!good) at = 0;
+    const int64_t page = at >> p.page_log2, slot = at & ((1 << p.page_log2) - 1);
+    const int lane = threadIdx.x % Lanes, d = kN * lane, dim = p.dim;
+    if (d >= dim) return;
+    for (uint32_t h0 = group % split.across; h0 < heads; h0 += kAtOnce * split.across) {
+        uint32_t code[kAtOnce][kWords<Bits>], byte[kAtOnce];
+#pragma unroll
+        for (int u = 0; u < kAtOnce; ++u) {
+            const uint32_t h = h0 + u * split.across;
+            if (h >= heads) break;
+            const bool v = h >= p.heads;
+            const taps_mx_place &c = p.cache[v];
+            const uint32_t hh = v ? h - p.heads : h;
+            const char *from = c.codes + page * c.code_stride[0] + hh * c.code_stride[1] +
+                               slot * c.code_stride[2] + lane * Bits;
+            if constexpr (Bits == 4) {
+                code[u][0] = *(const uint32_t *)from;
+            } else {
+                const u32x2 w = *(const u32x2 *)from;
+                code[u][0] = w[0], code[u][1] = w[1];
+            }
+            byte[u] = (uint8_t)c.scales[page * c.scale_stride[0] + hh * c.scale_stride[1] +
+                                        slot * c.scale_stride[2] + lane / 4];
+        }
+#pragma unroll
+        for (int u = 0; u < kAtOnce; ++u) {
+            const uint32_t h = h0 + u * split.across;
+            if (h >= heads) break;
+            const bool v = h >= p.heads;
+            const float scale = mx_scale(good ? byte[u] : TAPS_MX_NAN);
+            T *to = (T *)(v ? p.dst[1] : p.dst[0]) + t * (v ? p.dst_stride[1][0] : p.dst_stride[0][0]) +
+                    (v ? h - p.heads : h) * (v ? p.dst_stride[1][1] : p.dst_stride[0][1]) + d;
+            Raw<T> r;
+            if constexpr (sizeof(T) == 2) {
+                r.x = __builtin_bit_cast(typename Raw<T>::v8, mx_eight<T, Bits>(code[u], scale));
+            } else {
+                typedef float f32x2 __attribute__((ext_vector_type(2)));
+                f32x2 y[4];
+                if constexpr (Bits == 4) {
+                    y[0] = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(code[u][0], scale, 0);
+                    y[1] = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(code[u][0], scale, 1);
+                    y[2] = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(code[u][0], scale, 2);
+                    y[3] = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(code[u][0], scale, 3);
+                } else {
+                    y[0] = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(code[u][0], scale, false);
+                    y[1] = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(code[u][0], scale, true);
+                    y[2] = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(code[u][1], scale, false);
+                    y[3] = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(code[u][1], scale, true);
+                }
+#pragma unroll
+                for (int i = 0; i < kN; ++i) r.x[i] = y[i / 2][i % 2];
+            }
+            if (Vectors) {
+                *(typename Raw<T>::v8 *)to = r.x;
+            } else {
+#pragma unroll
+                for (int i = 0; i < kN; ++i) to[i] = r.x[i];   // head_dim is a multiple of 8
+            }
+        }
+    }
+}
+
+uint32_t groups_of(uint32_t tokens, uint32_t heads, int lanes) {
+    const uint32_t each = Split(2 * heads, lanes).tokens;
+    return (tokens + each - 1) / each;
+}
+
+// f with the element type of `dtype`, the number of bits, whether rows are read in vectors and
+// the lanes of a row, as types.
+template <int N> struct Int {
+    static constexpr int value = N;
+};
+template <class F> void choose(uint32_t dtype, uint32_t bits, bool vectors, int lanes, F &&f) {
+    const auto by_lanes = [&](auto type, auto b, auto vec) {
+        if (lanes == 4)
+            f(type, b, vec, Int<4>{});
+        else if (lanes == 8)
+            f(type, b, vec, Int<8>{});
+        else
+            f(type, b, vec, Int<16>{});
+    };
+    const auto by_vectors = [&](auto type, auto b) {
+        if (vectors)
+            by_lanes(type, b, Int<1>{});
+        else
+            by_lanes(type, b, Int<0>{});
+    };
+    const auto by_bits = [&](auto type) {
+        if (bits == 4)
+            by_vectors(type, Int<4>{});
+        else
+            by_vectors(type, Int<8>{});
+    };
+    if (dtype == TAPS_BF16)
+        by_bits((__bf16)0.f);
+    else if (dtype == TAPS_F16)
+        by_bits((_Float16)0.f);
+    else
+        by_bits(0.f);
+}
+
+}  // namespace
+
+hipError_t taps_launch_mx_append(const taps_mx_append_launch &p, uint32_t dtype, uint32_t bits,
+                                 bool vectors, hipStream_t stream) {
+    const int lanes = lanes_of(p.dim);
+    choose(dtype, bits, vectors, lanes, [&](auto type, auto b, auto vec, auto n) {
+        k_mx_append<decltype(type), b.value, vec.value != 0, n.value>
+            <<<grid_of(groups_of(p.tokens, p.heads, lanes)), kThreads, 0, stream>>>(p);
+    });
+    return hipGetLastError();
+}
+
+hipError_t taps_launch_mx_read(const taps_mx_read_launch &p, uint32_t dtype, uint32_t bits,
+                               bool vectors, hipStream_t stream) {
+    const int lanes = lanes_of(p.dim);
+    choose(dtype, bits, vectors, lanes, [&](auto type, auto b, auto vec, auto n) {
+        k_mx_read<decltype(type), b.value, vec.value != 0, n.value>
+            <<<grid_of(groups_of(p.tokens, p.heads, lanes)), kThreads, 0, stream>>>(p);
+    });
+    return hipGetLastError();
+}
