@@ -19,8 +19,9 @@ namespace {
 constexpr int kThreads = 256;
 constexpr uint32_t kGridRow = 1u << 22;   // workgroups in a launch's first dimension
 __device__ __forceinline__ uint32_t workgroup() { return blockIdx.y * kGridRow + blockIdx.x; }
-dim3 grid_of(uint32_t groups) {
-    return groups <= kGridRow ? dim3(groups) : dim3(kGridRow, (groups + kGridRow - 1) / kGridRow);
+dim3 grid_of(uint32_t groups) {   // of keys, and of values
+    return groups <= kGridRow ? dim3(groups, 1, 2)
+                              : dim3(kGridRow, (groups + kGridRow - 1) / kGridRow, 2);
 }
 
 // Elements of a lane, and lanes of a row: whole blocks, up to the next power of two.
@@ -53,15 +54,13 @@ __device__ __forceinline__ Raw<T> fetch(const T *row, int d, int dim) {
 template <bool Vectors> struct Turn {
     float c[kN], s[kN];
     int d, half;        // first element; rotary / 2
-    bool any, all, near;   // some, all are rotated; pairs are neighbours
-    __device__ __forceinline__ Turn(const taps_mx_append_launch &p, int64_t position, int d0) {
+    __device__ __forceinline__ void start(const taps_mx_append_launch &p, int64_t position, int d0) {
         d = d0, half = p.rotary / 2;
-        any = d < (int)p.rotary, all = d + kN <= (int)p.rotary;
-        near = p.interleaved;
+        const bool near = p.interleaved;   // pairs are neighbours
         const float *row = p.table + position * (int64_t)p.rotary;
 #pragma unroll
         for (int i = 0; i < kN; ++i) c[i] = 1.f, s[i] = 0.f;
-        if (!any) return;
+        if (d >= (int)p.rotary) return;
         if (Vectors && !near) {   // four elements lie in one half of the pairs
 #pragma unroll
             for (int g = 0; g < kN; g += 4) {
@@ -88,7 +87,8 @@ template <bool Vectors> struct Turn {
         if (Vectors) {
 #pragma unroll
             for (int g = 0; g < kN; g += 4) {
-                const f32x4 u = *(const f32x4 *)(row + (d + g >= half ? d + g - half : d + g + half));
+                const int at = d + g >= half ? d + g - half : d + g + half;
+                const f32x4 u = *(const f32x4 *)(row + (rotated(g) ? at : 0));
 #pragma unroll
                 for (int i = 0; i < 4; ++i) y[g + i] = u[i];
             }
@@ -151,27 +151,17 @@ __device__ __forceinline__ void encode(const float (&x)[kN], float scale, uint32
     }
 }
 
-// How a workgroup's groups of lanes share tokens and heads: `across` groups
-// take a token's heads in turns, the others take other tokens.
-struct Split {
-    uint32_t across, tokens;   // groups per token, tokens per workgroup
-    __host__ __device__ Split(uint32_t heads, int lanes) {
-        const uint32_t groups = kThreads / lanes;
-        across = groups;
-        while (across > 1 && across / 2 >= heads) across /= 2;
-        tokens = groups / across;
-    }
-};
-// Rows that a group of lanes has on their way at once.
-constexpr int kAtOnce = 4;
+// A workgroup's groups of lanes: `across` of them share a token's heads, the others take
+// other tokens; keys and values are other workgroups' (blockIdx.z).
+// Rows that a group has on their way at once.
+constexpr int kAppendAtOnce = 4, kReadAtOnce = 8;
+constexpr uint64_t kFill = 1024;   // workgroups that fill the card
 
 template <class T, int Bits, bool Vectors, int Lanes>
 __global__ __launch_bounds__(kThreads) void k_mx_append(taps_mx_append_launch p) {
     __shared__ __attribute__((aligned(16))) float lds[kThreads * kN];
-    const uint32_t heads = 2 * p.heads;
-    const Split split(heads, Lanes);
-    const uint32_t group = threadIdx.x / Lanes;
-    const uint32_t t = workgroup() * split.tokens + group / split.across;
+    const uint32_t side = blockIdx.z, across = p.across, group = threadIdx.x / Lanes;
+    const uint32_t t = workgroup() * (kThreads / Lanes / across) + group / across;
     if (t >= p.tokens) return;   // whole groups leave; sums and pairs stay inside a group
     const taps_plan_token place = p.plan_tokens[t];
     if (place.slot < 0) return;
@@ -179,10 +169,21 @@ __global__ __launch_bounds__(kThreads) void k_mx_append(taps_mx_append_launch p)
     const int64_t slot = place.slot & ((1 << p.page_log2) - 1);
     const int lane = threadIdx.x % Lanes, d = kN * lane, dim = p.dim;
     const bool held = lane < 4 * (int)((p.dim + 31) / 32);   // codes of whole blocks
-    const Turn<Vectors> turn(p, place.position, d);
+    const uint32_t h_first = group % across;
+    const T *from = (const T *)p.src[side] + t * p.src_stride[side][0] + h_first * p.src_stride[side][1];
+    const taps_mx_place &c = p.cache[side];
+    char *codes = c.codes + page * c.code_stride[0] + slot * c.code_stride[2] +
+                  h_first * c.code_stride[1] + lane * Bits;
+    char *scales = c.scales + page * c.scale_stride[0] + slot * c.scale_stride[2] +
+                   h_first * c.scale_stride[1] + lane / 4;
+    const int64_t from_step = across * p.src_stride[side][1];
+    const int64_t code_step = across * c.code_stride[1], scale_step = across * c.scale_stride[1];
+    const bool norms = side == 0 && p.weight, rotates = side == 0 && p.rotary;
+    Turn<Vectors> turn;
+    if (rotates) turn.start(p, place.position, d);
     float *row = lds + group * Lanes * kN;
     float w[kN];
-    if (p.weight) {
+    if (norms) {
         if (p.float_weight) {
             const Raw<float> r = fetch<float, false>((const float *)p.weight, d, dim);
 #pragma unroll
@@ -193,28 +194,21 @@ __global__ __launch_bounds__(kThreads) void k_mx_append(taps_mx_append_launch p)
             for (int i = 0; i < kN; ++i) w[i] = (float)r.x[i];
         }
     }
-    for (uint32_t h0 = group % split.across; h0 < heads; h0 += kAtOnce * split.across) {
-        Raw<T> raw[kAtOnce];
+    for (uint32_t h0 = h_first; h0 < p.heads; h0 += kAppendAtOnce * across) {
+        Raw<T> raw[kAppendAtOnce];
 #pragma unroll
-        for (int u = 0; u < kAtOnce; ++u) {
-            const uint32_t h = h0 + u * split.across;
-            if (h >= heads) break;
-            const bool v = h >= p.heads;
-            raw[u] = fetch<T, Vectors>(
-                (const T *)(v ? p.src[1] : p.src[0]) + t * (v ? p.src_stride[1][0] : p.src_stride[0][0]) +
-                    (v ? h - p.heads : h) * (v ? p.src_stride[1][1] : p.src_stride[0][1]),
-                d, dim);
+        for (int u = 0; u < kAppendAtOnce; ++u) {
+            if (h0 + u * across < p.heads) raw[u] = fetch<T, Vectors>(from, d, dim);
+            from += from_step;
         }
 #pragma unroll
-        for (int u = 0; u < kAtOnce; ++u) {
+        for (int u = 0; u < kAppendAtOnce; ++u) {
 #pragma clang fp contract(off)
-            const uint32_t h = h0 + u * split.across;
-            if (h >= heads) break;
-            const bool v = h >= p.heads;
+            if (h0 + u * across >= p.heads) break;
             float x[kN];
 #pragma unroll
             for (int i = 0; i < kN; ++i) x[i] = (float)raw[u].x[i];
-            if (!v && p.weight) {
+            if (norms) {
                 double sum = 0.0;
 #pragma unroll
                 for (int i = 0; i < kN; ++i) sum = __builtin_fma((double)x[i], (double)x[i], sum);
@@ -223,9 +217,9 @@ __global__ __launch_bounds__(kThreads) void k_mx_append(taps_mx_append_launch p)
 #pragma unroll
                 for (int i = 0; i < kN; ++i) x[i] = d + i < dim ? x[i] * rstd * w[i] : 0.f;
             }
-            if (!v && p.rotary) {
+            if (rotates) {
                 float y[kN];
-                if (turn.near) {
+                if (p.interleaved) {
 #pragma unroll
                     for (int i = 0; i < kN; ++i) y[i] = x[i ^ 1];
                 } else {
@@ -234,17 +228,16 @@ __global__ __launch_bounds__(kThreads) void k_mx_append(taps_mx_append_launch p)
                     __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
                     __builtin_amdgcn_wave_barrier();
                     __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
-                    if (turn.any) turn.partners(row, y);
+                    turn.partners(row, y);
                     __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
                     __builtin_amdgcn_wave_barrier();
                     __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
                 }
 #pragma unroll
-                for (int i = 0; i < kN; ++i)
-                    if (turn.rotated(i)) {
-                        const float a = x[i] * turn.c[i], b = y[i] * turn.s[i];
-                        x[i] = a + b;
-                    }
+                for (int i = 0; i < kN; ++i) {
+                    const float a = x[i] * turn.c[i], b = y[i] * turn.s[i];
+                    x[i] = turn.rotated(i) ? a + b : x[i];
+                }
             }
             uint32_t top = 0;
 #pragma unroll
@@ -259,95 +252,104 @@ __global__ __launch_bounds__(kThreads) void k_mx_append(taps_mx_append_launch p)
             uint32_t code[kWords<Bits>];
             encode<Bits>(x, mx_scale(finite ? byte : 127), code);
             if (held) {
-                const taps_mx_place &c = p.cache[v];
-                const uint32_t hh = v ? h - p.heads : h;
-                char *to = c.codes + page * c.code_stride[0] + hh * c.code_stride[1] +
-                           slot * c.code_stride[2] + lane * Bits;
                 if constexpr (Bits == 4)
-                    *(uint32_t *)to = code[0];
+                    *(uint32_t *)codes = code[0];
                 else
-                    *(u32x2 *)to = u32x2{code[0], code[1]};
-                if (lane % 4 == 0)
-                    c.scales[page * c.scale_stride[0] + hh * c.scale_stride[1] +
-                             slot * c.scale_stride[2] + lane / 4] = (char)byte;
+                    *(u32x2 *)codes = u32x2{code[0], code[1]};
+                if (lane % 4 == 0) *scales = (char)byte;
             }
+            codes += code_step, scales += scale_step;
         }
+    }
+}
+
+// Eight codes in the type T.
+template <class T, int Bits>
+__device__ __forceinline__ typename Raw<T>::v8 decode(const uint32_t *code, float scale) {
+    if constexpr (sizeof(T) == 2) {
+        return __builtin_bit_cast(typename Raw<T>::v8, mx_eight<T, Bits>(code, scale));
+    } else {
+        typedef float f32x2 __attribute__((ext_vector_type(2)));
+        f32x2 y[4];
+        if constexpr (Bits == 4) {
+            y[0] = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(code[0], scale, 0);
+            y[1] = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(code[0], scale, 1);
+            y[2] = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(code[0], scale, 2);
+            y[3] = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(code[0], scale, 3);
+        } else {
+            y[0] = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(code[0], scale, false);
+            y[1] = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(code[0], scale, true);
+            y[2] = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(code[1], scale, false);
+            y[3] = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(code[1], scale, true);
+        }
+        typename Raw<T>::v8 x;
+#pragma unroll
+        for (int i = 0; i < kN; ++i) x[i] = y[i / 2][i % 2];
+        return x;
     }
 }
 
 template <class T, int Bits, bool Vectors, int Lanes>
 __global__ __launch_bounds__(kThreads) void k_mx_read(taps_mx_read_launch p) {
-    const uint32_t heads = 2 * p.heads;
-    const Split split(heads, Lanes);
-    const uint32_t group = threadIdx.x / Lanes;
-    const uint32_t t = workgroup() * split.tokens + group / split.across;
+    const uint32_t side = blockIdx.z, across = p.across, group = threadIdx.x / Lanes;
+    const uint32_t t = workgroup() * (kThreads / Lanes / across) + group / across;
     if (t >= p.tokens) return;
     int64_t at = p.wide_slots ? ((const int64_t *)p.slots)[t] : (int64_t)((const int32_t *)p.slots)[t];
     const bool good = at >= 0 && at < p.n_slots;
     if (!good) at = 0;
     const int64_t page = at >> p.page_log2, slot = at & ((1 << p.page_log2) - 1);
-    const int lane = threadIdx.x % Lanes, d = kN * lane, dim = p.dim;
-    if (d >= dim) return;
-    for (uint32_t h0 = group % split.across; h0 < heads; h0 += kAtOnce * split.across) {
-        uint32_t code[kAtOnce][kWords<Bits>], byte[kAtOnce];
+    const int lane = threadIdx.x % Lanes, d = kN * lane;
+    if (d >= (int)p.dim) return;
+    const uint32_t h_first = group % across;
+    const taps_mx_place &c = p.cache[side];
+    const char *codes = c.codes + page * c.code_stride[0] + slot * c.code_stride[2] +
+                        h_first * c.code_stride[1] + lane * Bits;
+    const char *scales = c.scales + page * c.scale_stride[0] + slot * c.scale_stride[2] +
+                         h_first * c.scale_stride[1] + lane / 4;
+    T *to = (T *)p.dst[side] + t * p.dst_stride[side][0] + h_first * p.dst_stride[side][1] + d;
+    const int64_t code_step = across * c.code_stride[1], scale_step = across * c.scale_stride[1];
+    const int64_t to_step = across * p.dst_stride[side][1];
+    for (uint32_t h0 = h_first; h0 < p.heads; h0 += kReadAtOnce * across) {
+        uint32_t code[kReadAtOnce][kWords<Bits>], byte[kReadAtOnce];
 #pragma unroll
-        for (int u = 0; u < kAtOnce; ++u) {
-            const uint32_t h = h0 + u * split.across;
-            if (h >= heads) break;
-            const bool v = h >= p.heads;
-            const taps_mx_place &c = p.cache[v];
-            const uint32_t hh = v ? h - p.heads : h;
-            const char *from = c.codes + page * c.code_stride[0] + hh * c.code_stride[1] +
-                               slot * c.code_stride[2] + lane * Bits;
-            if constexpr (Bits == 4) {
-                code[u][0] = *(const uint32_t *)from;
-            } else {
-                const u32x2 w = *(const u32x2 *)from;
-                code[u][0] = w[0], code[u][1] = w[1];
+        for (int u = 0; u < kReadAtOnce; ++u) {
+            if (h0 + u * across < p.heads) {
+                if constexpr (Bits == 4) {
+                    code[u][0] = *(const uint32_t *)codes;
+                } else {
+                    const u32x2 w = *(const u32x2 *)codes;
+                    code[u][0] = w[0], code[u][1] = w[1];
+                }
+                byte[u] = (uint8_t)*scales;
             }
-            byte[u] = (uint8_t)c.scales[page * c.scale_stride[0] + hh * c.scale_stride[1] +
-                                        slot * c.scale_stride[2] + lane / 4];
+            codes += code_step, scales += scale_step;
         }
 #pragma unroll
-        for (int u = 0; u < kAtOnce; ++u) {
-            const uint32_t h = h0 + u * split.across;
-            if (h >= heads) break;
-            const bool v = h >= p.heads;
-            const float scale = mx_scale(good ? byte[u] : TAPS_MX_NAN);
-            T *to = (T *)(v ? p.dst[1] : p.dst[0]) + t * (v ? p.dst_stride[1][0] : p.dst_stride[0][0]) +
-                    (v ? h - p.heads : h) * (v ? p.dst_stride[1][1] : p.dst_stride[0][1]) + d;
-            Raw<T> r;
-            if constexpr (sizeof(T) == 2) {
-                r.x = __builtin_bit_cast(typename Raw<T>::v8, mx_eight<T, Bits>(code[u], scale));
-            } else {
-                typedef float f32x2 __attribute__((ext_vector_type(2)));
-                f32x2 y[4];
-                if constexpr (Bits == 4) {
-                    y[0] = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(code[u][0], scale, 0);
-                    y[1] = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(code[u][0], scale, 1);
-                    y[2] = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(code[u][0], scale, 2);
-                    y[3] = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(code[u][0], scale, 3);
-                } else {
-                    y[0] = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(code[u][0], scale, false);
-                    y[1] = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(code[u][0], scale, true);
-                    y[2] = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(code[u][1], scale, false);
-                    y[3] = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(code[u][1], scale, true);
-                }
-#pragma unroll
-                for (int i = 0; i < kN; ++i) r.x[i] = y[i / 2][i % 2];
-            }
+        for (int u = 0; u < kReadAtOnce; ++u) {
+            if (h0 + u * across >= p.heads) break;
+            const typename Raw<T>::v8 x =
+                decode<T, Bits>(code[u], mx_scale(good ? byte[u] : TAPS_MX_NAN));
             if (Vectors) {
-                *(typename Raw<T>::v8 *)to = r.x;
+                __builtin_nontemporal_store(x, (typename Raw<T>::v8 *)to);
             } else {
 #pragma unroll
-                for (int i = 0; i < kN; ++i) to[i] = r.x[i];   // head_dim is a multiple of 8
+                for (int i = 0; i < kN; ++i) to[i] = x[i];   // head_dim is a multiple of 8
             }
+            to += to_step;
         }
     }
 }
 
-uint32_t groups_of(uint32_t tokens, uint32_t heads, int lanes) {
-    const uint32_t each = Split(2 * heads, lanes).tokens;
+// Groups of lanes for a token's heads, a power of two: one, so that neighbouring groups read and
+// write neighbouring slots, unless the launch would not fill the card then.
+uint32_t across_of(uint32_t tokens, uint32_t heads, int lanes) {
+    const uint32_t groups = kThreads / lanes;
+    uint32_t across = 1;
+    while (across < groups && across < heads && 2 * (uint64_t)tokens * across < kFill * groups) across *= 2;
+    return across;
+}
+uint32_t workgroups_of(uint32_t tokens, uint32_t across, int lanes) {
+    const uint32_t each = kThreads / lanes / across;
     return (tokens + each - 1) / each;
 }
 
@@ -387,22 +389,24 @@ template <class F> void choose(uint32_t dtype, uint32_t bits, bool vectors, int 
 
 }  // namespace
 
-hipError_t taps_launch_mx_append(const taps_mx_append_launch &p, uint32_t dtype, uint32_t bits,
+hipError_t taps_launch_mx_append(taps_mx_append_launch p, uint32_t dtype, uint32_t bits,
                                  bool vectors, hipStream_t stream) {
     const int lanes = lanes_of(p.dim);
+    p.across = across_of(p.tokens, p.heads, lanes);
     choose(dtype, bits, vectors, lanes, [&](auto type, auto b, auto vec, auto n) {
         k_mx_append<decltype(type), b.value, vec.value != 0, n.value>
-            <<<grid_of(groups_of(p.tokens, p.heads, lanes)), kThreads, 0, stream>>>(p);
+            <<<grid_of(workgroups_of(p.tokens, p.across, lanes)), kThreads, 0, stream>>>(p);
     });
     return hipGetLastError();
 }
 
-hipError_t taps_launch_mx_read(const taps_mx_read_launch &p, uint32_t dtype, uint32_t bits,
+hipError_t taps_launch_mx_read(taps_mx_read_launch p, uint32_t dtype, uint32_t bits,
                                bool vectors, hipStream_t stream) {
     const int lanes = lanes_of(p.dim);
+    p.across = across_of(p.tokens, p.heads, lanes);
     choose(dtype, bits, vectors, lanes, [&](auto type, auto b, auto vec, auto n) {
         k_mx_read<decltype(type), b.value, vec.value != 0, n.value>
-            <<<grid_of(groups_of(p.tokens, p.heads, lanes)), kThreads, 0, stream>>>(p);
+            <<<grid_of(workgroups_of(p.tokens, p.across, lanes)), kThreads, 0, stream>>>(p);
     });
     return hipGetLastError();
 }

@@ -18,6 +18,7 @@ struct taps_mx_append_launch {
     const float *table;
     const taps_plan_token *plan_tokens;
     uint32_t tokens, heads, dim, rotary, page_log2;
+    uint32_t across;   // set by the launch
     float eps, most;   // most: magnitudes above it are taken for it
     uint8_t interleaved, float_weight;
 };
@@ -29,6 +30,7 @@ struct taps_mx_read_launch {
     const void *slots;
     int64_t n_slots;
     uint32_t tokens, heads, dim, page_log2;
+    uint32_t across;   // set by the launch
     uint8_t wide_slots;
 };
 
@@ -39,10 +41,10 @@ struct taps_mx_attend_launch : taps_attend_launch {
 };
 
 // vectors: rows start at multiples of eight elements, rotary_dim is a multiple of 8.
-hipError_t taps_launch_mx_append(const taps_mx_append_launch &p, uint32_t dtype, uint32_t bits,
+hipError_t taps_launch_mx_append(taps_mx_append_launch p, uint32_t dtype, uint32_t bits,
                                  bool vectors, hipStream_t stream);
 // vectors: rows start at multiples of eight elements.
-hipError_t taps_launch_mx_read(const taps_mx_read_launch &p, uint32_t dtype, uint32_t bits,
+hipError_t taps_launch_mx_read(taps_mx_read_launch p, uint32_t dtype, uint32_t bits,
                                bool vectors, hipStream_t stream);
 hipError_t taps_launch_mx_attend(const taps_mx_attend_launch &p, uint32_t dtype, uint32_t bits,
                                  hipStream_t stream);

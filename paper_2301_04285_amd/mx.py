@@ -17,7 +17,7 @@ from __future__ import annotations
 import ctypes as C
 import os
 import re
-from typing import List, NamedTuple
+from typing import List
 
 import torch
 
@@ -71,61 +71,77 @@ def declared_symbols() -> List[str]:
     return sorted(set(re.findall(r"^\s*taps_status\s*(taps_\w+)\s*\(", text, flags=re.M)))
 
 
-class MxPages(NamedTuple):
+class MxPages:
     """Pages of keys or of values: codes and scales, 8-bit unsigned tensors [pages, kv_heads,
     page_size, bytes] of any strides but the last.  A slot has a byte of ``scales`` for every 32
-    elements of a head, and 16 (4 bits) or 32 (8 bits) of ``codes``."""
-    codes: torch.Tensor
-    scales: torch.Tensor
+    elements of a head, and 16 (4 bits) or 32 (8 bits) of ``codes``.  They are looked at once,
+    here: what they hold may change, their sizes and places may not."""
 
-    @property
-    def bits(self) -> int:
-        return self.codes.shape[-1] // (4 * self.scales.shape[-1])
+    __slots__ = "codes", "scales", "bits", "_n", "_shape", "_device", "_at"
+
+    def __init__(self, codes: torch.Tensor, scales: torch.Tensor):
+        for x, name in ((codes, "codes"), (scales, "scales")):
+            if x.dtype is not torch.uint8:
+                raise ValueError(f"{name} are {x.dtype}, not 8-bit unsigned")
+            if x.dim() != 4:
+                raise ValueError(f"{name} are {tuple(x.shape)}, not pages")
+            if x.stride(3) != 1 and x.shape[3] > 1:
+                raise ValueError(f"the {name} of a slot are not contiguous")
+        if scales.shape[:3] != codes.shape[:3] or scales.device != codes.device:
+            raise ValueError(f"codes {tuple(codes.shape)} on {codes.device} beside scales "
+                             f"{tuple(scales.shape)} on {scales.device}")
+        *pages, blocks = scales.shape
+        self.bits = codes.shape[3] // (4 * blocks) if blocks else 0
+        if self.bits not in (4, 8) or codes.shape[3] != 4 * self.bits * blocks:
+            raise ValueError(f"codes of {codes.shape[3]} bytes are not 4 or 8 bits of {blocks} "
+                             f"blocks of {BLOCK} elements")
+        self.codes, self.scales = codes, scales
+        self._n, self._shape = pages[0], (pages[1], pages[2], blocks)
+        self._device = codes.get_device() if codes.is_cuda else None
+        self._at = Pages(codes.data_ptr(), codes.stride()[:3], scales.data_ptr(),
+                         scales.stride()[:3])
+
+    def __iter__(self):
+        return iter((self.codes, self.scales))
+
+    def __repr__(self):
+        n, (heads, size, blocks) = self._n, self._shape
+        return (f"MxPages({n} pages of {size} slots, {heads} heads of {blocks} blocks, "
+                f"{self.bits} bits)")
 
 
-def _format(head_dim: int, bits: int) -> int:
-    """Blocks of a head."""
-    if bits not in (4, 8):
-        raise ValueError(f"bits {bits} is neither 4 nor 8")
-    if head_dim < 1:
-        raise ValueError(f"head_dim {head_dim} is not positive")
+def _blocks(head_dim: int) -> int:
     return -(-head_dim // BLOCK)
 
 
 def new_pages(n_pages: int, kv_heads: int, page_size: int, head_dim: int, bits: int,
               device="cuda") -> MxPages:
     """Pages of zeros."""
-    blocks = _format(head_dim, bits)
+    if bits not in (4, 8):
+        raise ValueError(f"bits {bits} is neither 4 nor 8")
+    if head_dim < 1:
+        raise ValueError(f"head_dim {head_dim} is not positive")
+    blocks = _blocks(head_dim)
     return MxPages(*(torch.zeros((n_pages, kv_heads, page_size, n), dtype=torch.uint8, device=device)
                      for n in (4 * bits * blocks, blocks)))
 
 
-def _pages(t, what: str, device: int, n_pages: int, shape, bits: int):
-    """(Pages, bits) of at least ``n_pages`` pages of ``shape`` = (kv_heads, page_size, head_dim);
-    bits 0: as they are."""
-    codes, scales = t
-    blocks = -(-shape[2] // BLOCK)
-    held = codes.shape[-1] // (4 * blocks) if codes.dim() == 4 else 0
-    if held not in (4, 8) or (bits and held != bits):
-        raise ValueError(f"{what}: codes {tuple(codes.shape)} are not {bits or '4 or 8'} bits of "
-                         f"{shape[2]} elements")
-    n = codes.shape[0]
-    for x, name, size in ((codes, "codes", 4 * held * blocks), (scales, "scales", blocks)):
-        if x.dtype is not torch.uint8:
-            raise ValueError(f"{what}: {name} are {x.dtype}, not 8-bit unsigned")
-        if n < n_pages or x.shape != (n, shape[0], shape[1], size):
-            raise ValueError(f"{what}: {name} are {tuple(x.shape)}, not at least {n_pages} x "
-                             f"{(*shape[:2], size)}")
-        _on_gpu(x, f"{what}: {name}", device)
-        if x.stride(3) != 1 and size > 1:
-            raise ValueError(f"{what}: the {name} of a slot are not contiguous")
-    return Pages(codes.data_ptr(), codes.stride()[:3], scales.data_ptr(), scales.stride()[:3]), held
+def _fits(pages: MxPages, what: str, device: int, n_pages: int, shape) -> Pages:
+    """shape: (kv_heads, page_size, blocks)."""
+    if pages._n < n_pages or pages._shape != shape:
+        raise ValueError(f"{what} is {pages}, not at least {n_pages} pages of {shape[1]} slots, "
+                         f"{shape[0]} heads of {shape[2]} blocks")
+    if pages._device != device:
+        _on_gpu(pages.codes, what, device)
+    return pages._at
 
 
-def _caches(k_cache, v_cache, device: int, n_pages: int, shape):
-    k, bits = _pages(k_cache, "k_cache", device, n_pages, shape, 0)
-    v, _ = _pages(v_cache, "v_cache", device, n_pages, shape, bits)
-    return k, v, bits
+def _caches(k_cache: MxPages, v_cache: MxPages, device: int, n_pages: int, shape):
+    shape = shape[0], shape[1], _blocks(shape[2])
+    if k_cache.bits != v_cache.bits:
+        raise ValueError(f"keys of {k_cache.bits} bits beside values of {v_cache.bits}")
+    return (_fits(k_cache, "k_cache", device, n_pages, shape),
+            _fits(v_cache, "v_cache", device, n_pages, shape))
 
 
 def taps_mx_append(k, v, k_cache: MxPages, v_cache: MxPages, plan: PagedPlan, table=None,
@@ -143,9 +159,9 @@ def taps_mx_append(k, v, k_cache: MxPages, v_cache: MxPages, plan: PagedPlan, ta
         kw = _vector(k_weight, "k_weight", plan.head_dim, device, dtype)
         weight = _DTYPES[k_weight.dtype]
     args = AppendArgs(code, weight, rotary, 1 if interleaved else 0, eps, kw, at, rows)
-    kc, vc, bits = _caches(k_cache, v_cache, device, plan.n_pages, plan._page_shape)
+    kc, vc = _caches(k_cache, v_cache, device, plan.n_pages, plan._page_shape)
     _check(load().taps_mx_append(
-        C.byref(args), bits, *plan.pointers(stream, raw, device),
+        C.byref(args), k_cache.bits, *plan.pointers(stream, raw, device),
         _heads(k, "k", device, dtype, plan._k_shape, 3),
         _heads(v, "v", device, dtype, plan._k_shape, 3), kc, vc, raw), "taps_mx_append")
 
@@ -161,18 +177,17 @@ def taps_mx_read(k_cache: MxPages, v_cache: MxPages, slots, head_dim: int, dtype
             slots.dtype not in (torch.int32, torch.int64):
         raise ValueError("slots is not a contiguous vector of integers")
     _on_gpu(slots, "slots", device)
-    if k_cache.codes.dim() != 4:
-        raise ValueError(f"k_cache: codes {tuple(k_cache.codes.shape)} are not pages")
-    n_pages, heads, page_size = k_cache.codes.shape[:3]
-    kc, vc, bits = _caches(k_cache, v_cache, device, n_pages, (heads, page_size, head_dim))
+    heads, page_size, _ = k_cache._shape
+    n_pages = k_cache._n
+    kc, vc = _caches(k_cache, v_cache, device, n_pages, (heads, page_size, head_dim))
     shape = slots.shape[0], heads, head_dim
     if out is None:
-        k, v = _on(stream, lambda: [torch.empty(shape, dtype=dtype, device=slots.device)
-                                    for _ in range(2)])
+        # one piece of memory: an allocation less
+        k, v = _on(stream, lambda: torch.empty((2, *shape), dtype=dtype, device=slots.device)).unbind()
     else:
         k, v = out
         dtype = k.dtype
-    args = ReadArgs(_dtype(k), bits, shape[0], heads, head_dim, page_size, n_pages,
+    args = ReadArgs(_dtype(k), k_cache.bits, shape[0], heads, head_dim, page_size, n_pages,
                     slots.element_size(), slots.data_ptr())
     _check(load().taps_mx_read(C.byref(args), kc, vc, _heads(k, "k", device, dtype, shape, 3),
                                _heads(v, "v", device, dtype, shape, 3), raw), "taps_mx_read")
@@ -189,7 +204,7 @@ def taps_mx_attend(q, k_cache: MxPages, v_cache: MxPages, plan: PagedPlan, scale
     device, raw, dtype, shape = _device(), _stream(stream), q.dtype, plan._q_shape
     code = _dtype(q)
     qh = _heads(q, "q", device, dtype, shape, 3)
-    kc, vc, bits = _caches(k_cache, v_cache, device, plan.n_pages, plan._page_shape)
+    kc, vc = _caches(k_cache, v_cache, device, plan.n_pages, plan._page_shape)
     n = plan.workspace_bytes
     sums = workspace = None
     given = out
@@ -202,7 +217,7 @@ def taps_mx_attend(q, k_cache: MxPages, v_cache: MxPages, plan: PagedPlan, scale
     if n:
         workspace = _on(stream, lambda: torch.empty(n, dtype=torch.uint8, device=q.device))
     _check(load().taps_mx_attend(
-        code, bits, *plan.pointers(stream, raw, device), qh, kc, vc,
+        code, k_cache.bits, *plan.pointers(stream, raw, device), qh, kc, vc,
         plan.head_dim ** -0.5 if scale is None else scale, oh,
         None if sums is None else sums.data_ptr(),
         None if workspace is None else workspace.data_ptr(), n, raw), "taps_mx_attend")

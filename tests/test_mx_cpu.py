@@ -148,6 +148,24 @@ def test_pages():
         mx.new_pages(3, 2, 16, 0, 4, device="cpu")
 
 
+def test_pages_refusals():
+    def zeros(*shape, dtype=torch.uint8):
+        return torch.zeros(shape, dtype=dtype)
+    codes, scales = zeros(3, 2, 16, 64), zeros(3, 2, 16, 4)
+    for match, c, s in [("codes are torch.int8", codes.char(), scales),
+                        ("scales are torch.float32", codes, scales.float()),
+                        ("not pages", codes[0], scales), ("not pages", codes, scales[0]),
+                        ("codes of a slot", zeros(3, 2, 64, 16).transpose(2, 3), scales),
+                        ("scales of a slot", codes, zeros(3, 2, 4, 16).transpose(2, 3)),
+                        ("beside scales", codes, scales[:2]), ("beside scales", codes[:, :1], scales),
+                        ("beside scales", codes[:, :, :8], scales),
+                        ("not 4 or 8 bits", codes[..., :48], scales),
+                        ("not 4 or 8 bits", codes[..., :63], scales[..., :3]),
+                        ("not 4 or 8 bits", codes, scales[..., :0])]:
+        with pytest.raises(ValueError, match=match):
+            mx.MxPages(c, s)
+
+
 @pytest.mark.parametrize("bits", [4, 8])
 def test_reference_codes(bits):
     """Every number that a code stands for is held as it is; others move to a neighbour that no
