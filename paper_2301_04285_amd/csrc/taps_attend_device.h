@@ -514,67 +514,32 @@ template <int D> constexpr int narrow_bytes() {
            kWaves * kNarrowRows * 2 * 4;
 }
 
-// The results of a narrow item's wavefronts, each of which had all its rows and every fourth tile
-// of 32 keys from `start` on, are joined in LDS and written.
-template <class T, int D, class Cache>
-__device__ __forceinline__ void join_waves(const taps_attend_launch &p, const taps_plan_item &item,
-                                           const Cache &cache, uint32_t head, Rows<T, D> &rows,
-                                           const Seen &seen, int start, char *lds) {
-    constexpr int kBlocks = D / 32;
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int half = lane >> 5;
+// Bytes of LDS in which `Waves` wavefronts leave the results of NRows rows.
+template <int D, int Waves, int NRows> constexpr int joined_bytes() {
+    return Waves * NRows * (D + 4) * 4;
+}
+
+// Adds up and writes what the wavefronts left: sums [wave][row][D + 4], scaled to the largest of
+// their maxima, and ml [wave][row][2], their maxima and sums of numerators.
+template <class T, int D, int Waves, int NRows>
+__device__ __forceinline__ void write_joined(const taps_attend_launch &p, const taps_plan_item &item,
+                                             uint32_t head, const float *sums, const float *ml) {
     const float c = p.scale * kLog2e;
-    float *ml = (float *)(lds + narrow_bytes<D>() - 2 * kWaves * kNarrowRows * 4);
-    const float l_wave = rows.total();
-    __syncthreads();   // the tiles are done with
-    if (half == 0) {
-        ml[2 * (wave * kNarrowRows + lane)] = rows.m;
-        ml[2 * (wave * kNarrowRows + lane) + 1] = l_wave;
-    }
-    __syncthreads();
-    float m = kMinusInf;
-#pragma unroll
-    for (int w = 0; w < kWaves; ++w) m = fmaxf(m, ml[2 * (w * kNarrowRows + (lane & 31))]);
-    float *sums = (float *)lds;   // [wave][row][D + 4]
-    const auto leave = [&]() {
-        const float by = rows.m == kMinusInf ? 0.f : __builtin_amdgcn_exp2f((rows.m - m) * c);
-        float *at = sums + (wave * kNarrowRows + (lane & 31)) * (D + 4);
-#pragma unroll
-        for (int b = 0; b < kBlocks; ++b)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const f32x4 v = {rows.o[b][4 * i] * by, rows.o[b][4 * i + 1] * by,
-                                 rows.o[b][4 * i + 2] * by, rows.o[b][4 * i + 3] * by};
-                *(f32x4 *)(at + 32 * b + 8 * i + 4 * half) = v;
-            }
-    };
-    finish(p, item, cache, rows, seen, item.row0 + (lane & 31), l_wave, start + kNarrowKeys * wave,
-           kWaves * kNarrowKeys, lane, leave);
-    __syncthreads();
-    const int n_rows = min(kNarrowRows, item.rows - item.row0);
-    const auto result = [&](int r, int d) {
-        f32x4 o = {};
-#pragma unroll
-        for (int w = 0; w < kWaves; ++w)
-            o += *(const f32x4 *)(sums + (w * kNarrowRows + r) * (D + 4) + d);
-        return o;
-    };
-    const auto statistics = [&](int r, float &top, float &l) {
-        top = kMinusInf, l = 0.f;
-#pragma unroll
-        for (int w = 0; w < kWaves; ++w) top = fmaxf(top, ml[2 * (w * kNarrowRows + r)]);
-#pragma unroll
-        for (int w = 0; w < kWaves; ++w) {
-            const float mw = ml[2 * (w * kNarrowRows + r)], lw = ml[2 * (w * kNarrowRows + r) + 1];
-            l += mw == kMinusInf ? lw : lw * __builtin_amdgcn_exp2f((mw - top) * c);
-        }
-    };
-    for (int k = threadIdx.x; k < n_rows * (D / 4); k += kThreads) {
+    const int n_rows = min(NRows, item.rows - item.row0);
+    for (int k = threadIdx.x; k < n_rows * (D / 4); k += 64 * Waves) {
         const int r = k / (D / 4), d = 4 * (k % (D / 4));
         if (d >= (int)p.dim) continue;
-        float top, l;
-        statistics(r, top, l);
-        const f32x4 o = result(r, d);
+        float top = kMinusInf, l = 0.f;
+#pragma unroll
+        for (int w = 0; w < Waves; ++w) top = fmaxf(top, ml[2 * (w * NRows + r)]);
+#pragma unroll
+        for (int w = 0; w < Waves; ++w) {
+            const float mw = ml[2 * (w * NRows + r)], lw = ml[2 * (w * NRows + r) + 1];
+            l += mw == kMinusInf ? lw : lw * __builtin_amdgcn_exp2f((mw - top) * c);
+        }
+        f32x4 o = {};
+#pragma unroll
+        for (int w = 0; w < Waves; ++w) o += *(const f32x4 *)(sums + (w * NRows + r) * (D + 4) + d);
         if (item.part < 0) {
             const float inv = inverse(top, l);
             char *out = out_row<T>(p, item, head, item.row0 + r);
@@ -587,6 +552,49 @@ __device__ __forceinline__ void join_waves(const taps_attend_launch &p, const ta
             if (d == 0) p.part_ml[2 * at] = top, p.part_ml[2 * at + 1] = l;
         }
     }
+}
+
+// This lane's part of its row's result, times `by`, to `at`, [D].
+template <class T, int D>
+__device__ __forceinline__ void leave_row(const Rows<T, D> &rows, float by, float *at, int lane) {
+#pragma unroll
+    for (int b = 0; b < D / 32; ++b)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const f32x4 v = {rows.o[b][4 * i] * by, rows.o[b][4 * i + 1] * by,
+                             rows.o[b][4 * i + 2] * by, rows.o[b][4 * i + 3] * by};
+            *(f32x4 *)(at + 32 * b + 8 * i + 4 * (lane >> 5)) = v;
+        }
+}
+
+// The results of a narrow item's wavefronts, each of which had all its rows and every fourth tile
+// of 32 keys from `start` on, are joined in LDS and written.
+template <class T, int D, class Cache>
+__device__ __forceinline__ void join_waves(const taps_attend_launch &p, const taps_plan_item &item,
+                                           const Cache &cache, uint32_t head, Rows<T, D> &rows,
+                                           const Seen &seen, int start, char *lds) {
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const float c = p.scale * kLog2e;
+    float *ml = (float *)(lds + narrow_bytes<D>() - 2 * kWaves * kNarrowRows * 4);
+    const float l_wave = rows.total();
+    __syncthreads();   // the tiles are done with
+    if (lane < kNarrowRows) {
+        ml[2 * (wave * kNarrowRows + lane)] = rows.m;
+        ml[2 * (wave * kNarrowRows + lane) + 1] = l_wave;
+    }
+    __syncthreads();
+    float m = kMinusInf;
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) m = fmaxf(m, ml[2 * (w * kNarrowRows + (lane & 31))]);
+    float *sums = (float *)lds;
+    const auto leave = [&]() {
+        const float by = rows.m == kMinusInf ? 0.f : __builtin_amdgcn_exp2f((rows.m - m) * c);
+        leave_row(rows, by, sums + (wave * kNarrowRows + (lane & 31)) * (D + 4), lane);
+    };
+    finish(p, item, cache, rows, seen, item.row0 + (lane & 31), l_wave, start + kNarrowKeys * wave,
+           kWaves * kNarrowKeys, lane, leave);
+    __syncthreads();
+    write_joined<T, D, kWaves, kNarrowRows>(p, item, head, sums, ml);
 }
 
 // Launches of as many of n items as a grid's dimension, fewer than 2^32 threads, holds.

@@ -156,7 +156,10 @@ int64_t piece_of(const std::vector<Strip> &strips, int32_t kind, int64_t cus, in
 // every slot: of those the dear items come first, whatever their sequence
 // (prompts of 2048 of eight sequences, 32 heads: 350 us with all dear items first, 321
 // so, 321 by sequences alone; 20 of 100 to 700 tokens: 107, 108 and 119).
-// Narrow items share no keys: dear ones first.
+// Narrow items share no keys: dear ones first, but those of few rows last, for which there are
+// kernels of their own.
+bool is_few(const taps_plan_item &i) { return i.kind == kNarrow && i.rows - i.row0 <= kFewRows; }
+
 void in_order(std::vector<taps_plan_item> *items, int64_t cus, int64_t heads) {
     const auto cost = [](const taps_plan_item &i) { return Strip::cost_of(i.kind, i.hi - i.lo); };
     const auto dear = [&](const taps_plan_item &x, const taps_plan_item &y) {
@@ -188,6 +191,8 @@ void in_order(std::vector<taps_plan_item> *items, int64_t cus, int64_t heads) {
         std::stable_sort(rest, end, dear);
         at = end;
     }
+    std::stable_partition(items->begin(), items->end(),
+                          [](const taps_plan_item &i) { return !is_few(i); });
 }
 
 // Whether sequences of more than 128 rows are cut into strips of 256 rows (wide
@@ -328,7 +333,8 @@ taps_status lay_out(const taps_paged_batch *b, uint32_t cus, Layout *out) {
         if (part_rows >= (1ull << 31)) return fail(TAPS_ERR_ARG, "too many rows are split");
     }
     in_order(&out->items, cus, heads);
-    for (const taps_plan_item &i : out->items) h.n_wide += i.kind == kWide;
+    for (const taps_plan_item &i : out->items)
+        h.n_wide += i.kind == kWide, h.n_few += is_few(i);
     if (out->items.size() * b->kv_heads >= (1ull << 31) || b->kv_heads > 65535)
         return fail(TAPS_ERR_ARG, "too many workgroups");
 

@@ -137,7 +137,7 @@ inline void set_attend(taps_attend_launch *p, const taps_plan_header &h, const v
     p->joins = (const taps_plan_join *)(dev + h.joins_at);
     p->q_token = 2 * q.stride[1], p->q_head = 2 * q.stride[2];
     p->o_token = 2 * out.stride[1], p->o_head = 2 * out.stride[2];
-    p->n_items = h.n_items, p->n_wide = h.n_wide;
+    p->n_items = h.n_items, p->n_wide = h.n_wide, p->n_few = h.n_few;
     p->n_joins = h.n_joins, p->join_rounds = h.join_rounds;
     p->q_heads = h.q_heads, p->kv_heads = h.kv_heads, p->group = h.q_heads / h.kv_heads;
     p->dim = h.head_dim;

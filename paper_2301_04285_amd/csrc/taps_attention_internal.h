@@ -16,7 +16,7 @@ constexpr uint32_t kPlanMagic = 0x54415031;
 
 // Query rows of the kinds of items (taps_attend.hip).  A row is a pair of a
 // token and one of the query heads of a key head.
-constexpr int kWideRows = 256, kBlockRows = 128, kNarrowRows = 32;
+constexpr int kWideRows = 256, kBlockRows = 128, kNarrowRows = 32, kFewRows = 16;
 // Only plans for heads of more have wide items.
 constexpr uint32_t kWideAbove = 64;
 // Keys of a tile: of wide and block items, and of narrow ones.
@@ -32,7 +32,8 @@ struct taps_plan_header {
     uint32_t max_positions;   // largest position of a new token, plus one
     uint32_t appendable;      // every sequence has kv_lens >= q_lens
     uint32_t join_rounds;     // workgroups that the rows of a join are spread over, at most
-    uint32_t n_wide, reserved;
+    uint32_t n_wide;
+    uint32_t n_few;           // the last n_few items: narrow ones of up to kFewRows rows
     uint32_t zeros[4];        // what attention reads for keys that are not there
     // byte offsets of the arrays
     uint64_t tokens_at, pages_at, items_at, joins_at;
@@ -119,7 +120,7 @@ struct taps_attend_launch {
     // strides in bytes
     int64_t q_token, q_head, o_token, o_head;
     int64_t k_page, k_head, k_slot, v_page, v_head, v_slot;
-    uint32_t n_items, n_wide, n_joins, join_rounds, q_heads, kv_heads, group, dim;
+    uint32_t n_items, n_wide, n_few, n_joins, join_rounds, q_heads, kv_heads, group, dim;
     uint32_t page_log2, causal, window;
     float scale;
 };

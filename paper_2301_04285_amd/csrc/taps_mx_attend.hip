@@ -24,12 +24,18 @@ template <int D, int Bits> struct Piece {
     static __device__ __forceinline__ bool exists(int lane, int dim) {
         return kChunks != 2 || dim > 32 || lane < 32;
     }
-    __device__ __forceinline__ void fetch(const char *codes, const char *scales, int lane) {
-        const uint32_t *from = (const uint32_t *)(codes + chunk(lane) * Bits);
+    // From uniform addresses and this lane's offsets of its quarter's codes and first scale.
+    __device__ __forceinline__ void fetch(const char *codes, const char *scales, uint32_t code_at,
+                                          uint32_t scale_at, int lane) {
+        typedef uint32_t words __attribute__((ext_vector_type(kCodes), aligned(4)));
+        const words w = *(const words *)(codes + code_at);
 #pragma unroll
-        for (int i = 0; i < kCodes; ++i) code[i] = from[i];
-        byte[0] = (uint8_t)scales[chunk(lane) / 4];
-        if (kBytes > 1) byte[kBytes - 1] = (uint8_t)scales[(chunk(lane) + kChunks - 1) / 4];
+        for (int i = 0; i < kCodes; ++i) code[i] = w[i];
+        byte[0] = (uint8_t)scales[scale_at];
+        if (kBytes > 1) {
+            const uint32_t more = (chunk(lane) + kChunks - 1) / 4 - chunk(lane) / 4;
+            byte[kBytes - 1] = (uint8_t)scales[scale_at + more];
+        }
     }
     __device__ __forceinline__ void clear() {
 #pragma unroll
@@ -80,45 +86,65 @@ template <class T, int Bits> struct MxCache {
     }
 };
 
-// Fetches a wavefront's 16 keys of K or of V of a tile and puts them into LDS.  Keys outside
-// lo .. hi - 1 are fetched from an end of that range and become zeros, as does what is not there
-// of a head's second block.
-template <class T, int D, int Bits, bool V> struct Stager {
+// 16 keys of K or of V that share a page, on their way to a wavefront.
+template <class T, int D, int Bits, bool V> struct Keys {
     using P = Piece<D, Bits>;
     const char *codes, *scales;
     int64_t code_page, scale_page;
-    uint32_t code_slot, scale_slot;
+    uint32_t code_slot, scale_slot, code_at, scale_at;   // _at: of this lane's quarter
     int lo, hi, page_log2, lane;
     bool exists;
-    P piece;
-    __device__ __forceinline__ Stager(const taps_mx_attend_launch &p, const taps_plan_item &item,
-                                      uint32_t head, int l) {
+    __device__ __forceinline__ Keys(const taps_mx_attend_launch &p, const taps_plan_item &item,
+                                    uint32_t head, int l) {
         codes = V ? p.v_cache + (int64_t)head * p.v_head : p.k_cache + (int64_t)head * p.k_head;
         scales = V ? p.v_scales + (int64_t)head * p.vs_head : p.k_scales + (int64_t)head * p.ks_head;
         code_page = V ? p.v_page : p.k_page, scale_page = V ? p.vs_page : p.ks_page;
         code_slot = V ? p.v_slot : p.k_slot, scale_slot = V ? p.vs_slot : p.ks_slot;
         lo = item.lo, hi = item.hi, page_log2 = p.page_log2, lane = l;
         exists = P::exists(lane, p.dim);
+        // a quarter that is not there: the head's first, to be cleared
+        code_at = P::key(lane) * code_slot + (exists ? P::chunk(lane) * Bits : 0);
+        scale_at = P::key(lane) * scale_slot + (exists ? P::chunk(lane) / 4 : 0);
     }
-    // The group of 16 keys from key0 on, a multiple of 16; outside the item: the nearest inside.
-    __device__ __forceinline__ void fetch(int key0, int page) {
-        key0 = min(max(key0, lo & ~15), (hi - 1) & ~15);
+    // Where the group from key0 on lies, a multiple of 16.  A page has all its slots, so those outside
+    // lo .. hi - 1 are fetched too, and cleared.
+    struct At {
+        const char *codes, *scales;
+    };
+    __device__ __forceinline__ At at(int key0, int page) const {
         const int64_t slot = key0 & ((1 << page_log2) - 1);
-        const uint32_t row = min(max(key0 + P::key(lane), lo), hi - 1) - key0;
-        if (exists)
-            piece.fetch(codes + page * code_page + slot * code_slot + row * code_slot,
-                        scales + page * scale_page + slot * scale_slot + row * scale_slot, lane);
+        return {codes + page * code_page + slot * code_slot,
+                scales + page * scale_page + slot * scale_slot};
     }
-    // key0: as fetched; `at`: its number in the tile of LDS.
-    __device__ __forceinline__ void put(char *tile, int at, int key0) {
+    // The group behind one, on the same page.
+    __device__ __forceinline__ At behind(const At &a) const {
+        return {a.codes + 16 * code_slot, a.scales + 16 * scale_slot};
+    }
+    // The nearest group inside the item to the one from key0 on.
+    __device__ __forceinline__ At nearest(int key0, int page) const {
+        return at(min(max(key0, lo & ~15), (hi - 1) & ~15), page);
+    }
+    __device__ __forceinline__ void fetch(P &to, const At &a) const {
+        to.fetch(a.codes, a.scales, code_at, scale_at, lane);
+    }
+    // After the wait for it; key0: as fetched.
+    __device__ __forceinline__ void blank(P &of, int key0) const {
         const int key = key0 + P::key(lane);
-        if (!exists || key < lo || key >= hi) piece.clear();
+        if (key < lo || key >= hi) of.clear();
+    }
+    __device__ __forceinline__ void blank_missing(P &of) const {
+        if (P::kChunks == 2 && !exists) of.clear();
+    }
+    // To a tile in LDS, where key0 has the number `at`.
+    __device__ __forceinline__ void put(P &from, char *tile, int at, int key0) const {
+        if (key0 < lo || key0 + 16 > hi) blank(from, key0);
+        blank_missing(from);
         const int n = at + P::key(lane);
         const int mask = V ? Tile<D>::v_mask(n) : Tile<D>::k_mask(n);
 #pragma unroll
         for (int j = 0; j < P::kChunks; ++j)
             *(u32x4 *)(tile + n * Tile<D>::kRow + 16 * ((P::chunk(lane) + j) ^ mask)) =
-                piece.template eight<T>(j, lane);
+                from.template eight<T>(j, lane);
     }
 };
 
@@ -139,20 +165,22 @@ __device__ __forceinline__ void attend_rows(const taps_mx_attend_launch &p, cons
     Rows<T, D> rows;
     rows.start(p, item, head, row, lane);
     const Seen seen(p, item, row0);
-    Stager<T, D, Bits, false> k(p, item, head, lane);
-    Stager<T, D, Bits, true> v(p, item, head, lane);
+    const Keys<T, D, Bits, false> k(p, item, head, lane);
+    const Keys<T, D, Bits, true> v(p, item, head, lane);
+    Piece<D, Bits> k_piece, v_piece;
     const bool takes_k = Waves == 4 || wave < 4, takes_v = Waves == 4 || wave >= 4;
     const int mine = 16 * (wave & 3);
+    int page = start < hi ? page_at(p, pages, start + mine, item.lo, item.hi) : 0;
     const auto fetch = [&](int t0) {
         if (t0 >= hi) return;
-        const int page = page_at(p, pages, t0 + mine, item.lo, item.hi);
-        if (takes_k) k.fetch(t0 + mine, page);
-        if (takes_v) v.fetch(t0 + mine, page);
+        if (takes_k) k.fetch(k_piece, k.nearest(t0 + mine, page));
+        if (takes_v) v.fetch(v_piece, v.nearest(t0 + mine, page));
+        page = page_at(p, pages, t0 + kWideKeys + mine, item.lo, item.hi);
     };
     const auto put = [&](int t0, char *tile) {
         if (t0 >= hi) return;
-        if (takes_k) k.put(tile, mine, t0 + mine);
-        if (takes_v) v.put(tile + kPart, mine, t0 + mine);
+        if (takes_k) k.put(k_piece, tile, mine, t0 + mine);
+        if (takes_v) v.put(v_piece, tile + kPart, mine, t0 + mine);
     };
     fetch(start);
     put(start, lds);
@@ -184,7 +212,14 @@ __global__ __launch_bounds__(kWideThreads, 2) void k_mx_attend_wide(taps_mx_atte
     attend_rows<T, D, Bits, 8>(p, p.items[blockIdx.x / p.kv_heads], head, lds);
 }
 
-// Up to 32 query rows: every wavefront has all of them and its own keys.
+// What a wavefront wrote to LDS is read by its other lanes, and before it is written anew.
+__device__ __forceinline__ void exchange() {
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+}
+
+// 17 to 32 query rows: every wavefront has all of them and its own keys.
 template <class T, int D, int Bits>
 __device__ __forceinline__ void attend_narrow(const taps_mx_attend_launch &p,
                                               const taps_plan_item &item, uint32_t head, char *lds) {
@@ -197,29 +232,31 @@ __device__ __forceinline__ void attend_narrow(const taps_mx_attend_launch &p,
     rows.start(p, item, head, item.row0 + (lane & 31), lane);
     const Seen seen(p, item, item.row0);
     char *tile = lds + wave * Tile<D>::bytes(kNarrowKeys);
-    Stager<T, D, Bits, false> k[2] = {{p, item, head, lane}, {p, item, head, lane}};
-    Stager<T, D, Bits, true> v[2] = {{p, item, head, lane}, {p, item, head, lane}};
+    const Keys<T, D, Bits, false> k(p, item, head, lane);
+    const Keys<T, D, Bits, true> v(p, item, head, lane);
+    Piece<D, Bits> k_piece[2], v_piece[2];
+    int page[2] = {0, 0};
+    const auto look_up = [&](int t0) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) page[h] = page_at(p, pages, t0 + 16 * h, lo, hi);
+    };
     const auto fetch = [&](int t0) {
         if (lo >= hi || t0 >= hi) return;
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
-            const int page = page_at(p, pages, t0 + 16 * h, lo, hi);
-            k[h].fetch(t0 + 16 * h, page);
-            v[h].fetch(t0 + 16 * h, page);
+            k.fetch(k_piece[h], k.nearest(t0 + 16 * h, page[h]));
+            v.fetch(v_piece[h], v.nearest(t0 + 16 * h, page[h]));
         }
-    };
-    const auto exchange = [&]() {
-        __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
-        __builtin_amdgcn_wave_barrier();
-        __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+        look_up(t0 + kStep);
     };
     int t0 = start + kNarrowKeys * wave;
+    if (lo < hi) look_up(t0);
     fetch(t0);
     for (; lo < hi && t0 < hi; t0 += kStep) {
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
-            k[h].put(tile, 16 * h, t0 + 16 * h);
-            v[h].put(tile + kNarrowKeys * Tile<D>::kRow, 16 * h, t0 + 16 * h);
+            k.put(k_piece[h], tile, 16 * h, t0 + 16 * h);
+            v.put(v_piece[h], tile + kNarrowKeys * Tile<D>::kRow, 16 * h, t0 + 16 * h);
         }
         exchange();
         fetch(t0 + kStep);
@@ -233,15 +270,368 @@ __device__ __forceinline__ void attend_narrow(const taps_mx_attend_launch &p,
     join_waves(p, item, MxCache<T, Bits>(p, head), head, rows, seen, start, lds);
 }
 
+// Up to 16 query rows: both products as 16x16x32 tiles, in which a lane has eight of a tile's 32
+// keys for one row, half of what it has in the others' tiles.  Keys go from the registers that they
+// are fetched to into the first product: a lane's quarter of a key is its part of
+// the operand, with the queries laid out the same.  Values pass through LDS to be transposed.
+template <class T> struct SmallMfma;
+template <> struct SmallMfma<__bf16> {
+    static __device__ __forceinline__ f32x4 run(s16x8 a, s16x8 b, f32x4 c) {
+        return __builtin_amdgcn_mfma_f32_16x16x32_bf16(
+            __builtin_bit_cast(Mfma<__bf16>::v8, a), __builtin_bit_cast(Mfma<__bf16>::v8, b), c, 0, 0, 0);
+    }
+};
+template <> struct SmallMfma<_Float16> {
+    static __device__ __forceinline__ f32x4 run(s16x8 a, s16x8 b, f32x4 c) {
+        return __builtin_amdgcn_mfma_f32_16x16x32_f16(
+            __builtin_bit_cast(Mfma<_Float16>::v8, a), __builtin_bit_cast(Mfma<_Float16>::v8, b), c, 0, 0,
+            0);
+    }
+};
+
+// LDS image of 32 values: rows of 16-byte chunks, permuted by a mask of the key's number.  Eight keys'
+// writes of one chunk, and reads of two chunks of four keys, fall on different banks.
+template <int D> struct Values {
+    static constexpr int kRow = D <= 64 ? 128 : 256, kBytes = kNarrowKeys * kRow;
+    static __device__ __forceinline__ int mask(int key) {
+        const int m = 2 * (key & 3) + ((key >> 2) & 1);
+        return D <= 64 ? m : m + (key & 8);
+    }
+};
+
+struct True {
+    static constexpr bool value = true;
+};
+struct False {
+    static constexpr bool value = false;
+};
+
+// 16 values as they lie in memory: a block of 32 elements a lane, so that neighbouring lanes share lines.
+template <class T, int D, int Bits> struct Blocks {
+    static constexpr int kN = D / 32, kBytes = 4 * Bits;   // blocks of a row; bytes of a block's codes
+    struct Raw {
+        uint32_t code[Bits], byte;
+    };
+    int key, block;
+    bool writes, exists;    // the lane has a block of a tile, and of the head
+    uint32_t code_at, scale_at;
+    __device__ __forceinline__ Blocks(const taps_mx_attend_launch &p, int lane) {
+        key = lane / kN, block = lane % kN;
+        writes = lane < 16 * kN, exists = writes && 32 * block < (int)p.dim;
+        code_at = exists ? key * (uint32_t)p.v_slot + block * kBytes : 0;
+        scale_at = exists ? key * (uint32_t)p.vs_slot + block : 0;
+    }
+    __device__ __forceinline__ void fetch(Raw &to, const char *codes, const char *scales) const {
+#pragma unroll
+        for (int i = 0; i < Bits; i += 4) {
+            const u32x4 w = *(const u32x4 *)(codes + code_at + 4 * i);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) to.code[i + j] = w[j];
+        }
+        to.byte = (uint8_t)scales[scale_at];
+    }
+    static __device__ __forceinline__ void clear(Raw &of) {
+#pragma unroll
+        for (int i = 0; i < Bits; ++i) of.code[i] = 0;
+        of.byte = 127;
+    }
+    // Where the lane's chunks of eight values go: at ^ 16 j.
+    __device__ __forceinline__ uint32_t place() const {
+        return key * Values<D>::kRow + 16 * ((4 * block) ^ Values<D>::mask(key));
+    }
+    static __device__ __forceinline__ u32x4 eight(const Raw &of, int j, float scale) {
+        return mx_eight<T, Bits>(of.code + j * kWords<Bits>, scale);
+    }
+};
+
+template <int D, int Waves> constexpr int few_bytes() {
+    return max_of(Waves * Values<D>::kBytes, joined_bytes<D, Waves, kFewRows>()) + 8 * Waves * kFewRows;
+}
+
+template <class T, int D, int Bits, int Waves>
+__device__ __forceinline__ void attend_few(const taps_mx_attend_launch &p, const taps_plan_item &item,
+                                           uint32_t head, char *lds) {
+    constexpr int kSteps = D / 32, kBlocks = D / 16, kStep = Waves * kNarrowKeys;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int32_t *pages = p.pages + item.page0;
+    const int lo = item.lo, hi = item.hi, start = lo & ~31;
+    const float c = p.scale * kLog2e;
+    const int row = item.row0 + (lane & 15), quarter = lane >> 4;
+    const bool real = row < item.rows;
+    const int token = row / (int)p.group, sub = row - token * (int)p.group;
+    // keys of the item that this lane's row sees: first .. last
+    int first = lo, last = hi - 1;
+    if (p.causal) {
+        const int pos = item.first_pos + token;
+        last = min(last, pos);
+        if (p.window) first = max(first, pos - (int)p.window + 1);
+    }
+    if (!real) last = -1, first = 0;
+    s16x8 q[kSteps];
+    {
+        const char *at = p.q + (int64_t)(item.token0 + token) * p.q_token +
+                         (int64_t)(head * p.group + sub) * p.q_head;
+#pragma unroll
+        for (int k = 0; k < kSteps; ++k) {
+            const int d = 8 * (kSteps * quarter + k);
+            q[k] = s16x8{};
+            if (real && d < (int)p.dim) q[k] = *(const s16x8 *)(at + 2 * d);
+        }
+    }
+    float m = real ? kMinusInf : 0.f, l = 0.f;   // a row that is not there never raises it
+    f32x4 o[kBlocks];
+#pragma unroll
+    for (int b = 0; b < kBlocks; ++b) o[b] = f32x4{};
+    const Seen seen(p, item, item.row0);
+
+    const Keys<T, D, Bits, false> keys(p, item, head, lane);
+    const Keys<T, D, Bits, true> values(p, item, head, lane);
+    const Blocks<T, D, Bits> blocks(p, lane);
+    // Two tiles are on their way at any time, each in a set of registers.
+    struct Set {
+        Piece<D, Bits> k[2];
+        typename Blocks<T, D, Bits>::Raw v[2];
+        int page[2];
+    } set[2];
+    const bool one_page = p.page_log2 >= 5;   // tiles start at multiples of 32
+    const auto look_up = [&](Set &s, int t) {
+        s.page[0] = page_at(p, pages, t, lo, hi);
+        if (!one_page) s.page[1] = page_at(p, pages, t + 16, lo, hi);
+    };
+    const auto fetch = [&](Set &s, int t) {
+        auto k0 = keys.at(t, s.page[0]), k1 = keys.behind(k0);
+        auto v0 = values.at(t, s.page[0]), v1 = values.behind(v0);
+        if (!one_page) {
+            k0 = keys.nearest(t, s.page[0]), k1 = keys.nearest(t + 16, s.page[1]);
+            v0 = values.nearest(t, s.page[0]), v1 = values.nearest(t + 16, s.page[1]);
+        }
+        keys.fetch(s.k[0], k0);
+        keys.fetch(s.k[1], k1);
+        blocks.fetch(s.v[0], v0.codes, v0.scales);
+        blocks.fetch(s.v[1], v1.codes, v1.scales);
+    };
+    char *tile = lds + wave * Values<D>::kBytes;
+    // This wavefront's tiles: those that not all rows see all of, the edges, come first, then those
+    // between them, plain .. plain_end - 1.
+    const int begin = start + kNarrowKeys * wave;
+    const auto up = [&](int t) {   // the first tile from t on
+        return t <= begin ? begin : begin + (t - begin + kStep - 1) / kStep * kStep;
+    };
+    const int plain = up(seen.from), plain_end = max(seen.to - kNarrowKeys + 2, plain);
+    const auto edge_from = [&](int t) { return t >= plain && t < plain_end ? up(plain_end) : t; };
+    // where a lane writes its block, and reads its columns of the first 16
+    uint32_t write_at = blocks.place();
+    // lane of a group of 16: key (lane % 16) / 4 of the quarter's four, columns 4 (lane % 4) ..
+    const int v_key = 4 * quarter + (lane & 15) / 4;
+    uint32_t read_at = v_key * Values<D>::kRow + 8 * (lane & 1) +
+                       16 * (((lane >> 1) & 1) ^ Values<D>::mask(v_key));
+    // A tile of 32 keys; an edge: some rows do not see some of them.  Again: maxima and sums are
+    // known, and an edge's rows are taken one by one, with zeros for the values that a row does not see.
+    // next: the tile that the set of registers is for then (hi: none), after_next: the one after it
+    const auto step = [&](auto edge, auto again, auto surely, Set &s, int t0, int next, int after_next) {
+        constexpr bool kEdge = decltype(edge)::value, kAgain = decltype(again)::value;
+        // no address below is kept from tile to tile, registers are few
+        asm volatile("" : "+v"(write_at), "+v"(read_at));
+        // what was loaded is used here and not, shifted, right behind the load, which would wait for it
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+#pragma unroll
+            for (int i = 0; i < Piece<D, Bits>::kBytes; ++i) asm volatile("" : "+v"(s.k[h].byte[i]));
+            asm volatile("" : "+v"(s.v[h].byte));
+        }
+        f32x4 x[2] = {};
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            // those that are not there may be anything: their scores are replaced
+            keys.blank_missing(s.k[h]);
+#pragma unroll
+            for (int k = 0; k < kSteps; ++k)
+                x[h] = SmallMfma<T>::run(
+                    __builtin_bit_cast(s16x8, s.k[h].template eight<T>(k, lane)), q[k], x[h]);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const int key = t0 + 16 * h + blocks.key;
+            if ((kSteps == 2 && !blocks.exists) || (kEdge && (key < lo || key >= hi)))
+                blocks.clear(s.v[h]);
+            const float scale = mx_scale(s.v[h].byte);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const u32x4 v = blocks.eight(s.v[h], j, scale);
+                if (kSteps == 4 || blocks.writes)
+                    *(u32x4 *)(tile + (write_at ^ (16 * j)) + 16 * h * Values<D>::kRow) = v;
+            }
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        exchange();
+        if (!kAgain && (decltype(surely)::value || next < hi)) {
+            fetch(s, next);
+            look_up(s, after_next);
+        }
+        // x[h][i]: key t0 + 16 h + 4 quarter + i
+        if (kEdge) {
+            const uint32_t sees = max(last - first + 1, 0), at = t0 + 4 * quarter - first;
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) x[h][i] = at + (16 * h + i) < sees ? x[h][i] : kMinusInf;
+        }
+        u32x4 y;
+        const auto numerators = [&]() {
+            const float shift = m <= kNoScore ? 0.f : m * c - kLiftLog2<T>;
+            float sum = 0.f;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const float e = __builtin_amdgcn_exp2f(x[i / 2][2 * (i % 2)] * c - shift);
+                const float f = __builtin_amdgcn_exp2f(x[i / 2][2 * (i % 2) + 1] * c - shift);
+                sum += e + f;
+                y[i] = pack2<T>(e, f);
+            }
+            return sum;
+        };
+        float sum = numerators();
+        // the first keys, and scores too far above the maximum
+        if (!kAgain && __any(m == kMinusInf || sum > kMostSum<T>)) {
+            float most = x[0][0];
+#pragma unroll
+            for (int i = 1; i < 8; ++i) most = fmaxf(most, x[i / 4][i % 4]);
+            most = half_max(most);
+            most = fmaxf(most, __shfl_xor(most, 16, 64));
+            const float to = fmaxf(m, most);
+            const float by = to == kMinusInf ? 1.f : __builtin_amdgcn_exp2f((m - to) * c);
+            m = to;
+            l *= by;
+#pragma unroll
+            for (int b = 0; b < kBlocks; ++b) o[b] *= by;
+            sum = numerators();
+        }
+        if (!kAgain) l += sum;
+        // 16 columns of the values as the second product's operand
+        const auto columns = [&](int b) {
+            const char *at = tile + (read_at ^ (32 * b));
+            const s16x4 u = Rows<T, D>::transposed(at);
+            const s16x4 w = Rows<T, D>::transposed(at + 16 * Values<D>::kRow);
+            return s16x8{u[0], u[1], u[2], u[3], w[0], w[1], w[2], w[3]};
+        };
+        if constexpr (!kAgain || !kEdge) {
+#pragma unroll
+            for (int b = 0; b < kBlocks; ++b)
+                o[b] = SmallMfma<T>::run(columns(b), __builtin_bit_cast(s16x8, y), o[b]);
+        } else {
+            const int rows = __builtin_amdgcn_readfirstlane(min(kFewRows, item.rows - item.row0));
+            for (int r = 0; r < rows; ++r) {
+                const int from = __shfl(first, r, 64), to = __shfl(last, r, 64);
+#pragma unroll
+                for (int b = 0; b < kBlocks; ++b) {
+                    s16x8 v = columns(b);
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) {
+                        const int key = t0 + 16 * (e / 4) + 4 * quarter + e % 4;
+                        v[e] = key >= from && key <= to ? v[e] : (short)0;
+                    }
+                    const f32x4 one = SmallMfma<T>::run(v, __builtin_bit_cast(s16x8, y), f32x4{});
+                    __builtin_amdgcn_sched_barrier(0);   // whatever rows the lanes have
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) o[b][i] = (lane & 15) == r ? o[b][i] + one[i] : o[b][i];
+                }
+            }
+        }
+        exchange();
+    };
+    if (lo < hi) {
+        const int last_set = plain + kStep < plain_end ? plain + kStep : hi;   // of set 0, after the edges
+        int t0 = edge_from(begin);
+        const int first_set = t0 < hi ? t0 : last_set;
+        look_up(set[1], plain);
+        look_up(set[0], first_set);
+        if (plain < plain_end) fetch(set[1], plain);   // in the order in which they are waited for
+        if (first_set < hi) fetch(set[0], first_set);
+        look_up(set[1], plain + 2 * kStep);
+        const auto after = [&](int t) {
+            const int next = edge_from(t + kStep);
+            return next < hi ? next : last_set;
+        };
+        look_up(set[0], t0 < hi ? after(t0) : plain + 3 * kStep);
+        while (t0 < hi) {
+            const int next = after(t0);
+            step(True{}, False{}, False{}, set[0], t0, next, next == last_set ? plain + 3 * kStep : after(next));
+            t0 = edge_from(t0 + kStep);
+        }
+        for (t0 = plain; t0 + 3 * kStep < plain_end; t0 += 2 * kStep) {
+            step(False{}, False{}, True{}, set[1], t0, t0 + 2 * kStep, t0 + 4 * kStep);
+            step(False{}, False{}, True{}, set[0], t0 + kStep, t0 + 3 * kStep, t0 + 5 * kStep);
+        }
+        for (; t0 < plain_end; t0 += 2 * kStep) {   // up to three
+            const int next = t0 + 2 * kStep < plain_end ? t0 + 2 * kStep : hi;
+            step(False{}, False{}, False{}, set[1], t0, next, hi);
+            if (t0 + kStep < plain_end) step(False{}, False{}, False{}, set[0], t0 + kStep, hi, hi);
+        }
+        // The numerator of a hidden key, 0, times a value that is infinite or NaN is NaN.  Only where
+        // rows differ in what they see is there such a thing; all of them are taken again then.
+        if (seen.differ(item)) {
+            float sum = 0.f;
+#pragma unroll
+            for (int b = 0; b < kBlocks; ++b)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) sum += o[b][i] * 0.f;
+            if (__builtin_expect(__any(sum != sum), 0)) {
+#pragma unroll
+                for (int b = 0; b < kBlocks; ++b) o[b] = f32x4{};
+                for (t0 = begin; t0 < hi; t0 += kStep) {
+                    look_up(set[0], t0);
+                    fetch(set[0], t0);
+                    step(True{}, True{}, False{}, set[0], t0, hi, hi);
+                }
+            }
+        }
+    }
+    float total = half_sum(l);
+    total += __shfl_xor(total, 16, 64);
+    if (total == 0.f && m == kMinusInf && first <= last) m = kNoScore;
+
+    float *ml = (float *)(lds + few_bytes<D, Waves>() - 8 * Waves * kFewRows);
+    float *sums = (float *)lds;
+    __syncthreads();   // the tiles are done with
+    if (quarter == 0) {
+        ml[2 * (wave * kFewRows + lane)] = m;
+        ml[2 * (wave * kFewRows + lane) + 1] = total;
+    }
+    __syncthreads();
+    float top = kMinusInf;
+#pragma unroll
+    for (int w = 0; w < Waves; ++w) top = fmaxf(top, ml[2 * (w * kFewRows + (lane & 15))]);
+    const float by = m == kMinusInf ? 0.f : __builtin_amdgcn_exp2f((m - top) * c);
+    float *mine = sums + (wave * kFewRows + (lane & 15)) * (D + 4);
+#pragma unroll
+    for (int b = 0; b < kBlocks; ++b) *(f32x4 *)(mine + 16 * b + 4 * quarter) = o[b] * by;
+    __syncthreads();
+    write_joined<T, D, Waves, kFewRows>(p, item, head, sums, ml);
+}
+
+// Four wavefronts an item, three items to a unit; eight where there are no more items than units
+// and a lone one's time counts (16 heads of 64, one token over 1024 keys: 9.8 us for 11.3; 64
+// tokens over up to 4000, 784 items: 48 for 39).
+constexpr uint32_t kUnits = 256;
+
+template <class T, int D, int Bits, int Waves>
+__global__ __launch_bounds__(64 * Waves, Waves == 4 ? 3 : 2) void k_mx_attend_few(taps_mx_attend_launch p) {
+    __shared__ __attribute__((aligned(16))) char lds[few_bytes<D, Waves>()];
+    const uint32_t head = blockIdx.x % p.kv_heads;
+    attend_few<T, D, Bits, Waves>(p, p.items[blockIdx.x / p.kv_heads], head, lds);
+}
+
 // A block or a narrow item; both fit a unit twice.
 template <class T, int D, int Bits>
 __global__ __launch_bounds__(kThreads, 2) void k_mx_attend(taps_mx_attend_launch p) {
-    __shared__ __attribute__((aligned(16))) char lds[max_of(narrow_bytes<D>(),
-                                                            2 * Tile<D>::bytes(kWideKeys))];
+    __shared__ __attribute__((aligned(16))) char lds[max_of(
+        max_of(narrow_bytes<D>(), few_bytes<D, kWaves>()), 2 * Tile<D>::bytes(kWideKeys))];
     const uint32_t head = blockIdx.x % p.kv_heads;
     const taps_plan_item item = p.items[blockIdx.x / p.kv_heads];
     if (item.kind == kBlock)
         attend_rows<T, D, Bits, 4>(p, item, head, lds);
+    else if (item.rows - item.row0 <= kFewRows)
+        attend_few<T, D, Bits, kWaves>(p, item, head, lds);
     else
         attend_narrow<T, D, Bits>(p, item, head, lds);
 }
@@ -252,9 +642,18 @@ template <class T, int D, int Bits> void launch_items(taps_mx_attend_launch p, h
             k_mx_attend_wide<T, D, Bits><<<groups, kWideThreads, 0, stream>>>(s);
         });
     p.items += p.n_wide;
-    in_slices(p, p.n_items - p.n_wide, kThreads, [&](const auto &s, uint32_t groups) {
-        k_mx_attend<T, D, Bits><<<groups, kThreads, 0, stream>>>(s);
-    });
+    const uint32_t others = p.n_items - p.n_wide;
+    if (p.n_few == others)
+        in_slices(p, others, 512, [&](const auto &s, uint32_t groups) {
+            if (groups <= kUnits)
+                k_mx_attend_few<T, D, Bits, 8><<<groups, 512, 0, stream>>>(s);
+            else
+                k_mx_attend_few<T, D, Bits, 4><<<groups, 256, 0, stream>>>(s);
+        });
+    else
+        in_slices(p, others, kThreads, [&](const auto &s, uint32_t groups) {
+            k_mx_attend<T, D, Bits><<<groups, kThreads, 0, stream>>>(s);
+        });
 }
 
 template <class T, int Bits>
