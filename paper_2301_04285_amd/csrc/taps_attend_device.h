@@ -514,6 +514,127 @@ template <int D> constexpr int narrow_bytes() {
            kWaves * kNarrowRows * 2 * 4;
 }
 
+// 256 query rows, 32 a wavefront; a unit has one workgroup at a time.  A tile takes
+// two phases: products (the numerators of the last tile by its values, the scores
+// of this one), and softmax.  While the first four wavefronts, one on each SIMD,
+// are in one of them, the others are in the other, so that the matrix cores
+// have a wavefront of their own at any time and a tile's loads serve twice the
+// rows of a block item.
+// 512 tokens over 32768 keys, 32 heads of 128 over 8: 243 us here, 1120 TFLOP/s (279
+// in blocks), the matrix cores busy for 58 % of the cycles at 1.9 GHz; the phases that
+// wait for each other take the rest.  The products alone, without loads, softmax and
+// reads of LDS, reach 1377 at the clocks that they leave, so a fifth is the most
+// there is to win.  Eight sequences of 2048 tokens, 32 heads, not causal, take 0.21 us a
+// key, 1280 TFLOP/s, and 90 us that do not grow with the keys.  Loading the next item's
+// first tiles and queries while the last ends wins none of those back (one workgroup
+// a unit that stays: 364 and 360 us).  Causal, a wavefront waits besides for the
+// tiles behind its last key that the strip's last one sees: 112 keys on average, a
+// tenth of the time for prompts of 2048.
+// L loads a wavefront's 16 keys of a tile, of K or of V (`second`), to LDS: load(t0, page, part) begins
+// to, and wait(newer) ends it, for all but the newest where `newer`.  `page` is that of the tile kAhead
+// tiles on; start() is for the tile of the first load().
+template <class T, int D, class L, class Launch, class Cache>
+__device__ __forceinline__ void attend_wide(const Launch &p, const taps_plan_item &item, uint32_t head,
+                                            const Cache &cache, char *lds) {
+    constexpr int kPart = kWideKeys * Tile<D>::kRow;   // a tile's K, or its V
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const bool second = wave >= 4;   // the workgroup's second half
+    const int32_t *pages = p.pages + item.page0;
+    const int start = item.lo & ~15;   // whole groups of 16 share a page
+    const float c = p.scale * kLog2e;
+    const int row0 = item.row0 + 32 * wave, row = row0 + (lane & 31);
+    Rows<T, D> rows;
+    rows.start(p, item, head, row, lane);
+    const Seen seen(p, item, row0);
+    if (item.lo < item.hi) {
+        // Both halves use all tiles that they see; the first loads K, the other V.  K of tile i is read in phases
+        // 2 i and 2 i + 1, V in the two after them.  Three tiles of each are kept: K of tile i + 2
+        // is loaded in phase 2 i + 1, V of tile i + 1 in phase 2 i.
+        typename Rows<T, D>::template Scores<kWideKeys> x;
+        typename Rows<T, D>::template Numerators<kWideKeys> y;
+        L loader(p, item, head, second, wave, lane);
+        const char *k_lds = lds, *v_lds = lds + 3 * kPart;
+        const int tiles = (item.hi - start + kWideKeys - 1) / kWideKeys;
+        const int used = min(max((seen.end - start + kWideKeys - 1) / kWideKeys, 1), tiles);
+        const auto tile0 = [&](int i) { return start + i * kWideKeys; };
+        const auto page_of = [&](int t0) {
+            return page_at(p, pages, t0 + loader.key0 + L::kAhead * kWideKeys, item.lo, item.hi);
+        };
+        const auto soften = [&](int t0) {
+            rows.soften(x, y, t0, seen.masks(t0, kWideKeys), c, lane);
+        };
+        // buffers: of tiles i - 1, i, i + 1 in the first half's loop, i - 2, i - 1, i in the
+        // other's; the oldest is loaded anew
+        int b0 = 2, b1 = 0, b2 = 1;
+        const auto turn = [&]() {
+            const int b = b0;
+            b0 = b1, b1 = b2, b2 = b;
+        };
+        const char *mine = second ? v_lds : k_lds;
+        loader.start(tile0(0), page_of(tile0(-L::kAhead)));
+        loader.load(tile0(0), page_of(tile0(0)), mine);
+        if (tiles > 1) loader.load(tile0(1), page_of(tile0(1)), mine + kPart);
+        int page = page_of(tile0(2));
+        loader.wait(false);
+        end_phase();
+        if (!second) {
+            for (int i = 0; i < used; ++i, turn()) {
+                if (i)
+                    rows.products(v_lds + b0 * kPart, y, k_lds + b1 * kPart, x, lane);
+                else
+                    rows.score(k_lds, x, lane);
+                end_phase();
+                if (i + 2 < tiles) loader.load(tile0(i + 2), page, k_lds + b0 * kPart);
+                page = page_of(tile0(i + 3));
+                soften(tile0(i));
+                loader.wait(i + 2 < tiles);
+                end_phase();
+            }
+            rows.spend(v_lds + b0 * kPart, y, lane);   // the last tile's
+            for (int i = used; i < tiles; ++i, turn()) {
+                end_phase();
+                if (i + 2 < tiles) loader.load(tile0(i + 2), page, k_lds + b0 * kPart);
+                page = page_of(tile0(i + 3));
+                loader.wait(i + 2 < tiles);
+                end_phase();
+            }
+        } else {
+            end_phase();
+            rows.score(k_lds, x, lane);
+            end_phase();
+            int i = 1;
+            const auto begin = [&]() {
+                if (i + 1 < tiles) loader.load(tile0(i + 1), page, v_lds + b0 * kPart);
+                page = page_of(tile0(i + 2));
+            };
+            for (; i < used; ++i, turn()) {
+                begin();
+                soften(tile0(i - 1));
+                end_phase();
+                rows.products(v_lds + b1 * kPart, y, k_lds + b2 * kPart, x, lane);
+                loader.wait(i + 1 < tiles);
+                end_phase();
+            }
+            begin();
+            soften(tile0(used - 1));
+            if (used < tiles) end_phase();
+            rows.spend(v_lds + b1 * kPart, y, lane);
+            for (; i < tiles; ++i, turn()) {
+                if (i > used) {
+                    begin();
+                    end_phase();
+                }
+                loader.wait(i + 1 < tiles);
+                end_phase();
+            }
+        }
+    }
+    const float l = rows.total();
+    finish(p, item, cache, rows, seen, row, l, start, 32, lane, [&]() {
+        if (row < item.rows) write_rows(p, item, head, rows, row, l, lane >> 5);
+    });
+}
+
 // Bytes of LDS in which `Waves` wavefronts leave the results of NRows rows.
 template <int D, int Waves, int NRows> constexpr int joined_bytes() {
     return Waves * NRows * (D + 4) * 4;

@@ -148,68 +148,121 @@ template <class T, int D, int Bits, bool V> struct Keys {
     }
 };
 
-// 32 query rows for each of Waves wavefronts (block: 4, wide: 8), tiles of 64 keys in two
-// buffers: while one is in use the next is on its way through registers into the
-// other.  Eight wavefronts share the work of K and V, four do both.
-template <class T, int D, int Bits, int Waves>
-__device__ __forceinline__ void attend_rows(const taps_mx_attend_launch &p, const taps_plan_item &item,
-                                            uint32_t head, char *lds) {
-    constexpr int kPart = kWideKeys * Tile<D>::kRow;
+// 128 query rows, 32 for each of four wavefronts, tiles of 64 keys in two buffers: while one is in use
+// the next is on its way through registers into the other.  With Split 2 there are four more
+// wavefronts, which take every second tile; the results are joined in LDS.
+template <class T, int D, int Bits, int Split>
+__device__ __forceinline__ void attend_block(const taps_mx_attend_launch &p, const taps_plan_item &item,
+                                             uint32_t head, char *lds) {
+    constexpr int kPart = kWideKeys * Tile<D>::kRow, kStep = Split * kWideKeys;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int share = Split == 1 ? 0 : wave >> 2, mine = 16 * (wave & 3);   // keys of a tile to load
     const int32_t *pages = p.pages + item.page0;
     const int start = item.lo & ~15;
     // no tile of an item without keys: its lo need not be a multiple of 16
     const int hi = item.lo < item.hi ? item.hi : start;
     const float c = p.scale * kLog2e;
-    const int row0 = item.row0 + 32 * wave, row = row0 + (lane & 31);
+    const int row0 = item.row0 + 32 * (wave & 3), row = row0 + (lane & 31);
     Rows<T, D> rows;
     rows.start(p, item, head, row, lane);
     const Seen seen(p, item, row0);
     const Keys<T, D, Bits, false> k(p, item, head, lane);
     const Keys<T, D, Bits, true> v(p, item, head, lane);
     Piece<D, Bits> k_piece, v_piece;
-    const bool takes_k = Waves == 4 || wave < 4, takes_v = Waves == 4 || wave >= 4;
-    const int mine = 16 * (wave & 3);
-    int page = start < hi ? page_at(p, pages, start + mine, item.lo, item.hi) : 0;
+    const int first = start + kWideKeys * share;
+    int page = start < hi ? page_at(p, pages, first + mine, item.lo, item.hi) : 0;
     const auto fetch = [&](int t0) {
         if (t0 >= hi) return;
-        if (takes_k) k.fetch(k_piece, k.nearest(t0 + mine, page));
-        if (takes_v) v.fetch(v_piece, v.nearest(t0 + mine, page));
-        page = page_at(p, pages, t0 + kWideKeys + mine, item.lo, item.hi);
+        k.fetch(k_piece, k.nearest(t0 + mine, page));
+        v.fetch(v_piece, v.nearest(t0 + mine, page));
+        page = page_at(p, pages, t0 + kStep + mine, item.lo, item.hi);
     };
     const auto put = [&](int t0, char *tile) {
         if (t0 >= hi) return;
-        if (takes_k) k.put(k_piece, tile, mine, t0 + mine);
-        if (takes_v) v.put(v_piece, tile + kPart, mine, t0 + mine);
+        k.put(k_piece, tile, mine, t0 + mine);
+        v.put(v_piece, tile + kPart, mine, t0 + mine);
     };
-    fetch(start);
-    put(start, lds);
+    char *buffers = lds + 4 * kPart * share;
+    fetch(first);
+    put(first, buffers);
     __syncthreads();
     int buffer = 0;
-    for (int t0 = start; t0 < hi; t0 += kWideKeys, buffer ^= 1) {
-        const char *tile = lds + 2 * buffer * kPart;
-        fetch(t0 + kWideKeys);
-        if (t0 < seen.end) {
+    // every share takes the same number of steps
+    for (int at = start, t0 = first; at < hi; at += kStep, t0 += kStep, buffer ^= 1) {
+        const char *tile = buffers + 2 * buffer * kPart;
+        fetch(t0 + kStep);
+        if (t0 < min(hi, seen.end)) {
             typename Rows<T, D>::template Scores<kWideKeys> x;
             typename Rows<T, D>::template Numerators<kWideKeys> y;
             rows.score(tile, x, lane);
             rows.soften(x, y, t0, seen.masks(t0, kWideKeys), c, lane);
             rows.spend(tile + kPart, y, lane);
         }
-        put(t0 + kWideKeys, lds + 2 * (buffer ^ 1) * kPart);
+        put(t0 + kStep, buffers + 2 * (buffer ^ 1) * kPart);
         __syncthreads();
     }
-    const float l = rows.total();
+    float l = rows.total();
+    if constexpr (Split > 1) {
+        float *left = (float *)lds + (row - item.row0) * (D + 8);   // results, maximum, sum
+        if (share) {
+            leave_row(rows, 1.f, left, lane);
+            if (lane < 32) left[D] = rows.m, left[D + 1] = l;
+        }
+        __syncthreads();
+        if (share) return;
+        const float other = left[D], m = fmaxf(rows.m, other);
+        const float by = rows.m == kMinusInf ? 1.f : __builtin_amdgcn_exp2f((rows.m - m) * c);
+        const float by_other = other == kMinusInf ? 1.f : __builtin_amdgcn_exp2f((other - m) * c);
+        rows.m = m, l = l * by + left[D + 1] * by_other;
+#pragma unroll
+        for (int b = 0; b < D / 32; ++b)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const f32x4 o = *(const f32x4 *)(left + 32 * b + 8 * i + 4 * (lane >> 5));
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                    rows.o[b][4 * i + j] = rows.o[b][4 * i + j] * by + o[j] * by_other;
+            }
+    }
     finish(p, item, MxCache<T, Bits>(p, head), rows, seen, row, l, start, 32, lane, [&]() {
         if (row < item.rows) write_rows(p, item, head, rows, row, l, lane >> 5);
     });
 }
 
+// Loads of a wide item's wavefront: a tile's codes wait in registers until the tile before is on its
+// way to LDS, in numbers.
+template <class T, int D, int Bits> struct MxLoader {
+    static constexpr int kAhead = 1;
+    const Keys<T, D, Bits, false> k;
+    const Keys<T, D, Bits, true> v;
+    Piece<D, Bits> piece;
+    const int key0;
+    const bool second;
+    __device__ __forceinline__ MxLoader(const taps_mx_attend_launch &p, const taps_plan_item &item,
+                                        uint32_t head, bool values, int wave, int lane)
+        : k(p, item, head, lane), v(p, item, head, lane), key0(16 * (wave & 3)), second(values) {}
+    __device__ __forceinline__ void start(int t0, int page) {
+        if (second)
+            v.fetch(piece, v.nearest(t0 + key0, page));
+        else
+            k.fetch(piece, k.nearest(t0 + key0, page));
+    }
+    __device__ __forceinline__ void load(int t0, int page, const char *part) {
+        if (second)
+            v.put(piece, const_cast<char *>(part), key0, t0 + key0);
+        else
+            k.put(piece, const_cast<char *>(part), key0, t0 + key0);
+        start(t0 + kWideKeys, page);
+    }
+    __device__ __forceinline__ void wait(bool) const {}
+};
+
 template <class T, int D, int Bits>
 __global__ __launch_bounds__(kWideThreads, 2) void k_mx_attend_wide(taps_mx_attend_launch p) {
-    __shared__ __attribute__((aligned(16))) char lds[2 * Tile<D>::bytes(kWideKeys)];
+    __shared__ __attribute__((aligned(16))) char lds[6 * kWideKeys * Tile<D>::kRow];
     const uint32_t head = blockIdx.x % p.kv_heads;
-    attend_rows<T, D, Bits, 8>(p, p.items[blockIdx.x / p.kv_heads], head, lds);
+    const taps_plan_item item = p.items[blockIdx.x / p.kv_heads];
+    attend_wide<T, D, MxLoader<T, D, Bits>>(p, item, head, MxCache<T, Bits>(p, head), lds);
 }
 
 // What a wavefront wrote to LDS is read by its other lanes, and before it is written anew.
@@ -621,7 +674,7 @@ __global__ __launch_bounds__(64 * Waves, Waves == 4 ? 3 : 2) void k_mx_attend_fe
     attend_few<T, D, Bits, Waves>(p, p.items[blockIdx.x / p.kv_heads], head, lds);
 }
 
-// A block or a narrow item; both fit a unit twice.
+// Any item but a wide one; two fit a unit.
 template <class T, int D, int Bits>
 __global__ __launch_bounds__(kThreads, 2) void k_mx_attend(taps_mx_attend_launch p) {
     __shared__ __attribute__((aligned(16))) char lds[max_of(
@@ -629,11 +682,24 @@ __global__ __launch_bounds__(kThreads, 2) void k_mx_attend(taps_mx_attend_launch
     const uint32_t head = blockIdx.x % p.kv_heads;
     const taps_plan_item item = p.items[blockIdx.x / p.kv_heads];
     if (item.kind == kBlock)
-        attend_rows<T, D, Bits, 4>(p, item, head, lds);
+        attend_block<T, D, Bits, 1>(p, item, head, lds);
     else if (item.rows - item.row0 <= kFewRows)
         attend_few<T, D, Bits, kWaves>(p, item, head, lds);
     else
         attend_narrow<T, D, Bits>(p, item, head, lds);
+}
+
+// The same with a unit for each: twice the wavefronts share its keys.
+template <class T, int D, int Bits>
+__global__ __launch_bounds__(2 * kThreads, 2) void k_mx_attend_alone(taps_mx_attend_launch p) {
+    constexpr int kBlockBytes = max_of(4 * Tile<D>::bytes(kWideKeys), kBlockRows * (D + 8) * 4);
+    __shared__ __attribute__((aligned(16))) char lds[max_of(few_bytes<D, 2 * kWaves>(), kBlockBytes)];
+    const uint32_t head = blockIdx.x % p.kv_heads;
+    const taps_plan_item item = p.items[blockIdx.x / p.kv_heads];
+    if (item.kind == kNarrow && item.rows - item.row0 <= kFewRows)
+        attend_few<T, D, Bits, 2 * kWaves>(p, item, head, lds);
+    else
+        attend_block<T, D, Bits, 2>(p, item, head, lds);
 }
 
 template <class T, int D, int Bits> void launch_items(taps_mx_attend_launch p, hipStream_t stream) {
@@ -643,17 +709,17 @@ template <class T, int D, int Bits> void launch_items(taps_mx_attend_launch p, h
         });
     p.items += p.n_wide;
     const uint32_t others = p.n_items - p.n_wide;
-    if (p.n_few == others)
-        in_slices(p, others, 512, [&](const auto &s, uint32_t groups) {
-            if (groups <= kUnits)
-                k_mx_attend_few<T, D, Bits, 8><<<groups, 512, 0, stream>>>(s);
-            else
-                k_mx_attend_few<T, D, Bits, 4><<<groups, 256, 0, stream>>>(s);
-        });
-    else
-        in_slices(p, others, kThreads, [&](const auto &s, uint32_t groups) {
+    const bool few = p.n_few == others;
+    in_slices(p, others, 2 * kThreads, [&](const auto &s, uint32_t groups) {
+        if (few && groups <= kUnits)
+            k_mx_attend_few<T, D, Bits, 8><<<groups, 512, 0, stream>>>(s);
+        else if (few)
+            k_mx_attend_few<T, D, Bits, 4><<<groups, 256, 0, stream>>>(s);
+        else if (groups <= kUnits)
+            k_mx_attend_alone<T, D, Bits><<<groups, 2 * kThreads, 0, stream>>>(s);
+        else
             k_mx_attend<T, D, Bits><<<groups, kThreads, 0, stream>>>(s);
-        });
+    });
 }
 
 template <class T, int Bits>
