@@ -183,14 +183,18 @@ def taps_mx_read(k_cache: MxPages, v_cache: MxPages, slots, head_dim: int, dtype
     shape = slots.shape[0], heads, head_dim
     if out is None:
         # one piece of memory: an allocation less
-        k, v = _on(stream, lambda: torch.empty((2, *shape), dtype=dtype, device=slots.device)).unbind()
+        both = _on(stream, lambda: torch.empty((2, *shape), dtype=dtype, device=slots.device))
+        k, v = both.unbind()
+        at, row = both.data_ptr(), heads * head_dim
+        kh = Heads(at, 0, row, head_dim)
+        vh = Heads(at + shape[0] * row * both.element_size(), 0, row, head_dim)
     else:
         k, v = out
         dtype = k.dtype
+        kh, vh = _heads(k, "k", device, dtype, shape, 3), _heads(v, "v", device, dtype, shape, 3)
     args = ReadArgs(_dtype(k), k_cache.bits, shape[0], heads, head_dim, page_size, n_pages,
                     slots.element_size(), slots.data_ptr())
-    _check(load().taps_mx_read(C.byref(args), kc, vc, _heads(k, "k", device, dtype, shape, 3),
-                               _heads(v, "v", device, dtype, shape, 3), raw), "taps_mx_read")
+    _check(load().taps_mx_read(C.byref(args), kc, vc, kh, vh, raw), "taps_mx_read")
     return k, v
 
 

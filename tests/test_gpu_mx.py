@@ -295,6 +295,14 @@ MORE = [
     ([5, 1], [640, 1300], 8, 2, 64, 32, {"units": 4096}),
     ([4], [9000], 4, 1, 128, 64, {"units": 4096, "window": 5000}),
     ([2, 2], [700, 30], 8, 2, 104, 16, {"kv_starts": [300, 29]}),
+    # more items than units: of 128 rows, of 17 to 32 and of up to 16
+    ([40] * 11 + [10] * 12 + [3] * 12, [40] * 11 + [150, 11, 32, 31] * 6, 16, 8, 128, 16, {}),
+    ([40] * 11 + [10] * 12 + [3] * 12, [90] * 11 + [150, 11, 32, 31] * 6, 16, 8, 64, 32,
+     {"window": 30}),
+    ([40] * 11 + [9] * 12 + [3] * 12, [70] * 11 + [150, 11, 32, 31] * 6, 16, 8, 96, 64,
+     {"kv_starts": [33] * 11 + [7] * 24}),
+    ([1] * 30 + [4] * 5, [5, 700, 64, 65, 33] * 7, 32, 8, 128, 16, {}),
+    ([1] * 30 + [4] * 5, [5, 700, 64, 65, 33] * 7, 32, 8, 72, 64, {"window": 50}),
 ]
 
 
@@ -379,6 +387,9 @@ def test_attend_many_small_numerators(dtype, bits):
     ([3], [1500], 4, 2, 96, 64, {"units": 4096}),
     ([300], [1700], 4, 2, 128, 64, {"units": 1}),            # 256 rows an item
     ([300], [2900], 4, 2, 80, 16, {"units": 1, "window": 1500}),
+    # more items than units
+    ([40] * 12 + [10] * 12 + [3] * 12, [60] * 12 + [150, 11, 32, 31] * 6, 16, 8, 128, 16, {}),
+    ([3] * 40, [60, 70, 150, 11, 32] * 8, 8, 8, 64, 16, {"window": 25}),
 ])
 def test_attend_blocks_of_nan(spec, dtype, bits):
     """Blocks that are NaN, among the new tokens and before: they reach the tokens that see them
