@@ -7,6 +7,8 @@ runs the share of the device that holds the last tokens, whose queries see the
 most keys: the earlier tokens' keys are in a paged cache; the chunk's queries are
 normed and rotated, its keys and values appended on the way, and attended.  The
 printed times stand beside the communication seconds that the plan was chosen by.
+With ``--cache-bits`` 4 or 8 the cache is held in a microscaling format; the sequence is then
+also read back, as it would be to hand it to another device.
 """
 from __future__ import annotations
 
@@ -55,12 +57,17 @@ def _slots(share: Share):
         share.batch * per_seq
 
 
-def run(share: Share, dtype, repeats: int = 10, seed: int = 0):
+def run(share: Share, dtype, repeats: int = 10, seed: int = 0, cache_bits: int = 16):
     """Runs the share on random projections; {step: seconds} and the largest difference
     of a few rows from 64-bit attention over the same cache, relative to it."""
     import torch
 
-    from . import attention
+    from . import attention, mx
+    if cache_bits not in (4, 8, 16):
+        raise ValueError(f"a cache of {cache_bits} bits")
+    append_to, attend_over = attention.taps_cache_append, attention.taps_attend
+    if cache_bits < 16:
+        append_to, attend_over = mx.taps_mx_append, mx.taps_mx_attend
     gen = torch.Generator(device="cuda")
     gen.manual_seed(seed)
 
@@ -73,11 +80,17 @@ def run(share: Share, dtype, repeats: int = 10, seed: int = 0):
     table = attention.rotation_table(keys, dim)
     q_weight, k_weight = (1 + 0.1 * randn(dim) for _ in range(2))
     q, k, v = randn(b * new, 3 * n, dim).split(n, dim=1)   # as one projection leaves them
-    caches = [torch.zeros((n_pages, n, PAGE, dim), dtype=dtype, device="cuda") for _ in range(2)]
+    if cache_bits < 16:
+        caches = [mx.new_pages(n_pages, n, PAGE, dim, cache_bits) for _ in range(2)]
+        slots = torch.from_numpy(pages).cuda().long()[:, torch.arange(keys).cuda() // PAGE] * PAGE + \
+            torch.arange(keys).cuda() % PAGE
+    else:
+        caches = [torch.zeros((n_pages, n, PAGE, dim), dtype=dtype, device="cuda")
+                  for _ in range(2)]
     if old:   # the earlier chunks' keys, which other devices projected
         before = attention.PagedPlan([old] * b, [old] * b, pages, **shape)
-        attention.taps_cache_append(randn(b * old, n, dim), randn(b * old, n, dim), *caches, before,
-                                    table=table, k_weight=k_weight)
+        append_to(randn(b * old, n, dim), randn(b * old, n, dim), *caches, before, table=table,
+                  k_weight=k_weight)
     plan = attention.PagedPlan([new] * b, [keys] * b, pages, **shape)
     chunk = q.unflatten(0, (b, new))
     state = {}
@@ -90,12 +103,15 @@ def run(share: Share, dtype, repeats: int = 10, seed: int = 0):
                                             first=old)
 
     def append():
-        attention.taps_cache_append(k, v, *caches, plan, table=table, k_weight=k_weight)
+        append_to(k, v, *caches, plan, table=table, k_weight=k_weight)
 
     def attend():
-        state["out"] = attention.taps_attend(state["q"].flatten(0, 1), *caches, plan)
+        state["out"] = attend_over(state["q"].flatten(0, 1), *caches, plan)
+
+    def read():
+        state["kv"] = mx.taps_mx_read(*caches, slots.flatten(), dim, dtype)
     seconds = {}
-    for step in (norm_rotate, gradients, append, attend):
+    for step in (norm_rotate, gradients, append, attend, *((read,) if cache_bits < 16 else ())):
         step()
         start, end = (torch.cuda.Event(enable_timing=True) for _ in range(2))
         start.record()
@@ -104,16 +120,21 @@ def run(share: Share, dtype, repeats: int = 10, seed: int = 0):
         end.record()
         end.synchronize()
         seconds[step.__name__] = start.elapsed_time(end) * 1e-3 / repeats
-    return seconds, _difference(share, state, caches, pages)
+    if cache_bits < 16:
+        kept = [x.unflatten(0, (b, keys)).transpose(1, 2) for x in state["kv"]]
+    else:
+        kept = [c[torch.from_numpy(pages).long()].transpose(1, 2).flatten(2, 3) for c in caches]
+    return seconds, _difference(share, state, kept)
 
 
-def _difference(share: Share, state, caches, pages) -> float:
+def _difference(share: Share, state, kept) -> float:
+    """kept: keys and values [sequences, heads, keys and more, dim]."""
     worst = 0.0
     rng = np.random.default_rng(1)
     for _ in range(4):
         s, t, h = (int(rng.integers(x)) for x in (share.batch, share.tokens, share.heads))
         seen = share.keys - share.tokens + t + 1
-        k, v = (c[pages[s], h].flatten(0, 1)[:seen].double().cpu().numpy() for c in caches)
+        k, v = (c[s, h, :seen].double().cpu().numpy() for c in kept)
         q = state["q"][s, t, h].double().cpu().numpy()
         p = k @ q * share.dim ** -0.5
         p = np.exp(p - p.max())
@@ -133,6 +154,8 @@ def main() -> int:
     ap.add_argument("--config", type=int, default=3, choices=(2, 3, 5),
                     help="workloads.config of the transformer (one layer is planned)")
     ap.add_argument("--repeats", type=int, default=10)
+    ap.add_argument("--cache-bits", type=int, default=16, choices=(4, 8, 16),
+                    help="of an element of the cache: 16, or a microscaling format's")
     ap.add_argument("--time-limit", type=float, default=300.0, help="seconds for the ILP")
     args = ap.parse_args()
 
@@ -156,11 +179,12 @@ def main() -> int:
     share = share_of(op, log2_degrees[int(tables.op_offsets[scores]) + plan.choice[scores]]
                      [:op.n_axes])
     dtype = torch.float16 if "fp16" in w.name else torch.bfloat16
-    seconds, difference = run(share, dtype, args.repeats)
+    seconds, difference = run(share, dtype, args.repeats, cache_bits=args.cache_bits)
     print(json.dumps({
         "workload": f"{w.name} / {name}", "plan_communication_s": plan.objective,
         "share": {"sequences": share.batch, "heads": share.heads, "query_tokens": share.tokens,
                   "keys": share.keys, "head_dim": share.dim},
+        "cache_bits": args.cache_bits,
         "seconds": seconds, "attend_tflops": share.flops / seconds["attend"] * 1e-12,
         "difference": difference}), flush=True)
     return 0
