@@ -96,12 +96,12 @@ struct Place {
 struct HalfCache {
     typedef Place At;
     const taps_attend_launch &p;
-    const char *k_head, *v_head;
-    __device__ __forceinline__ HalfCache(const taps_attend_launch &launch, uint32_t head)
-        : p(launch), k_head(p.k_cache + (int64_t)head * p.k_head),
-          v_head(p.v_cache + (int64_t)head * p.v_head) {}
+    const uint32_t head;
+    __device__ __forceinline__ HalfCache(const taps_attend_launch &launch, uint32_t h)
+        : p(launch), head(h) {}
     __device__ __forceinline__ Place at(int page, int key) const {
-        return Place(p, k_head, v_head, page, key);
+        return Place(p, p.k_cache + (int64_t)head * p.k_head, p.v_cache + (int64_t)head * p.v_head, page,
+                     key);
     }
     __device__ __forceinline__ const char *row(const Place &a, const Place &b, bool second,
                                                uint32_t slot) const {

@@ -92,7 +92,7 @@ template <int D> struct Tile {
         return (((key >> 1) & 1) | ((key >> 1) & 2)) ^ ((key >> 3) & 1);   // the low two bits
     }
     static __device__ __forceinline__ int v_mask(int key) {
-        if (D == 128) return 4 * (key & 1) + 5 * (key & 2);
+        if (D == 128) return 4 * (key & 3) + ((key >> 2) & 1);
         if (D == 64) return 2 * (key & 1) + 2 * (key & 2);
         return key & 2;
     }

@@ -148,8 +148,8 @@ template <class T, int D, int Bits, bool V> struct Keys {
     }
 };
 
-// 128 query rows, 32 for each of four wavefronts, tiles of 64 keys in two buffers: while one is in use
-// the next is on its way through registers into the other.  With Split 2 there are four more
+// 128 query rows, 32 for each of four wavefronts, tiles of 64 keys in two buffers: before one is used
+// the next, which came to registers meanwhile, goes to the other.  With Split 2 there are four more
 // wavefronts, which take every second tile; the results are joined in LDS.
 template <class T, int D, int Bits, int Split>
 __device__ __forceinline__ void attend_block(const taps_mx_attend_launch &p, const taps_plan_item &item,
@@ -185,12 +185,14 @@ __device__ __forceinline__ void attend_block(const taps_mx_attend_launch &p, con
     char *buffers = lds + 4 * kPart * share;
     fetch(first);
     put(first, buffers);
+    fetch(first + kStep);
     __syncthreads();
     int buffer = 0;
     // every share takes the same number of steps
     for (int at = start, t0 = first; at < hi; at += kStep, t0 += kStep, buffer ^= 1) {
         const char *tile = buffers + 2 * buffer * kPart;
-        fetch(t0 + kStep);
+        put(t0 + kStep, buffers + 2 * (buffer ^ 1) * kPart);
+        fetch(t0 + 2 * kStep);
         if (t0 < min(hi, seen.end)) {
             typename Rows<T, D>::template Scores<kWideKeys> x;
             typename Rows<T, D>::template Numerators<kWideKeys> y;
@@ -198,7 +200,6 @@ __device__ __forceinline__ void attend_block(const taps_mx_attend_launch &p, con
             rows.soften(x, y, t0, seen.masks(t0, kWideKeys), c, lane);
             rows.spend(tile + kPart, y, lane);
         }
-        put(t0 + kStep, buffers + 2 * (buffer ^ 1) * kPart);
         __syncthreads();
     }
     float l = rows.total();
@@ -676,7 +677,7 @@ __global__ __launch_bounds__(64 * Waves, Waves == 4 ? 3 : 2) void k_mx_attend_fe
 
 // Any item but a wide one; two fit a unit.
 template <class T, int D, int Bits>
-__global__ __launch_bounds__(kThreads, 2) void k_mx_attend(taps_mx_attend_launch p) {
+__global__ __launch_bounds__(kThreads, D <= 64 ? 3 : 2) void k_mx_attend(taps_mx_attend_launch p) {
     __shared__ __attribute__((aligned(16))) char lds[max_of(
         max_of(narrow_bytes<D>(), few_bytes<D, kWaves>()), 2 * Tile<D>::bytes(kWideKeys))];
     const uint32_t head = blockIdx.x % p.kv_heads;
