@@ -149,6 +149,8 @@ int64_t piece_of(const std::vector<Strip> &strips, int32_t kind, int64_t cus, in
     return best;
 }
 
+bool is_few(const taps_plan_item &i) { return i.kind == kNarrow && i.rows - i.row0 <= kFewRows; }
+
 // The order in which items start: kind by kind.  Workgroups that run at the same
 // time should find each other's keys in the cache, and the last ones to start
 // should be cheap.  So the items of a sequence follow each other, its dear ones
@@ -158,8 +160,6 @@ int64_t piece_of(const std::vector<Strip> &strips, int32_t kind, int64_t cus, in
 // so, 321 by sequences alone; 20 of 100 to 700 tokens: 107, 108 and 119).
 // Narrow items share no keys: dear ones first, but those of few rows last, for which there are
 // kernels of their own.
-bool is_few(const taps_plan_item &i) { return i.kind == kNarrow && i.rows - i.row0 <= kFewRows; }
-
 void in_order(std::vector<taps_plan_item> *items, int64_t cus, int64_t heads) {
     const auto cost = [](const taps_plan_item &i) { return Strip::cost_of(i.kind, i.hi - i.lo); };
     const auto dear = [&](const taps_plan_item &x, const taps_plan_item &y) {

@@ -10,6 +10,15 @@
 // Eight elements a lane: four lanes are a block, and meet for its largest magnitude.
 // A rotated element's other half of the pair is in another lane (but for neighbouring
 // pairs); lanes hand them over through LDS, inside a wavefront.
+//
+// Bytes bound both: a row is read and written once.  A group of lanes takes all heads of its token,
+// so that a wavefront's groups read and write neighbouring slots of a head at a time, whole lines;
+// with a token's heads over the groups a launch touched half lines all over the pages.
+//   append   16384 tokens, 32 heads of 128 bf16, keys normed and rotated, to 4 bits: 268 MB in,
+//            71 out, 84 us, 4.0 TB/s (about 130 with heads over the groups)
+//   read     the same back: 71 in, 268 out, 62 us, 5.5 TB/s
+//            147 thousand tokens of 8 heads: 124 in, 602 out, 127 us, 5.7 TB/s (240)
+// Few tokens only wait for memory: 64 of 8 heads 4.5 and 3.1 us.
 #include "taps_lanes.h"
 #include "taps_mx_device.h"
 #include "taps_mx_internal.h"
@@ -100,7 +109,9 @@ template <bool Vectors> struct Turn {
     }
 };
 
-// 1 / sqrt(v) in 64 bits: the instruction's half precision and two steps of Newton's.
+// 1 / sqrt(v) in 64 bits: the instruction's approximation and two steps of Newton's.  With the
+// sum in 64 bits too, a key's codes do not hang on the order in which a wavefront adds: an element
+// next to the border between two codes would show it.
 __device__ __forceinline__ double inverse_root(double v) {
     double y = __builtin_amdgcn_rsq(v);
     if (v == 0.0 || v == __builtin_inf()) return y;

@@ -1,10 +1,17 @@
 // taps_mx_attend.hip -- attention of new tokens over a paged cache in microscaling
 // formats.
 //
-// The mathematics, the kinds of items and the layouts of both products are
-// those of taps_attend.hip.  Keys and values become 16-bit numbers (exact but at the
-// ends of fp16's range) on their way to LDS: a lane fetches a quarter of a key, waits
-// for it while the tile before is in use, and converts two elements an instruction.
+// The mathematics, the kinds of items and, but for those of up to 16 rows, the layouts of both
+// products are those of taps_attend.hip.  Codes come to registers and become 16-bit numbers there,
+// two an instruction with their power of two (exact but at the ends of fp16's range): for items of
+// many rows once on the way to LDS, where all rows share them; for those of few rows where the
+// products want them.  Products of codes themselves (fp4 by fp8 with scales), which would save the
+// conversions of keys, hold their sums to 2^-12 of the largest term and were not taken.
+//
+// Kernels, by the items of a launch (without the wide ones, which have their own):
+//   k_mx_attend_few     all of up to 16 rows;
+//   k_mx_attend_alone   others, no more than there are units: eight wavefronts to each;
+//   k_mx_attend         others.
 #include "taps_attend_device.h"
 #include "taps_mx_device.h"
 #include "taps_mx_internal.h"
@@ -231,7 +238,9 @@ __device__ __forceinline__ void attend_block(const taps_mx_attend_launch &p, con
 }
 
 // Loads of a wide item's wavefront: a tile's codes wait in registers until the tile before is on its
-// way to LDS, in numbers.
+// way to LDS, in numbers.  The conversions fall into the phase of the softmax, beside the other half's
+// products: 8 prompts of 2048, 32 heads of 128, 325 us in 4 bits and 336 to 358 in 8 by the card (316 to
+// 349 over a 16-bit cache; 405 without the phases), 512 tokens over 32768 keys 241 to 252 (246).
 template <class T, int D, int Bits> struct MxLoader {
     static constexpr int kAhead = 1;
     const Keys<T, D, Bits, false> k;
@@ -328,6 +337,15 @@ __device__ __forceinline__ void attend_narrow(const taps_mx_attend_launch &p,
 // keys for one row, half of what it has in the others' tiles.  Keys go from the registers that they
 // are fetched to into the first product: a lane's quarter of a key is its part of
 // the operand, with the queries laid out the same.  Values pass through LDS to be transposed.
+// Every wavefront has two tiles on their way, each in registers of its own.
+//
+// Bytes bound it.  Two tokens over 131001 keys, 8 heads of 128 in 4 bits: 285 MB in 54 us, 5.3 TB/s,
+// and 5 for the join; the loads alone, with the join, take 57.4 of the 59.5 us.  64 tokens over up to
+// 4000 keys: 160 MB in 33 and 5 (loads alone 38.8 of 39.4).  24 times four tokens over up to 9999 in 8
+// bits: 280 MB in 59 and 5 (loads alone 62 to 67 of 66, by whether lanes take them in the order of
+// memory; values do, keys in that order would have to pass through LDS, which cost a lone token 3 us
+// of 11).  With one tile on its way they took 64, 44.7 and 75; with 32x32x16 tiles, keys through
+// LDS and half of the lanes' scores of rows that are not there 75, 54 and 77.
 template <class T> struct SmallMfma;
 template <> struct SmallMfma<__bf16> {
     static __device__ __forceinline__ f32x4 run(s16x8 a, s16x8 b, f32x4 c) {
@@ -343,13 +361,14 @@ template <> struct SmallMfma<_Float16> {
     }
 };
 
-// LDS image of 32 values: rows of 16-byte chunks, permuted by a mask of the key's number.  Eight keys'
-// writes of one chunk, and reads of two chunks of four keys, fall on different banks.
+// LDS image of 32 values: rows of 16-byte chunks, permuted by a mask of the key's number.  16 lanes
+// write a chunk of each block of four keys (heads of up to 64: eight), 32 read two chunks of eight
+// keys: the mask's lowest two bits differ among the first, the others among the second.
 template <int D> struct Values {
     static constexpr int kRow = D <= 64 ? 128 : 256, kBytes = kNarrowKeys * kRow;
     static __device__ __forceinline__ int mask(int key) {
-        const int m = 2 * (key & 3) + ((key >> 2) & 1);
-        return D <= 64 ? m : m + (key & 8);
+        if (D <= 64) return (key & 2) + 5 * ((key >> 2) & 1);
+        return 2 * (key & 1) + 5 * ((key >> 1) & 1) + 2 * (key & 4);
     }
 };
 
@@ -675,7 +694,9 @@ __global__ __launch_bounds__(64 * Waves, Waves == 4 ? 3 : 2) void k_mx_attend_fe
     attend_few<T, D, Bits, Waves>(p, p.items[blockIdx.x / p.kv_heads], head, lds);
 }
 
-// Any item but a wide one; two fit a unit.
+// Any item but a wide one; two fit a unit, three for heads of up to 64.  8 prompts of 1024, 16 heads of
+// 64 in 4 bits: 41 us (32 over a 16-bit cache, whose tiles go past the registers); the conversions and
+// the waits for them at a short item's start are what it has more.
 template <class T, int D, int Bits>
 __global__ __launch_bounds__(kThreads, D <= 64 ? 3 : 2) void k_mx_attend(taps_mx_attend_launch p) {
     __shared__ __attribute__((aligned(16))) char lds[max_of(
@@ -690,7 +711,8 @@ __global__ __launch_bounds__(kThreads, D <= 64 ? 3 : 2) void k_mx_attend(taps_mx
         attend_narrow<T, D, Bits>(p, item, head, lds);
 }
 
-// The same with a unit for each: twice the wavefronts share its keys.
+// The same with a unit for each: twice the wavefronts share its keys.  Prompts of up to 701 tokens
+// and single ones, 212 items of up to 17 tiles one after the other: 24.8 us, 32.8 without.
 template <class T, int D, int Bits>
 __global__ __launch_bounds__(2 * kThreads, 2) void k_mx_attend_alone(taps_mx_attend_launch p) {
     constexpr int kBlockBytes = max_of(4 * Tile<D>::bytes(kWideKeys), kBlockRows * (D + 8) * 4);
