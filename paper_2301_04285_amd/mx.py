@@ -23,7 +23,7 @@ import torch
 
 from . import attention
 from .attention import (AppendArgs, Heads, PagedPlan, _DTYPES, _check, _device, _dtype, _heads,
-                        _no_gradient, _on, _on_gpu, _output, _stream, _table, _vector)
+                        _like, _no_gradient, _on, _on_gpu, _output, _stream, _table, _vector)
 
 HEADER = os.path.join(os.path.dirname(attention.HEADER), "taps_mx.h")
 
@@ -182,12 +182,10 @@ def taps_mx_read(k_cache: MxPages, v_cache: MxPages, slots, head_dim: int, dtype
     kc, vc = _caches(k_cache, v_cache, device, n_pages, (heads, page_size, head_dim))
     shape = slots.shape[0], heads, head_dim
     if out is None:
-        # one piece of memory: an allocation less
-        both = _on(stream, lambda: torch.empty((2, *shape), dtype=dtype, device=slots.device))
-        k, v = both.unbind()
-        at, row = both.data_ptr(), heads * head_dim
-        kh = Heads(at, 0, row, head_dim)
-        vh = Heads(at + shape[0] * row * both.element_size(), 0, row, head_dim)
+        k = _on(stream, lambda: torch.empty(shape, dtype=dtype, device=slots.device))
+        v = _on(stream, lambda: _like(k))
+        row = heads * head_dim
+        kh, vh = Heads(k.data_ptr(), 0, row, head_dim), Heads(v.data_ptr(), 0, row, head_dim)
     else:
         k, v = out
         dtype = k.dtype

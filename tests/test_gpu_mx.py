@@ -225,6 +225,19 @@ def test_read_refuses_no_slots_and_fills_what_it_is_given():
     assert none[0].shape == (0, 2, 64)
 
 
+def test_read_results_stand_apart():
+    """One result changes while autograd has the other in use."""
+    caches = [mx.new_pages(2, 2, 16, 64, 8) for _ in range(2)]
+    k, v = mx.taps_mx_read(*caches, torch.arange(20, device="cuda"), 64, torch.float32)
+    w = torch.ones(64, device="cuda", requires_grad=True)
+    total = (w * (k + 1)).sum() + (w * k).sum()
+    v.fill_(3.0)
+    total.backward()
+    assert torch.equal(w.grad, torch.full_like(w, 40.0))
+    v.mul_(w)
+    assert v.requires_grad and not k.requires_grad
+
+
 def test_append_and_read_back():
     """What is read is what the codes stand for, the nearest to what was appended."""
     g = gen_of(2)
