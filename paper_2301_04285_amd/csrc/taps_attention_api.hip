@@ -158,8 +158,7 @@ bool is_few(const taps_plan_item &i) { return i.kind == kNarrow && i.rows - i.ro
 // every slot: of those the dear items come first, whatever their sequence
 // (prompts of 2048 of eight sequences, 32 heads: 350 us with all dear items first, 321
 // so, 321 by sequences alone; 20 of 100 to 700 tokens: 107, 108 and 119).
-// Narrow items share no keys: dear ones first, but those of few rows last, for which there are
-// kernels of their own.
+// Narrow items share no keys: dear ones first.
 void in_order(std::vector<taps_plan_item> *items, int64_t cus, int64_t heads) {
     const auto cost = [](const taps_plan_item &i) { return Strip::cost_of(i.kind, i.hi - i.lo); };
     const auto dear = [&](const taps_plan_item &x, const taps_plan_item &y) {
@@ -191,8 +190,6 @@ void in_order(std::vector<taps_plan_item> *items, int64_t cus, int64_t heads) {
         std::stable_sort(rest, end, dear);
         at = end;
     }
-    std::stable_partition(items->begin(), items->end(),
-                          [](const taps_plan_item &i) { return !is_few(i); });
 }
 
 // Whether sequences of more than 128 rows are cut into strips of 256 rows (wide

@@ -33,7 +33,7 @@ struct taps_plan_header {
     uint32_t appendable;      // every sequence has kv_lens >= q_lens
     uint32_t join_rounds;     // workgroups that the rows of a join are spread over, at most
     uint32_t n_wide;
-    uint32_t n_few;           // the last n_few items: narrow ones of up to kFewRows rows
+    uint32_t n_few;           // of the items: narrow ones of up to kFewRows rows
     uint32_t zeros[4];        // what attention reads for keys that are not there
     // byte offsets of the arrays
     uint64_t tokens_at, pages_at, items_at, joins_at;
