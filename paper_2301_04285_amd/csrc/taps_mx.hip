@@ -59,7 +59,8 @@ __device__ __forceinline__ Raw<T> fetch(const T *row, int d, int dim) {
 }
 
 // cos and +-sin of a lane's elements, so that y = x cos + partner sin, and their partners'
-// places in the row; elements that are not rotated stay as they are.
+// places in the row.  Elements that are not rotated stay as they are: x 1 + x 0, which is NaN only
+// where x, and so its block, is not finite.
 template <bool Vectors> struct Turn {
     float c[kN], s[kN];
     int d, half;        // first element; rotary / 2
@@ -92,19 +93,20 @@ template <bool Vectors> struct Turn {
     }
     __device__ __forceinline__ bool rotated(int i) const { return d + i < 2 * half; }
     // Partners of elements i of this lane, from the row in LDS.
+    __device__ __forceinline__ int partner(int i) const {
+        return !rotated(i) ? d + i : d + i >= half ? d + i - half : d + i + half;
+    }
     __device__ __forceinline__ void partners(const float *row, float (&y)[kN]) const {
         if (Vectors) {
 #pragma unroll
             for (int g = 0; g < kN; g += 4) {
-                const int at = d + g >= half ? d + g - half : d + g + half;
-                const f32x4 u = *(const f32x4 *)(row + (rotated(g) ? at : 0));
+                const f32x4 u = *(const f32x4 *)(row + partner(g));
 #pragma unroll
                 for (int i = 0; i < 4; ++i) y[g + i] = u[i];
             }
         } else {
 #pragma unroll
-            for (int i = 0; i < kN; ++i)
-                y[i] = rotated(i) ? row[d + i >= half ? d + i - half : d + i + half] : 0.f;
+            for (int i = 0; i < kN; ++i) y[i] = row[partner(i)];
         }
     }
 };
@@ -121,9 +123,17 @@ __device__ __forceinline__ double inverse_root(double v) {
 }
 
 // Sum over groups of Lanes neighbouring lanes, in 64 bits.
+template <int Control> __device__ __forceinline__ double of_lane(double v) {
+    const uint64_t u = __builtin_bit_cast(uint64_t, v);
+    const uint32_t low = __builtin_amdgcn_mov_dpp((int)u, Control, 0xf, 0xf, true);
+    const uint32_t high = __builtin_amdgcn_mov_dpp((int)(u >> 32), Control, 0xf, 0xf, true);
+    return __builtin_bit_cast(double, (uint64_t)high << 32 | low);
+}
 template <int Lanes> __device__ __forceinline__ double row_sum64(double v) {
-#pragma unroll
-    for (int m = 1; m < Lanes; m *= 2) v += __shfl_xor(v, m, 64);
+    v += of_lane<0xb1>(v);   // 1 0 3 2
+    v += of_lane<0x4e>(v);   // 2 3 0 1
+    if (Lanes > 4) v += of_lane<0x141>(v);   // 8 lanes mirrored: the other four
+    if (Lanes > 8) v += of_lane<0x140>(v);   // 16 lanes mirrored: the other eight
     return v;
 }
 
@@ -224,15 +234,19 @@ __global__ __launch_bounds__(kThreads) void k_mx_append(taps_mx_append_launch p)
 #pragma unroll
                 for (int i = 0; i < kN; ++i) sum = __builtin_fma((double)x[i], (double)x[i], sum);
                 const float rstd =
-                    (float)inverse_root(row_sum64<Lanes>(sum) / (double)dim + (double)p.eps);
+                    (float)inverse_root(row_sum64<Lanes>(sum) * p.inverse_dim + (double)p.eps);
 #pragma unroll
-                for (int i = 0; i < kN; ++i) x[i] = d + i < dim ? x[i] * rstd * w[i] : 0.f;
+                for (int i = 0; i < kN; ++i) x[i] = x[i] * rstd * w[i];   // 0 beyond the head: w is
             }
             if (rotates) {
                 float y[kN];
                 if (p.interleaved) {
 #pragma unroll
-                    for (int i = 0; i < kN; ++i) y[i] = x[i ^ 1];
+                    for (int i = 0; i < kN; i += 2) {   // a neighbour's 0 would change the sign of x = -0
+                        const bool turned = turn.rotated(i);
+                        const float u = x[i], v = x[i + 1];
+                        y[i] = turned ? v : u, y[i + 1] = turned ? u : v;
+                    }
                 } else {
                     *(f32x4 *)(row + d) = f32x4{x[0], x[1], x[2], x[3]};
                     *(f32x4 *)(row + d + 4) = f32x4{x[4], x[5], x[6], x[7]};
@@ -247,7 +261,7 @@ __global__ __launch_bounds__(kThreads) void k_mx_append(taps_mx_append_launch p)
 #pragma unroll
                 for (int i = 0; i < kN; ++i) {
                     const float a = x[i] * turn.c[i], b = y[i] * turn.s[i];
-                    x[i] = turn.rotated(i) ? a + b : x[i];
+                    x[i] = a + b;
                 }
             }
             uint32_t top = 0;
@@ -255,13 +269,17 @@ __global__ __launch_bounds__(kThreads) void k_mx_append(taps_mx_append_launch p)
             for (int i = 0; i < kN; ++i)
                 top = max(top, __builtin_bit_cast(uint32_t, x[i]) & 0x7fffffff);
             top = quad_max(top);
-            const bool finite = top < 0x7f800000;   // NaN's bits are the largest
-            top = min(top, __builtin_bit_cast(uint32_t, p.most));
-            const uint32_t byte = finite ? scale_byte<Bits>(top) : TAPS_MX_NAN;
+            const uint32_t most = __builtin_bit_cast(uint32_t, p.most);
+            uint32_t byte = scale_byte<Bits>(min(top, most)), code[kWords<Bits>];
+            if (__builtin_expect(__any(top > most), 0)) {
+                const bool finite = top < 0x7f800000;   // NaN's bits are the largest
 #pragma unroll
-            for (int i = 0; i < kN; ++i) x[i] = finite ? fminf(fmaxf(x[i], -p.most), p.most) : 0.f;
-            uint32_t code[kWords<Bits>];
-            encode<Bits>(x, mx_scale(finite ? byte : 127), code);
+                for (int i = 0; i < kN; ++i) x[i] = finite ? fminf(fmaxf(x[i], -p.most), p.most) : 0.f;
+                encode<Bits>(x, mx_scale(byte), code);   // zeros whatever the scale
+                byte = finite ? byte : TAPS_MX_NAN;
+            } else {
+                encode<Bits>(x, mx_scale(byte), code);
+            }
             if (held) {
                 if constexpr (Bits == 4)
                     *(uint32_t *)codes = code[0];

@@ -91,6 +91,7 @@ taps_status taps_mx_append(const taps_append_args *a, uint32_t bits, const void 
     p.table = a->table;
     p.tokens = h->tokens, p.heads = h->kv_heads;
     p.dim = h->head_dim, p.rotary = a->rotary_dim;
+    p.inverse_dim = 1.0 / h->head_dim;
     p.page_log2 = h->page_log2;
     p.eps = a->eps, p.most = most_of(a->dtype, bits);
     p.interleaved = a->interleaved != 0;

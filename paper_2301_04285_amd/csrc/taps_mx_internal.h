@@ -19,6 +19,7 @@ struct taps_mx_append_launch {
     const taps_plan_token *plan_tokens;
     uint32_t tokens, heads, dim, rotary, page_log2;
     uint32_t across;   // set by the launch
+    double inverse_dim;
     float eps, most;   // most: magnitudes above it are taken for it
     uint8_t interleaved, float_weight;
 };
