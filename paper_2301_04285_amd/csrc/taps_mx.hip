@@ -44,12 +44,15 @@ template <class T> struct Raw {
     v8 x = {};
 };
 
-// Elements d .. d + 7 of a row of `dim`; zeros beyond it.
+// Elements d .. d + 7 of a row of `dim`; zeros beyond it.  Rows are read once and not kept in the L2
+// caches, whose lines the codes, written in parts of one, need: 8 prompts of 2048 appended and read
+// back 126 us, 137 where they are kept (codes that are read back are, attention will read them: 129
+// and 132 for 64 caches).
 template <class T, bool Vectors>
 __device__ __forceinline__ Raw<T> fetch(const T *row, int d, int dim) {
     Raw<T> r;
     if (Vectors) {
-        if (d < dim) r.x = *(const typename Raw<T>::v8 *)(row + d);
+        if (d < dim) r.x = __builtin_nontemporal_load((const typename Raw<T>::v8 *)(row + d));
     } else {
 #pragma unroll
         for (int i = 0; i < kN; ++i)
