@@ -362,13 +362,15 @@ template <> struct SmallMfma<_Float16> {
 };
 
 // LDS image of 32 values: rows of 16-byte chunks, permuted by a mask of the key's number.  16 lanes
-// write a chunk of each block of four keys (heads of up to 64: eight), 32 read two chunks of eight
-// keys: the mask's lowest two bits differ among the first, the others among the second.
-template <int D> struct Values {
+// write every fourth chunk of four keys (4 bits) or every second one of two (8 bits; heads of up to 64,
+// whose rows are half as long: of twice as many keys), 32 read two chunks of eight keys: the mask's lowest
+// two bits, or the lowest one, differ among the first, the others among the second.
+template <int D, int Bits> struct Values {
     static constexpr int kRow = D <= 64 ? 128 : 256, kBytes = kNarrowKeys * kRow;
     static __device__ __forceinline__ int mask(int key) {
-        if (D <= 64) return (key & 2) + 5 * ((key >> 2) & 1);
-        return 2 * (key & 1) + 5 * ((key >> 1) & 1) + 2 * (key & 4);
+        const int a = D <= 64 ? (key >> 1) & 1 : key & 1, b = D <= 64 ? (key >> 2) & 1 : (key >> 1) & 1;
+        const int far = D <= 64 ? 0 : 2 * (key & 4);
+        return (Bits == 4 ? 2 * a + 5 * b : 5 * a + 2 * b) + far;
     }
 };
 
@@ -379,55 +381,66 @@ struct False {
     static constexpr bool value = false;
 };
 
-// 16 values as they lie in memory: a block of 32 elements a lane, so that neighbouring lanes share lines.
+// 16 values as they lie in memory: 16 bytes of codes a lane and load, so that neighbouring lanes share lines.
 // They are not kept in the caches, for nothing else reads them (64 tokens over up to 4000 keys 35.3 us,
-// 39.3 with both kept, 37.0 with neither; two over 131001 54.5, 59.5, 52.3; four drafted tokens in 8 bits
-// 66.4, 66.3, 68.7, whose keys' lines take two loads).
+// 39.3 with keys and values kept, 37.0 with neither; two over 131001 54.5, 59.5, 52.3).  Blocks of 32 bytes
+// a lane, in 8 bits, take two loads with half of each line in each, and of heads of 64 leave half of the
+// lanes without: a lone token over 1024 keys 8.7 us, 9.8 so; four tokens each over up to 9999 65 to 66, 66.3.
+// (Keys, whose layout is the product's, in halves of a line a load: 73, the registers do not suffice.)
 template <class T, int D, int Bits> struct Blocks {
-    static constexpr int kN = D / 32, kBytes = 4 * Bits;   // blocks of a row; bytes of a block's codes
+    static constexpr int kN = D * Bits / 128;                // pieces of 16 bytes of a row
+    static constexpr int kLoads = (16 * kN + 63) / 64;       // of 16 values
+    static constexpr int kKeys = 16 / kLoads;                // of a load
+    static constexpr int kChunks = 16 / Bits;                // of a piece, of eight elements
     struct Raw {
-        uint32_t code[Bits], byte;
+        uint32_t code[4 * kLoads], byte[kLoads];
     };
-    int key, block;
-    bool writes, exists;    // the lane has a block of a tile, and of the head
-    uint32_t code_at, scale_at;
-    __device__ __forceinline__ Blocks(const taps_mx_attend_launch &p, int lane) {
-        key = lane / kN, block = lane % kN;
-        writes = lane < 16 * kN, exists = writes && 32 * block < (int)p.dim;
-        code_at = exists ? key * (uint32_t)p.v_slot + block * kBytes : 0;
-        scale_at = exists ? key * (uint32_t)p.vs_slot + block : 0;
+    int key, piece;
+    bool writes, exists;    // the lane has a piece of a tile, and of the head
+    uint32_t code_at, scale_at, code_slot, scale_slot;
+    __device__ __forceinline__ Blocks(const taps_mx_attend_launch &p, int lane)
+        : code_slot(p.v_slot), scale_slot(p.vs_slot) {
+        key = lane / kN, piece = lane % kN;
+        const int block = piece * kChunks / 4;
+        writes = lane < kKeys * kN, exists = writes && 32 * block < (int)p.dim;
+        code_at = exists ? key * code_slot + piece * 16 : 0;
+        scale_at = exists ? key * scale_slot + block : 0;
     }
     __device__ __forceinline__ void fetch(Raw &to, const char *codes, const char *scales) const {
 #pragma unroll
-        for (int i = 0; i < Bits; i += 4) {
-            const u32x4 w = __builtin_nontemporal_load((const u32x4 *)(codes + code_at + 4 * i));
+        for (int i = 0; i < kLoads; ++i) {
+            const u32x4 w = __builtin_nontemporal_load(
+                (const u32x4 *)(codes + kKeys * i * code_slot + code_at));
 #pragma unroll
-            for (int j = 0; j < 4; ++j) to.code[i + j] = w[j];
+            for (int j = 0; j < 4; ++j) to.code[4 * i + j] = w[j];
+            to.byte[i] = (uint8_t)(scales + kKeys * i * scale_slot)[scale_at];
         }
-        to.byte = (uint8_t)scales[scale_at];
     }
-    static __device__ __forceinline__ void clear(Raw &of) {
+    static __device__ __forceinline__ void clear(Raw &of, int load) {
 #pragma unroll
-        for (int i = 0; i < Bits; ++i) of.code[i] = 0;
-        of.byte = 127;
+        for (int i = 0; i < 4; ++i) of.code[4 * load + i] = 0;
+        of.byte[load] = 127;
     }
-    // Where the lane's chunks of eight values go: at ^ 16 j.
+    // Where the lane's chunks of eight values go: at ^ 16 j, those of another load kKeys rows further.
     __device__ __forceinline__ uint32_t place() const {
-        return key * Values<D>::kRow + 16 * ((4 * block) ^ Values<D>::mask(key));
+        return key * Values<D, Bits>::kRow + 16 * ((kChunks * piece) ^ Values<D, Bits>::mask(key));
     }
-    static __device__ __forceinline__ u32x4 eight(const Raw &of, int j, float scale) {
-        return mx_eight<T, Bits>(of.code + j * kWords<Bits>, scale);
+    static __device__ __forceinline__ u32x4 eight(const Raw &of, int load, int j, float scale) {
+        return mx_eight<T, Bits>(of.code + 4 * load + j * kWords<Bits>, scale);
     }
 };
 
 template <int D, int Waves> constexpr int few_bytes() {
-    return max_of(Waves * Values<D>::kBytes, joined_bytes<D, Waves, kFewRows>()) + 8 * Waves * kFewRows;
+    return max_of(Waves * Values<D, 4>::kBytes, joined_bytes<D, Waves, kFewRows>()) + 8 * Waves * kFewRows;
 }
 
 template <class T, int D, int Bits, int Waves>
 __device__ __forceinline__ void attend_few(const taps_mx_attend_launch &p, const taps_plan_item &item,
                                            uint32_t head, char *lds) {
     constexpr int kSteps = D / 32, kBlocks = D / 16, kStep = Waves * kNarrowKeys;
+    using Part = Piece<D, Bits>;
+    using Image = Values<D, Bits>;
+    using Lines = Blocks<T, D, Bits>;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int32_t *pages = p.pages + item.page0;
     const int lo = item.lo, hi = item.hi, start = lo & ~31;
@@ -462,11 +475,11 @@ __device__ __forceinline__ void attend_few(const taps_mx_attend_launch &p, const
 
     const Keys<T, D, Bits, false> keys(p, item, head, lane);
     const Keys<T, D, Bits, true> values(p, item, head, lane);
-    const Blocks<T, D, Bits> blocks(p, lane);
+    const Lines blocks(p, lane);
     // Two tiles are on their way at any time, each in a set of registers.
     struct Set {
-        Piece<D, Bits> k[2];
-        typename Blocks<T, D, Bits>::Raw v[2];
+        Part k[2];
+        typename Lines::Raw v[2];
         int page[2];
     } set[2];
     const bool one_page = p.page_log2 >= 5;   // tiles start at multiples of 32
@@ -486,7 +499,7 @@ __device__ __forceinline__ void attend_few(const taps_mx_attend_launch &p, const
         blocks.fetch(s.v[0], v0.codes, v0.scales);
         blocks.fetch(s.v[1], v1.codes, v1.scales);
     };
-    char *tile = lds + wave * Values<D>::kBytes;
+    char *tile = lds + wave * Image::kBytes;
     // This wavefront's tiles: those that not all rows see all of, the edges, come first, then those
     // between them, plain .. plain_end - 1.
     const int begin = start + kNarrowKeys * wave;
@@ -495,12 +508,12 @@ __device__ __forceinline__ void attend_few(const taps_mx_attend_launch &p, const
     };
     const int plain = up(seen.from), plain_end = max(seen.to - kNarrowKeys + 2, plain);
     const auto edge_from = [&](int t) { return t >= plain && t < plain_end ? up(plain_end) : t; };
-    // where a lane writes its block, and reads its columns of the first 16
+    // where a lane writes its piece, and reads its columns of the first 16
     uint32_t write_at = blocks.place();
     // lane of a group of 16: key (lane % 16) / 4 of the quarter's four, columns 4 (lane % 4) ..
     const int v_key = 4 * quarter + (lane & 15) / 4;
-    uint32_t read_at = v_key * Values<D>::kRow + 8 * (lane & 1) +
-                       16 * (((lane >> 1) & 1) ^ Values<D>::mask(v_key));
+    uint32_t read_at = v_key * Image::kRow + 8 * (lane & 1) +
+                       16 * (((lane >> 1) & 1) ^ Image::mask(v_key));
     // A tile of 32 keys; an edge: some rows do not see some of them.  Again: maxima and sums are
     // known, and an edge's rows are taken one by one, with zeros for the values that a row does not see.
     // next: the tile that the set of registers is for then (hi: none), after_next: the one after it
@@ -512,8 +525,9 @@ __device__ __forceinline__ void attend_few(const taps_mx_attend_launch &p, const
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
 #pragma unroll
-            for (int i = 0; i < Piece<D, Bits>::kBytes; ++i) asm volatile("" : "+v"(s.k[h].byte[i]));
-            asm volatile("" : "+v"(s.v[h].byte));
+            for (int i = 0; i < Part::kBytes; ++i) asm volatile("" : "+v"(s.k[h].byte[i]));
+#pragma unroll
+            for (int i = 0; i < Lines::kLoads; ++i) asm volatile("" : "+v"(s.v[h].byte[i]));
         }
         f32x4 x[2] = {};
 #pragma unroll
@@ -528,15 +542,19 @@ __device__ __forceinline__ void attend_few(const taps_mx_attend_launch &p, const
         }
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
-            const int key = t0 + 16 * h + blocks.key;
-            if ((kSteps == 2 && !blocks.exists) || (kEdge && (key < lo || key >= hi)))
-                blocks.clear(s.v[h]);
-            const float scale = mx_scale(s.v[h].byte);
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const u32x4 v = blocks.eight(s.v[h], j, scale);
-                if (kSteps == 4 || blocks.writes)
-                    *(u32x4 *)(tile + (write_at ^ (16 * j)) + 16 * h * Values<D>::kRow) = v;
+            for (int i = 0; i < Lines::kLoads; ++i) {
+                const int key = t0 + 16 * h + Lines::kKeys * i + blocks.key;
+                if ((kSteps == 2 && !blocks.exists) || (kEdge && (key < lo || key >= hi)))
+                    blocks.clear(s.v[h], i);
+                const float scale = mx_scale(s.v[h].byte[i]);
+#pragma unroll
+                for (int j = 0; j < Lines::kChunks; ++j) {
+                    const u32x4 v = blocks.eight(s.v[h], i, j, scale);
+                    if (Lines::kKeys * Lines::kN == 64 || blocks.writes)
+                        *(u32x4 *)(tile + (write_at ^ (16 * j)) +
+                                   (16 * h + Lines::kKeys * i) * Image::kRow) = v;
+                }
             }
             __builtin_amdgcn_sched_barrier(0);
         }
@@ -587,7 +605,7 @@ __device__ __forceinline__ void attend_few(const taps_mx_attend_launch &p, const
         const auto columns = [&](int b) {
             const char *at = tile + (read_at ^ (32 * b));
             const s16x4 u = Rows<T, D>::transposed(at);
-            const s16x4 w = Rows<T, D>::transposed(at + 16 * Values<D>::kRow);
+            const s16x4 w = Rows<T, D>::transposed(at + 16 * Image::kRow);
             return s16x8{u[0], u[1], u[2], u[3], w[0], w[1], w[2], w[3]};
         };
         if constexpr (!kAgain || !kEdge) {
