@@ -339,13 +339,12 @@ __device__ __forceinline__ void attend_narrow(const taps_mx_attend_launch &p,
 // the operand, with the queries laid out the same.  Values pass through LDS to be transposed.
 // Every wavefront has two tiles on their way, each in registers of its own.
 //
-// Bytes bound it.  Two tokens over 131001 keys, 8 heads of 128 in 4 bits: 285 MB in 54 us, 5.3 TB/s,
-// and 5 for the join; the loads alone, with the join, take 57.4 of the 59.5 us.  64 tokens over up to
-// 4000 keys: 160 MB in 33 and 5 (loads alone 38.8 of 39.4).  24 times four tokens over up to 9999 in 8
-// bits: 280 MB in 59 and 5 (loads alone 62 to 67 of 66, by whether lanes take them in the order of
-// memory; values do, keys in that order would have to pass through LDS, which cost a lone token 3 us
-// of 11).  With one tile on its way they took 64, 44.7 and 75; with 32x32x16 tiles, keys through
-// LDS and half of the lanes' scores of rows that are not there 75, 54 and 77.
+// Bytes bound it.  Two tokens over 131001 keys, 8 heads of 128 in 4 bits: 285 MB in 48 us, 5.9 TB/s,
+// and 5 for the join.  64 tokens over up to 4000 keys: 160 MB in 31 and 5.  24 times four tokens over
+// up to 9999 in 8 bits: 280 MB in 57 and 5 (keys do not come in the order of memory; in that order
+// they would have to pass through LDS, which cost a lone token 3 us of 11).  With one tile on its way
+// they took 4 to 9 us more, with 32x32x16 tiles, keys through LDS and half of the lanes' scores of rows
+// that are not there 11 to 15.
 template <class T> struct SmallMfma;
 template <> struct SmallMfma<__bf16> {
     static __device__ __forceinline__ f32x4 run(s16x8 a, s16x8 b, f32x4 c) {
@@ -704,7 +703,7 @@ __device__ __forceinline__ void attend_few(const taps_mx_attend_launch &p, const
 }
 
 // Four wavefronts an item, three items to a unit; eight where there are no more items than units
-// and a lone one's time counts (16 heads of 64, one token over 1024 keys: 9.8 us for 11.3; 64
+// and a lone one's time counts (16 heads of 64, one token over 1024 keys: 9.8 us for 11.3 when it was chosen; 64
 // tokens over up to 4000, 784 items: 48 for 39).
 constexpr uint32_t kUnits = 256;
 
