@@ -75,9 +75,10 @@ class MxPages:
     """Pages of keys or of values: codes and scales, 8-bit unsigned tensors [pages, kv_heads,
     page_size, bytes] of any strides but the last.  A slot has a byte of ``scales`` for every 32
     elements of a head, and 16 (4 bits) or 32 (8 bits) of ``codes``.  They are looked at once,
-    here: what they hold may change, their sizes and places may not."""
+    here: what they hold may change, their sizes and places may not.  Other tensors are other
+    pages, and a call with tensors that have moved since (``resize_``, ``set_``) raises."""
 
-    __slots__ = "codes", "scales", "bits", "_n", "_shape", "_device", "_at"
+    __slots__ = "_codes", "_scales", "_bits", "_n", "_shape", "_device", "_at", "_places"
 
     def __init__(self, codes: torch.Tensor, scales: torch.Tensor):
         for x, name in ((codes, "codes"), (scales, "scales")):
@@ -91,23 +92,27 @@ class MxPages:
             raise ValueError(f"codes {tuple(codes.shape)} on {codes.device} beside scales "
                              f"{tuple(scales.shape)} on {scales.device}")
         *pages, blocks = scales.shape
-        self.bits = codes.shape[3] // (4 * blocks) if blocks else 0
-        if self.bits not in (4, 8) or codes.shape[3] != 4 * self.bits * blocks:
+        self._bits = codes.shape[3] // (4 * blocks) if blocks else 0
+        if self._bits not in (4, 8) or codes.shape[3] != 4 * self._bits * blocks:
             raise ValueError(f"codes of {codes.shape[3]} bytes are not 4 or 8 bits of {blocks} "
                              f"blocks of {BLOCK} elements")
-        self.codes, self.scales = codes, scales
+        self._codes, self._scales = codes, scales
         self._n, self._shape = pages[0], (pages[1], pages[2], blocks)
         self._device = codes.get_device() if codes.is_cuda else None
-        self._at = Pages(codes.data_ptr(), codes.stride()[:3], scales.data_ptr(),
-                         scales.stride()[:3])
+        self._places = codes.data_ptr(), scales.data_ptr()
+        self._at = Pages(self._places[0], codes.stride()[:3], self._places[1], scales.stride()[:3])
+
+    codes = property(lambda self: self._codes)
+    scales = property(lambda self: self._scales)
+    bits = property(lambda self: self._bits)
 
     def __iter__(self):
-        return iter((self.codes, self.scales))
+        return iter((self._codes, self._scales))
 
     def __repr__(self):
         n, (heads, size, blocks) = self._n, self._shape
         return (f"MxPages({n} pages of {size} slots, {heads} heads of {blocks} blocks, "
-                f"{self.bits} bits)")
+                f"{self._bits} bits)")
 
 
 def _blocks(head_dim: int) -> int:
@@ -128,18 +133,20 @@ def new_pages(n_pages: int, kv_heads: int, page_size: int, head_dim: int, bits: 
 
 def _fits(pages: MxPages, what: str, device: int, n_pages: int, shape) -> Pages:
     """shape: (kv_heads, page_size, blocks)."""
+    if (pages._codes.data_ptr(), pages._scales.data_ptr()) != pages._places:
+        raise ValueError(f"the tensors of {what} have moved since it was made of them")
     if pages._n < n_pages or pages._shape != shape:
         raise ValueError(f"{what} is {pages}, not at least {n_pages} pages of {shape[1]} slots, "
                          f"{shape[0]} heads of {shape[2]} blocks")
     if pages._device != device:
-        _on_gpu(pages.codes, what, device)
+        _on_gpu(pages._codes, what, device)
     return pages._at
 
 
 def _caches(k_cache: MxPages, v_cache: MxPages, device: int, n_pages: int, shape):
     shape = shape[0], shape[1], _blocks(shape[2])
-    if k_cache.bits != v_cache.bits:
-        raise ValueError(f"keys of {k_cache.bits} bits beside values of {v_cache.bits}")
+    if k_cache._bits != v_cache._bits:
+        raise ValueError(f"keys of {k_cache._bits} bits beside values of {v_cache._bits}")
     return (_fits(k_cache, "k_cache", device, n_pages, shape),
             _fits(v_cache, "v_cache", device, n_pages, shape))
 
@@ -161,7 +168,7 @@ def taps_mx_append(k, v, k_cache: MxPages, v_cache: MxPages, plan: PagedPlan, ta
     args = AppendArgs(code, weight, rotary, 1 if interleaved else 0, eps, kw, at, rows)
     kc, vc = _caches(k_cache, v_cache, device, plan.n_pages, plan._page_shape)
     _check(load().taps_mx_append(
-        C.byref(args), k_cache.bits, *plan.pointers(stream, raw, device),
+        C.byref(args), k_cache._bits, *plan.pointers(stream, raw, device),
         _heads(k, "k", device, dtype, plan._k_shape, 3),
         _heads(v, "v", device, dtype, plan._k_shape, 3), kc, vc, raw), "taps_mx_append")
 
@@ -190,7 +197,7 @@ def taps_mx_read(k_cache: MxPages, v_cache: MxPages, slots, head_dim: int, dtype
         k, v = out
         dtype = k.dtype
         kh, vh = _heads(k, "k", device, dtype, shape, 3), _heads(v, "v", device, dtype, shape, 3)
-    args = ReadArgs(_dtype(k), k_cache.bits, shape[0], heads, head_dim, page_size, n_pages,
+    args = ReadArgs(_dtype(k), k_cache._bits, shape[0], heads, head_dim, page_size, n_pages,
                     slots.element_size(), slots.data_ptr())
     _check(load().taps_mx_read(C.byref(args), kc, vc, kh, vh, raw), "taps_mx_read")
     return k, v
@@ -219,7 +226,7 @@ def taps_mx_attend(q, k_cache: MxPages, v_cache: MxPages, plan: PagedPlan, scale
     if n:
         workspace = _on(stream, lambda: torch.empty(n, dtype=torch.uint8, device=q.device))
     _check(load().taps_mx_attend(
-        code, k_cache.bits, *plan.pointers(stream, raw, device), qh, kc, vc,
+        code, k_cache._bits, *plan.pointers(stream, raw, device), qh, kc, vc,
         plan.head_dim ** -0.5 if scale is None else scale, oh,
         None if sums is None else sums.data_ptr(),
         None if workspace is None else workspace.data_ptr(), n, raw), "taps_mx_attend")

@@ -166,6 +166,41 @@ def test_pages_refusals():
             mx.MxPages(c, s)
 
 
+def test_pages_stay_with_their_tensors():
+    """What was looked at once is what later calls write to: neither tensor can be put in the
+    place of another, and calls refuse pages whose tensors have moved."""
+    c = mx.new_pages(3, 2, 16, 128, 4, device="cpu")
+    for name in ("codes", "scales", "bits"):
+        x = getattr(c, name)
+        with pytest.raises(AttributeError):
+            setattr(c, name, x if name == "bits" else x.clone())
+        assert getattr(c, name) is x
+    fits = None, 3, (2, 16, 4)   # a device that is that of CPU tensors
+    c.codes.fill_(3)
+    c.scales[1] = 9
+    assert mx._fits(c, "k_cache", *fits) is c._at and c._at.codes == c.codes.data_ptr()
+
+    def grown(x):
+        x.resize_(9, *x.shape[1:])
+
+    def replaced(x):
+        x.set_(torch.zeros_like(x))
+
+    def given_data(x):
+        x.data = torch.zeros_like(x)
+
+    def freed(x):
+        x.untyped_storage().resize_(0)
+    for move in (grown, replaced, given_data, freed):
+        for name in ("codes", "scales"):
+            c = mx.new_pages(3, 2, 16, 128, 4, device="cpu")
+            held = c.codes.clone(), c.scales.clone()   # so that a new place is another one
+            move(getattr(c, name))
+            with pytest.raises(ValueError, match="k_cache have moved"):
+                mx._fits(c, "k_cache", *fits)
+            del held
+
+
 @pytest.mark.parametrize("bits", [4, 8])
 def test_reference_codes(bits):
     """Every number that a code stands for is held as it is; others move to a neighbour that no
