@@ -13,7 +13,8 @@ the library is missing the calls raise -- there is no other implementation to
 fall back to.  Outputs and workspaces come from torch's allocator, on the
 stream that the call runs on (``stream``, or the current one).  Torch's autograd
 follows ``norm_rotate`` alone: a backward pass through the new outputs of another
-call raises, and what a call writes to tensors it is given has no history.
+call raises, as do such calls on inputs with tangents (forward mode); what a call
+writes to tensors it is given has no history.
 """
 from __future__ import annotations
 
@@ -24,6 +25,7 @@ from typing import List
 
 import numpy as np
 import torch
+from torch.autograd import forward_ad
 
 from . import taps
 from .taps import TapsError, _stream   # noqa: F401
@@ -228,7 +230,12 @@ class _NoGradient(torch.autograd.Function):
 
 def _no_gradient(said: str, outputs, inputs):
     """``outputs``, which raise in a backward pass if one of the inputs asks for it: left without
-    a history they would pass for constants there."""
+    a history they would pass for constants there.  Raises if an input has a tangent, which has
+    no later pass that could."""
+    if forward_ad._current_level >= 0:   # unpack_dual asks too, in a third of a microsecond each
+        for t in inputs:
+            if t is not None and forward_ad.unpack_dual(t).tangent is not None:
+                raise RuntimeError(said)
     if torch.is_grad_enabled():
         for t in inputs:
             if t is not None and t.requires_grad:

@@ -10,7 +10,8 @@ held in microscaling formats of 4 or 8 bits, beside the 16-bit cache of ``attent
 Argument marshalling only, as in ``attention``: every step runs in
 ``libtaps_attention.so``, which raises if it is missing; outputs and workspaces come from
 torch's allocator, on the stream that the call runs on.  A cache has no
-gradients: a backward pass through the new outputs of ``taps_mx_attend`` raises.
+gradients: a backward pass through the new outputs of ``taps_mx_attend`` raises, as does
+the call on queries with tangents (forward mode).
 """
 from __future__ import annotations
 

@@ -7,6 +7,8 @@ import subprocess
 
 import numpy as np
 import pytest
+import torch
+from torch.autograd import forward_ad
 
 from paper_2301_04285_amd import attention as A, build_attention, taps
 from paper_2301_04285_amd.taps import TapsError
@@ -327,3 +329,18 @@ def test_plan_capacity():
     assert L.taps_paged_plan(C.byref(b), 0, None, None, C.byref(work)) == taps.ERR_ARG
     b.q_lens = None
     assert L.taps_paged_plan(C.byref(b), 0, None, C.byref(size), C.byref(work)) == taps.ERR_ARG
+
+
+def test_tangents_raise():
+    """Forward mode: outputs without a history would pass for constants."""
+    x, w = torch.ones(4), torch.ones(4)
+    outputs = torch.zeros(4), None
+    assert A._no_gradient("no gradient", outputs, (x, None, w)) is outputs
+    with forward_ad.dual_level():
+        assert A._no_gradient("no gradient", outputs, (x, None, w)) is outputs
+        for inputs in ((forward_ad.make_dual(x, w), None), (x, None, forward_ad.make_dual(w, x))):
+            with pytest.raises(RuntimeError, match="no gradient"):
+                A._no_gradient("no gradient", outputs, inputs)
+            with torch.no_grad(), pytest.raises(RuntimeError, match="no gradient"):
+                A._no_gradient("no gradient", outputs, inputs)
+    assert A._no_gradient("no gradient", outputs, (x, None, w)) is outputs

@@ -582,6 +582,31 @@ def test_gradients_raise():
         assert not mx.taps_mx_attend(q, *caches, plan).requires_grad
 
 
+def test_tangents_raise():
+    """Forward mode, over either cache: queries, weights and a cache with tangents."""
+    qkv, w, table, positions, caches, plan, _ = _step(4)
+    q = qkv[:, :8].contiguous()
+    half = [torch.zeros(caches[0].codes.shape[0], 2, 16, 64, dtype=BF16, device="cuda")
+            for _ in range(2)]
+
+    def norm(q, w):
+        return A.taps_norm_rotate(q, None, w, None, table, positions=positions)
+
+    def attend(q, k):
+        return A.taps_attend(q, k, half[1], plan)
+
+    def mx_attend(q):
+        return mx.taps_mx_attend(q, *caches, plan)
+    for call, args in ((norm, (q, w)), (attend, (q, half[0])), (mx_attend, (q,))):
+        with torch.autograd.forward_ad.dual_level():
+            call(*args)
+            for i, x in enumerate(args):
+                dual = torch.autograd.forward_ad.make_dual(x, torch.ones_like(x))
+                with pytest.raises(RuntimeError, match="has no gradient"):
+                    call(*args[:i], dual, *args[i + 1:])
+        call(*args)
+
+
 def test_gpu_refusals():
     q = torch.zeros(4, 8, 64, dtype=BF16, device="cuda")
     c = mx.new_pages(2, 8, 16, 64, 4)
