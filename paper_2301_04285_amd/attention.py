@@ -359,7 +359,8 @@ def taps_norm_rotate_backward(dq_out, dk_out, q, k, q_weight, k_weight, table, p
         None if dqw is None else dqw.data_ptr(), None if dkw is None else dkw.data_ptr(),
         workspace.data_ptr(), C.byref(C.c_uint64(size)), _stream(stream)),
         "taps_norm_rotate_backward")
-    return dq, dk, dqw, dkw
+    return _no_gradient("taps_norm_rotate_backward has no gradient", (dq, dk, dqw, dkw),
+                        (dq_out, dk_out, q, k, q_weight, k_weight))
 
 
 _function = None

@@ -242,6 +242,26 @@ def test_gradients_of_gradients_raise():
     assert torch.equal(first, same) and not same.requires_grad
 
 
+def test_the_backward_call_without_a_gradient_says_so():
+    g = gen_of(43)
+    args = [randn(g, 5, 2, 64) for _ in range(4)] + [randn(g, 64) for _ in range(2)]
+    table = A.rotation_table(5, 64)
+    want = A.taps_norm_rotate_backward(*args, table)
+    assert not any(t.requires_grad for t in want)
+    for which in range(6):
+        mine = [x.clone() for x in args]
+        mine[which].requires_grad_()
+        for t, x in zip(A.taps_norm_rotate_backward(*mine, table), want):
+            assert torch.equal(t, x)
+            with pytest.raises(RuntimeError, match="taps_norm_rotate_backward has no gradient"):
+                t.sum().backward()
+        with torch.no_grad():
+            assert not any(t.requires_grad for t in A.taps_norm_rotate_backward(*mine, table))
+    dq, _, _, dkw = A.taps_norm_rotate_backward(args[0].requires_grad_(), None, args[2], None,
+                                                args[4], None, table)
+    assert dq.requires_grad and dkw is None
+
+
 def test_calls_without_a_gradient_say_so():
     g = gen_of(42)
     q, k = (randn(g, 5, 2, 64) for _ in range(2))
