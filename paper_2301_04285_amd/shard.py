@@ -19,6 +19,9 @@ import numpy as np
 __all__ = ["Share", "share_of", "run"]
 
 PAGE = 64
+# Elements of keys that are made, or read back, at once: a share whose cache fits the device only
+# in a microscaling format has no room for all of them in 16 or 32 bits.
+PIECE = 1 << 28
 
 
 @dataclass(frozen=True)
@@ -57,6 +60,12 @@ def _slots(share: Share):
         share.batch * per_seq
 
 
+def _pieces(share: Share, n_keys: int):
+    """Key positions 0 .. n_keys - 1 of all sequences, PIECE elements at a time: (first, end)."""
+    step = max(1, PIECE // (share.batch * share.heads * share.dim))
+    return [(a, min(a + step, n_keys)) for a in range(0, n_keys, step)]
+
+
 def run(share: Share, dtype, repeats: int = 10, seed: int = 0, cache_bits: int = 16):
     """Runs the share on random projections; {step: seconds} and the largest difference
     of a few rows from 64-bit attention over the same cache, relative to it."""
@@ -82,15 +91,15 @@ def run(share: Share, dtype, repeats: int = 10, seed: int = 0, cache_bits: int =
     q, k, v = randn(b * new, 3 * n, dim).split(n, dim=1)   # as one projection leaves them
     if cache_bits < 16:
         caches = [mx.new_pages(n_pages, n, PAGE, dim, cache_bits) for _ in range(2)]
-        slots = torch.from_numpy(pages).cuda().long()[:, torch.arange(keys).cuda() // PAGE] * PAGE + \
-            torch.arange(keys).cuda() % PAGE
+        at = torch.arange(keys, device="cuda")
+        slots = torch.from_numpy(pages).cuda().long()[:, at // PAGE] * PAGE + at % PAGE
     else:
         caches = [torch.zeros((n_pages, n, PAGE, dim), dtype=dtype, device="cuda")
                   for _ in range(2)]
-    if old:   # the earlier chunks' keys, which other devices projected
-        before = attention.PagedPlan([old] * b, [old] * b, pages, **shape)
-        append_to(randn(b * old, n, dim), randn(b * old, n, dim), *caches, before, table=table,
-                  k_weight=k_weight)
+    for first, end in _pieces(share, old):   # earlier chunks' keys, which other devices projected
+        before = attention.PagedPlan([end - first] * b, [end] * b, pages, **shape)
+        append_to(*(randn(b * (end - first), n, dim) for _ in range(2)), *caches, before,
+                  table=table, k_weight=k_weight)
     plan = attention.PagedPlan([new] * b, [keys] * b, pages, **shape)
     chunk = q.unflatten(0, (b, new))
     state = {}
@@ -108,8 +117,22 @@ def run(share: Share, dtype, repeats: int = 10, seed: int = 0, cache_bits: int =
     def attend():
         state["out"] = attend_over(state["q"].flatten(0, 1), *caches, plan)
 
-    def read():
-        state["kv"] = mx.taps_mx_read(*caches, slots.flatten(), dim, dtype)
+    if cache_bits < 16:
+        parts = [slots[:, first:end].flatten() for first, end in _pieces(share, keys)]
+        kv = [torch.empty((len(parts[0]), n, dim), dtype=dtype, device="cuda") for _ in range(2)]
+
+    def read():   # every piece to the same place, from where it would be sent
+        for part in parts:
+            mx.taps_mx_read(*caches, part, dim, out=[x[:len(part)] for x in kv])
+
+    def kept(s, h, seen):
+        """The first keys and values of a sequence and head, as the cache has them."""
+        if cache_bits < 16:
+            some = [[x[:, h].contiguous() for x in mx.taps_mx_read(
+                *caches, slots[s, first:end].contiguous(), dim, dtype)]
+                for first, end in _pieces(share, seen)]
+            return [torch.cat(side) for side in zip(*some)]
+        return [c[torch.from_numpy(pages[s]).long(), h].flatten(0, 1)[:seen] for c in caches]
     seconds = {}
     for step in (norm_rotate, gradients, append, attend, *((read,) if cache_bits < 16 else ())):
         step()
@@ -120,21 +143,17 @@ def run(share: Share, dtype, repeats: int = 10, seed: int = 0, cache_bits: int =
         end.record()
         end.synchronize()
         seconds[step.__name__] = start.elapsed_time(end) * 1e-3 / repeats
-    if cache_bits < 16:
-        kept = [x.unflatten(0, (b, keys)).transpose(1, 2) for x in state["kv"]]
-    else:
-        kept = [c[torch.from_numpy(pages).long()].transpose(1, 2).flatten(2, 3) for c in caches]
     return seconds, _difference(share, state, kept)
 
 
 def _difference(share: Share, state, kept) -> float:
-    """kept: keys and values [sequences, heads, keys and more, dim]."""
+    """kept(sequence, head, n): its first n keys and values [n, dim]."""
     worst = 0.0
     rng = np.random.default_rng(1)
     for _ in range(4):
         s, t, h = (int(rng.integers(x)) for x in (share.batch, share.tokens, share.heads))
         seen = share.keys - share.tokens + t + 1
-        k, v = (c[s, h, :seen].double().cpu().numpy() for c in kept)
+        k, v = (x.cpu().double().numpy() for x in kept(s, h, seen))
         q = state["q"][s, t, h].double().cpu().numpy()
         p = k @ q * share.dim ** -0.5
         p = np.exp(p - p.max())
