@@ -94,7 +94,7 @@ struct Place {
 
 // What redo reads of a cache in 16 bits.
 struct HalfCache {
-    typedef Place At;
+    typedef const char *Key, *Value;
     const taps_attend_launch &p;
     const uint32_t head;
     __device__ __forceinline__ HalfCache(const taps_attend_launch &launch, uint32_t h)
@@ -103,15 +103,14 @@ struct HalfCache {
         return Place(p, p.k_cache + (int64_t)head * p.k_head, p.v_cache + (int64_t)head * p.v_head, page,
                      key);
     }
-    __device__ __forceinline__ const char *row(const Place &a, const Place &b, bool second,
-                                               uint32_t slot) const {
-        return (second ? b.k : a.k) + slot * (uint32_t)p.k_slot;
+    __device__ __forceinline__ const char *row(const char *k, uint32_t slot) const {
+        return k + slot * (uint32_t)p.k_slot;
     }
     __device__ __forceinline__ s16x8 keys(const char *row, int d) const {
         return *(const s16x8 *)(row + 2 * d);
     }
-    __device__ __forceinline__ short value(const Place &at, uint32_t slot, uint32_t stride, int d) const {
-        return *(const short *)(at.v + slot * stride + 2 * d);
+    __device__ __forceinline__ short value(const char *v, uint32_t slot, uint32_t stride, int d) const {
+        return *(const short *)(v + slot * stride + 2 * d);
     }
 };
 

@@ -401,8 +401,10 @@ struct Seen {
 // rows are done again: 249 us, 39 without; a row and a key at a time took 9.9 ms.)
 // Behind the kernels' other code: between it, it cost a lone token 0.7 us.
 // `cache` reads the keys and values of one key head: at() is where a group of 16 keys
-// that share a page lies, keys() eight elements of a slot's key from column d on, value()
-// one element of its value, in the type T.
+// that share a page lies, row() a slot's key, keys() eight of its elements from column d
+// on, value() one element of a slot's value, in the type T.  (Both places of a group in one
+// object, row() choosing between two: the 16-bit kernels' registers and spilled scalars fell
+// otherwise, and a mixed step of 12 heads of 96 took 24.9 us, 24.6 so.)
 template <class T, int D, class Cache>
 __device__ __forceinline__ void redo(const taps_attend_launch &p, const taps_plan_item &item,
                                      const Cache &cache, Rows<T, D> &rows, uint32_t again,
@@ -415,12 +417,14 @@ __device__ __forceinline__ void redo(const taps_attend_launch &p, const taps_pla
     for (int b = 0; b < kBlocks; ++b) rows.o[b] = f32x16{};
     for (; lo < hi && t0 < hi; t0 += step) {
         // two groups of 16 keys; of one that lies outside, and of keys outside, the nearest inside
-        typename Cache::At place[2];
+        typename Cache::Key k_at[2];
+        typename Cache::Value v_at[2];
         int key0[2];
 #pragma unroll
         for (int n = 0; n < 2; ++n) {
             key0[n] = min(max(t0 + 16 * n, lo & ~15), (hi - 1) & ~15);
-            place[n] = cache.at(page_at(p, p.pages + item.page0, key0[n], lo, hi), key0[n]);
+            const auto at = cache.at(page_at(p, p.pages + item.page0, key0[n], lo, hi), key0[n]);
+            k_at[n] = at.k, v_at[n] = at.v;
         }
         const auto in = [&](int key) { return key >= lo && key < hi; };
         const auto slot_of = [&](int key, int n) {
@@ -431,8 +435,7 @@ __device__ __forceinline__ void redo(const taps_attend_launch &p, const taps_pla
         x.s[0] = f32x16{};
         {
             const int key = t0 + (lane & 31), n = (lane >> 4) & 1;
-            const auto row = cache.row(place[0], place[1], n,
-                                       n ? slot_of(key, 1) : slot_of(key, 0));
+            const auto row = cache.row(n ? k_at[1] : k_at[0], n ? slot_of(key, 1) : slot_of(key, 0));
 #pragma unroll
             for (int k = 0; k < kSteps; ++k) {
                 const int d = 16 * k + 8 * half;
@@ -457,7 +460,7 @@ __device__ __forceinline__ void redo(const taps_attend_launch &p, const taps_pla
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
                     const int key = t0 + 16 * n + 8 * (e / 4) + 4 * half + e % 4;
-                    const short u = cache.value(place[n], slot_of(key, n), stride, d < dim ? d : 0);
+                    const short u = cache.value(v_at[n], slot_of(key, n), stride, d < dim ? d : 0);
                     v[n][e] = in(key) && d < dim ? u : (short)0;
                     if (e % 4 == 3) __builtin_amdgcn_sched_barrier(0);
                 }

@@ -58,11 +58,13 @@ template <int D, int Bits> struct Piece {
 
 // What redo reads of the cache, and where groups of 16 keys lie.
 template <class T, int Bits> struct MxCache {
-    struct At {
-        const char *k, *v, *ks, *vs;
-    };
-    struct Row {
+    struct Key {
         const char *codes, *scales;
+    };
+    typedef Key Value;
+    struct At {
+        Key k;
+        Value v;
     };
     const taps_mx_attend_launch &p;
     const char *k, *v, *ks, *vs;   // of the key head
@@ -71,24 +73,23 @@ template <class T, int Bits> struct MxCache {
           ks(p.k_scales + (int64_t)head * p.ks_head), vs(p.v_scales + (int64_t)head * p.vs_head) {}
     __device__ __forceinline__ At at(int page, int key) const {
         const int64_t slot = key & ((1 << p.page_log2) - 1);
-        return {k + page * p.k_page + slot * p.k_slot, v + page * p.v_page + slot * p.v_slot,
-                ks + page * p.ks_page + slot * p.ks_slot, vs + page * p.vs_page + slot * p.vs_slot};
+        return {{k + page * p.k_page + slot * p.k_slot, ks + page * p.ks_page + slot * p.ks_slot},
+                {v + page * p.v_page + slot * p.v_slot, vs + page * p.vs_page + slot * p.vs_slot}};
     }
-    __device__ __forceinline__ Row row(const At &a, const At &b, bool second, uint32_t slot) const {
-        return {(second ? b.k : a.k) + slot * (uint32_t)p.k_slot,
-                (second ? b.ks : a.ks) + slot * (uint32_t)p.ks_slot};
+    __device__ __forceinline__ Key row(const Key &a, uint32_t slot) const {
+        return {a.codes + slot * (uint32_t)p.k_slot, a.scales + slot * (uint32_t)p.ks_slot};
     }
-    __device__ __forceinline__ s16x8 keys(const Row &row, int d) const {
+    __device__ __forceinline__ s16x8 keys(const Key &row, int d) const {
         uint32_t code[kWords<Bits>];
 #pragma unroll
         for (int i = 0; i < kWords<Bits>; ++i) code[i] = ((const uint32_t *)(row.codes + d / 8 * Bits))[i];
         return __builtin_bit_cast(
             s16x8, mx_eight<T, Bits>(code, mx_scale((uint8_t)row.scales[d / 32])));
     }
-    __device__ __forceinline__ short value(const At &at, uint32_t slot, uint32_t stride, int d) const {
-        const uint8_t byte = at.v[slot * stride + d * Bits / 8];
+    __device__ __forceinline__ short value(const Value &at, uint32_t slot, uint32_t stride, int d) const {
+        const uint8_t byte = at.codes[slot * stride + d * Bits / 8];
         const uint32_t code = Bits == 4 && d % 2 ? byte >> 4 : byte;
-        const uint8_t scale = at.vs[slot * (uint32_t)p.vs_slot + d / 32];
+        const uint8_t scale = at.scales[slot * (uint32_t)p.vs_slot + d / 32];
         return (short)mx_pair<T, Bits, 0>(code, mx_scale(scale));
     }
 };
