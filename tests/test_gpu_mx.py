@@ -433,6 +433,94 @@ def test_attend_blocks_of_nan(spec, dtype, bits):
     assert want_bad and (clean or kv_heads == 1)
 
 
+NOT_FINITE = [
+    ([4, 30], [4, 200], 4, 2, 128, 16, {}),                  # few rows, several tokens
+    ([4, 2], [300, 77], 2, 1, 64, 16, {"window": 20}),
+    ([9], [1500], 8, 2, 96, 64, {"units": 4096}),            # 17 to 32 rows, in pieces
+    ([140], [500], 2, 1, 96, 32, {"window": 65}),
+    ([300], [330], 4, 2, 128, 64, {"units": 1}),
+    ([40], [1500], 8, 2, 128, 64, {"units": 4096}),
+    ([300], [1700], 4, 2, 128, 64, {"units": 1}),            # 256 rows an item
+    # more items than units
+    ([40] * 12 + [10] * 12 + [3] * 12, [60] * 12 + [150, 11, 32, 31] * 6, 16, 8, 64, 16, {}),
+    ([3] * 40, [60, 70, 150, 11, 32] * 8, 8, 8, 64, 16, {"window": 25}),
+]
+
+
+def not_finite_check(spec, q, kept, out, lse, dtype):
+    """The outputs and sums that are not finite are those that cannot be, the others near."""
+    q_lens, kv_lens, q_heads, kv_heads, dim, page, options = spec
+    bad, total = np.zeros(2, dtype=int), np.zeros(2, dtype=int)
+    at = 0
+    for s, (n, m) in enumerate(zip(q_lens, kv_lens)):
+        with np.errstate(invalid="ignore"):
+            *of_out, w_lse, b_lse = R.attend(R.f64(q[at:at + n]), *kept[s], m - n, 0, True,
+                                             options.get("window", 0), dim ** -0.5, dtype)
+        for i, (x, want, bound) in enumerate(((out, *of_out), (lse, w_lse, b_lse))):
+            got, off = R.f64(x[at:at + n]), ~np.isfinite(want)
+            assert np.array_equal(off, ~np.isfinite(got)), "not the same ones are finite"
+            assert np.array_equal(got[np.isinf(want)], want[np.isinf(want)])
+            # a bound of infinity (scores of -inf) times 0 is that of a sum of zeros: 0
+            bound = np.where(np.isnan(bound), 0, bound)
+            R.check(np.where(off, 0, got), np.where(off, 0, want), np.where(off, 1, bound),
+                    ("out", "lse")[i])
+            bad[i], total[i] = bad[i] + off.sum(), total[i] + off.size
+        at += n
+    return bad, total
+
+
+@pytest.mark.parametrize("bits", [4, 8])
+@pytest.mark.parametrize("dtype", [BF16, F16])
+@pytest.mark.parametrize("spec", NOT_FINITE)
+def test_attend_lse_beside_blocks_of_nan(spec, dtype, bits):
+    """A row's sum of exponentials has nothing to do with the values, and is NaN where a key is."""
+    q_lens, kv_lens, q_heads, kv_heads, dim, page, options = spec
+    say(f"[gpu] mx attend nan lse {spec} {dtype} {bits}")
+    for which in (1, 0):
+        q, caches, plan, kept, pages = attend_case(spec, dtype, bits)
+        rng = random.Random(7)
+        for s, (n, m) in enumerate(zip(q_lens, kv_lens)):
+            j = m - 1 - rng.randrange(min(m, n + 16))   # a new token, or one just before them
+            h, b = rng.randrange(kv_heads), rng.randrange(-(-dim // 32))
+            caches[which].scales[pages[s, j // page], h, j % page, b] = 255
+            kept[s][which][j, h, 32 * b:32 * b + 32] = math.nan
+        out, lse = mx.taps_mx_attend(q, *caches, plan, lse=True)
+        bad, total = not_finite_check(spec, q, kept, out, lse, dtype)
+        assert 0 < bad[0] and (bad[0] < total[0] or kv_heads == 1)
+        assert bad[1] == 0 if which else dim * bad[1] == bad[0]
+
+
+@pytest.mark.parametrize("bits", [4, 8])
+@pytest.mark.parametrize("spec", NOT_FINITE)
+def test_attend_beyond_the_range_of_fp16(spec, bits):
+    """Blocks of values, and single elements of keys, that are infinite in fp16: they reach the
+    tokens that see them and no others."""
+    q_lens, kv_lens, q_heads, kv_heads, dim, page, options = spec
+    say(f"[gpu] mx attend infinities {spec} {bits}")
+    q, caches, plan, kept, pages = attend_case(spec, F16, bits)
+    rng = random.Random(9)
+    for s, (n, m) in enumerate(zip(q_lens, kv_lens)):
+        for which in (1, 1, 0):
+            j = m - 1 - rng.randrange(min(m, n + 16))
+            h, b = rng.randrange(kv_heads), rng.randrange(dim // 32)
+            place = pages[s, j // page], h, j % page
+            codes = caches[which].codes[place][4 * bits * b:4 * bits * (b + 1)]
+            if which:   # 2^40 times what they stood for, 2^-17 or more
+                caches[which].scales[place][b] += 40
+                x = kept[s][1][j, h, 32 * b:32 * b + 32]
+                kept[s][1][j, h, 32 * b:32 * b + 32] = np.where(
+                    x == 0, 0, np.copysign(math.inf, x))
+            else:       # one element, 2^0 x 2^30, among zeros
+                codes.zero_()
+                codes[0] = 2 if bits == 4 else 0x38
+                caches[which].scales[place][b] = 157
+                kept[s][0][j, h, 32 * b:32 * b + 32] = [math.inf] + [0] * 31
+    # (scores of a row lie within a few units of each other: no numerator rounds to nothing)
+    out, lse = mx.taps_mx_attend(q, *caches, plan, lse=True)
+    bad, total = not_finite_check(spec, q, kept, out, lse, F16)
+    assert 0 < bad[0] and (bad[0] < total[0] or kv_heads == 1)
+
+
 @pytest.mark.parametrize("dim", [64, 96, 128])
 def test_tokens_without_keys(dim):
     """Sequences that have lost all their keys: zeros, whatever earlier workgroups left in LDS."""
@@ -472,6 +560,50 @@ def test_attend_far_offsets():
         for got, x in zip(mx.taps_mx_read(*caches, slots.to(kind), 128), (k, v)):
             codes, scales = M.encode(R.f64(x[[0, 40]]), 4, BF16)
             assert np.array_equal(R.f64(got), M.decode(codes, scales, 128))
+
+
+@pytest.mark.parametrize("bits,spec", [
+    (4, ([3, 10, 40, 1], [300, 200, 90, 17], 4, 2, 128, 16, {})),
+    (8, ([3, 10, 40, 1], [300, 200, 90, 17], 4, 2, 64, 32, {"window": 150})),
+    (8, ([300], [1700], 4, 2, 96, 16, {"units": 1})),        # 256 rows an item
+])
+def test_slots_far_apart(bits, spec):
+    """Slots as far apart as they may be, pages and heads between them; both kinds of strides odd
+    in all but what is asked for."""
+    q_lens, kv_lens, q_heads, kv_heads, dim, page, options = spec
+    say(f"[gpu] mx far slots {bits} {spec}")
+    q, caches, plan, _, pages = attend_case(spec, BF16, bits)
+    far = []
+    for c in caches:
+        apart = [2 ** 27 - 16, 2 ** 27 - 1]
+        far.append(mx.MxPages(*(torch.empty_strided(
+            t.shape, (kv_heads * size, size, slot, 1), dtype=torch.uint8, device="cuda").copy_(t)
+            for t, slot, size in zip(c, apart, (c.codes.shape[3] + 16, c.scales.shape[3] + 3)))))
+    want, want_lse = mx.taps_mx_attend(q, *caches, plan, lse=True)
+    got, lse = mx.taps_mx_attend(q, *far, plan, lse=True)
+    assert torch.equal(got, want) and torch.equal(lse, want_lse)
+    k, v = (randn(gen_of(5), sum(q_lens), kv_heads, dim) for _ in range(2))
+    every = torch.arange(caches[0].codes.shape[0] * page, device="cuda")
+    for c in (caches, far):
+        mx.taps_mx_append(k, v, *c, plan, table=A.rotation_table(max(kv_lens), dim))
+    for a, b in zip(caches, far):
+        assert all(torch.equal(x, y) for x, y in zip(a, b))
+    for a, b in zip(*(mx.taps_mx_read(*c, every, dim) for c in (caches, far))):
+        assert torch.equal(a.view(torch.int16), b.view(torch.int16))   # NaN where nothing is
+    del far
+    torch.cuda.empty_cache()
+
+
+def test_pages_that_sequences_share():
+    """Two sequences whose first pages are the same ones, only read."""
+    spec = ([1, 3], [200, 180], 8, 2, 128, 16, {})
+    q, caches, _, kept, pages = attend_case(spec, BF16, 4)
+    pages[1, :5] = pages[0, :5]
+    kept[1] = tuple(np.concatenate([a[:80], b[80:]]) for a, b in zip(*kept))
+    plan = A.PagedPlan(*spec[:2], pages, n_pages=caches[0].codes.shape[0], page_size=16, q_heads=8,
+                       kv_heads=2, head_dim=128)
+    out, lse = mx.taps_mx_attend(q, *caches, plan, lse=True)
+    attend_check(spec, q, kept, out, lse, 128 ** -0.5, BF16)
 
 
 # ---------------------------------------------------------------------------
@@ -555,6 +687,31 @@ def test_step_in_a_graph(bits):
         want = _run_step(*step)
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(got, want))
+
+
+@pytest.mark.parametrize("spec", [
+    ([1, 4], [9000, 700], 8, 2, 128, 64, {"units": 256}),        # few rows
+    ([10, 40], [9000, 700], 8, 2, 64, 16, {"units": 4096}),
+    ([300], [2900], 4, 2, 128, 64, {"units": 64}),               # 256 rows an item
+])
+def test_pieces_in_a_graph(spec):
+    """Attention whose keys are split, its workspace the graph's, between eager work."""
+    say(f"[gpu] mx pieces in a graph {spec}")
+    q, caches, plan, _, _ = attend_case(spec, BF16, 8)
+    assert plan.workspace_bytes
+    want = mx.taps_mx_attend(q, *caches, plan, lse=True)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = mx.taps_mx_attend(q, *caches, plan, lse=True)
+    g = gen_of(31)
+    for _ in range(4):
+        graph.replay()
+        torch.full((1 << 22,), math.nan, device="cuda")
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(out, want))
+        q.copy_(randn(g, *q.shape, scale=1.5))
+        want = mx.taps_mx_attend(q, *caches, plan, lse=True)
 
 
 def test_step_on_another_stream():
