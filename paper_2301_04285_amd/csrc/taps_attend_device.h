@@ -16,7 +16,7 @@ constexpr float kNoScore = -3.402823466e38f;
 // fp16 has its smallest normal number at 2^-14 and nothing below 2^-25, so there
 // the maximum's is placed at 2^10: keys that far below it still count, where many of
 // them together outweigh it.  bf16 has the exponents of 32 bits.
-// A row's maximum is raised only when a tile's numerators (this lane's 16 or 32)
+// A row's maximum is raised only when a tile's numerators (this lane's 8, 16 or 32)
 // add up to more than kMostSum: none exceeds it, inside the type's range, equal
 // ones do not reach it, and most tiles neither look for their maximum nor touch
 // the accumulators.

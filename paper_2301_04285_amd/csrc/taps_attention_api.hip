@@ -77,6 +77,8 @@ struct Layout {
     taps_plan_header head{};
 };
 
+// Times of plans, here and below, are over the 16-bit cache; one in microscaling formats takes
+// the same plans.
 // Shorter pieces are not made: a split costs a launch and a pass over partial
 // results, some 5 us for few rows, in which a narrow item takes about this many
 // keys (one token over 1024 keys of 16 heads: 11.3 us whole, 13.7 in four) and a

@@ -15,10 +15,13 @@
 // so that a wavefront's groups read and write neighbouring slots of a head at a time, whole lines;
 // with a token's heads over the groups a launch touched half lines all over the pages.
 //   append   16384 tokens, 32 heads of 128 bf16, keys normed and rotated, to 4 bits: 268 MB in,
-//            71 out, 70 us, 4.9 TB/s (about 130 with heads over the groups)
+//            71 out, 70 us, 4.9 TB/s (about 130 with heads over the groups); to 8 bits 89, from
+//            32 bits 124 and 139
 //   read     the same back: 71 in, 268 out, 56 us, 6.1 TB/s
-//            147 thousand tokens of 8 heads: 124 in, 602 out, 127 us, 5.7 TB/s (240)
-// Few tokens only wait for memory: 64 of 8 heads 4.4 and 3.1 us.
+//            139 thousand tokens of 8 heads: 151 in, 568 out, 127 us, 5.7 TB/s (240); from 8
+//            bits 143; to 32 bits, where a lane's eight elements are two stores with gaps
+//            of 16 bytes between the lanes', 559, 2.3 TB/s
+// Few tokens only wait for memory: 64 of 8 heads 4.4 and 3.2 us.
 #include "taps_lanes.h"
 #include "taps_mx_device.h"
 #include "taps_mx_internal.h"

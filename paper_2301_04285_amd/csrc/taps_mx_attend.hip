@@ -240,8 +240,8 @@ __device__ __forceinline__ void attend_block(const taps_mx_attend_launch &p, con
 
 // Loads of a wide item's wavefront: a tile's codes wait in registers until the tile before is on its
 // way to LDS, in numbers.  The conversions fall into the phase of the softmax, beside the other half's
-// products: 8 prompts of 2048, 32 heads of 128, 325 us in 4 bits and 336 to 358 in 8 by the card (316 to
-// 349 over a 16-bit cache; 405 without the phases), 512 tokens over 32768 keys 241 to 252 (246).
+// products: 8 prompts of 2048, 32 heads of 128, 325 to 335 us in 4 bits and 335 to 361 in 8 by the card (314 to
+// 349 over a 16-bit cache; 405 without the phases), 512 tokens over 32768 keys 241 to 261 (242 to 252).
 template <class T, int D, int Bits> struct MxLoader {
     static constexpr int kAhead = 1;
     const Keys<T, D, Bits, false> k;
@@ -382,8 +382,10 @@ struct False {
 };
 
 // 16 values as they lie in memory: 16 bytes of codes a lane and load, so that neighbouring lanes share lines.
-// They are not kept in the caches, for nothing else reads them (64 tokens over up to 4000 keys 35.3 us,
-// 39.3 with keys and values kept, 37.0 with neither; two over 131001 54.5, 59.5, 52.3).  Blocks of 32 bytes
+// They are not kept in the caches: only where sequences share pages does another item read them (64 tokens
+// over up to 4000 keys 35.3 us, 39.3 with keys and values kept, 37.0 with neither; two over 131001 54.5, 59.5,
+// 52.3.  64 over 4000 keys of which all share none, 3008, 3968: 51, 40.5, 39.1, with values kept 54, 39.9,
+// 39.0).  Blocks of 32 bytes
 // a lane, in 8 bits, take two loads with half of each line in each, and of heads of 64 leave half of the
 // lanes without: a lone token over 1024 keys 8.7 us, 9.8 so; four tokens each over up to 9999 65 to 66, 66.3.
 // (Keys, whose layout is the product's, in halves of a line a load: 73, the registers do not suffice.)
@@ -705,7 +707,8 @@ __device__ __forceinline__ void attend_few(const taps_mx_attend_launch &p, const
 
 // Four wavefronts an item, three items to a unit; eight where there are no more items than units
 // and a lone one's time counts (16 heads of 64, one token over 1024 keys: 9.8 us for 11.3 when it was chosen; 64
-// tokens over up to 4000, 784 items: 48 for 39).
+// tokens over up to 4000, 784 items: 48 for 39).  The units are those of the whole card, however many a plan
+// was cut for: results do not depend on the choice, times of a part of a card would.
 constexpr uint32_t kUnits = 256;
 
 template <class T, int D, int Bits, int Waves>
@@ -716,8 +719,10 @@ __global__ __launch_bounds__(64 * Waves, Waves == 4 ? 3 : 2) void k_mx_attend_fe
 }
 
 // Any item but a wide one; two fit a unit, three for heads of up to 64.  8 prompts of 1024, 16 heads of
-// 64 in 4 bits: 41 us (32 over a 16-bit cache, whose tiles go past the registers); the conversions and
-// the waits for them at a short item's start are what it has more.
+// 64 in 4 bits: 41 us (34 over a 16-bit cache, whose tiles go past the registers): a third of the
+// wavefronts' time are waits, the matrix cores are busy for 24 % of it.  16 times 8 tokens over 8192 keys, 32
+// heads of 128 over 8, items of 32 rows: 40 and 5 for the join (102 in all over a 16-bit cache), 143 MB at
+// 3.6 TB/s with one tile on its way; keys and values both pass through LDS, in use for 40 % of the time.
 template <class T, int D, int Bits>
 __global__ __launch_bounds__(kThreads, D <= 64 ? 3 : 2) void k_mx_attend(taps_mx_attend_launch p) {
     __shared__ __attribute__((aligned(16))) char lds[max_of(
@@ -732,8 +737,12 @@ __global__ __launch_bounds__(kThreads, D <= 64 ? 3 : 2) void k_mx_attend(taps_mx
         attend_narrow<T, D, Bits>(p, item, head, lds);
 }
 
-// The same with a unit for each: twice the wavefronts share its keys.  Prompts of up to 701 tokens
-// and single ones, 212 items of up to 17 tiles one after the other: 24.8 us, 32.8 without.
+// The same with a unit for each: twice the wavefronts share a block's keys.  Prompts of up to 701 tokens
+// and single ones, 212 items of up to 17 tiles one after the other: 24.7 us, 32.8 without.  Loads,
+// conversions, products and softmax of a tile follow each other: 46 % of the wavefronts' time are waits, a
+// unit's vector instructions issue for 40 % of it, its matrix cores are busy for 19 %.
+// Items of 17 to 32 rows are blocks here, of whose eight wavefronts two have rows: 8 tokens over 8192 keys,
+// 32 heads of 128 over 8, 27 us in 4 bits and 31 in 8 (21 over a 16-bit cache, in narrow items).
 template <class T, int D, int Bits>
 __global__ __launch_bounds__(2 * kThreads, 2) void k_mx_attend_alone(taps_mx_attend_launch p) {
     constexpr int kBlockBytes = max_of(4 * Tile<D>::bytes(kWideKeys), kBlockRows * (D + 8) * 4);
